@@ -356,6 +356,117 @@ bridger_status bridger_forest_packed(bridger_forest_t h, int32_t which, const vo
  * runtime's hold on the converted model (Sec. 4.1).  NULL is a no-op. */
 void bridger_forest_destroy(bridger_forest_t h);
 
+/* ------------------------------------------------------------------ row operators
+ * Operators over rows of scores, logits and features that are used next to a forest: the
+ * largest class scores of a row, the loss of a student model that learns from them, and the
+ * norm and matrix product with which a small dense model answers in 8 bits.  They take no
+ * handle.  Common rules:
+ *   - arrays are device pointers of the device that is current at the call, aligned to their
+ *     element size, row-major; ld* is the distance between two rows in elements, at least the
+ *     row's width (ignored for a single row).  Rows need no further alignment;
+ *   - `dtype` is BRIDGER_F32, BRIDGER_BF16 or BRIDGER_F16; all arithmetic is in 32 bits or
+ *     more, and every output is rounded once, to nearest even;
+ *   - the call is asynchronous on `stream` (NULL = the null stream), allocates nothing, keeps
+ *     nothing and may be captured into a graph; calls may run side by side;
+ *   - n_rows == 0 launches nothing; up to 2^31 - 1 rows;
+ *   - outputs must not overlap inputs or each other, except where stated; elements between
+ *     the rows of an output (ld larger than the width) are left as they were;
+ *   - equal inputs give equal bits, whatever the stream or the other work on the GPU.
+ */
+enum { BRIDGER_F32 = 0, BRIDGER_BF16 = 1, BRIDGER_F16 = 2 };
+
+/*
+ * The k largest of every row's n_classes scores, largest first, with their class ids (Table
+ * 4's topk; predict_labels is its k = 1).  Of equal scores (-0 and +0 are equal) the lower
+ * class comes first; a NaN comes after every number.  The values are the scores' own bits.
+ * Slots beyond n_classes hold -infinity and the id -1.
+ *   scores  [n_rows, n_classes], 1 <= n_classes < 2^31
+ *   k       1 <= k <= BRIDGER_MAX_TOP
+ *   values  [n_rows, k] of the scores' dtype, or NULL;  ids  int32 [n_rows, k], or NULL
+ *           (not both NULL); both without gaps between rows
+ */
+#define BRIDGER_MAX_TOP 256
+bridger_status bridger_top_k(const void *scores, int64_t ld, int32_t dtype, int64_t n_rows,
+                             int32_t n_classes, int32_t k, void *values, int32_t *ids,
+                             void *stream);
+
+/*
+ * Distillation from a teacher's largest logits: the divergence of a student's class
+ * distribution from the teacher's over the classes that the teacher kept.  Per row, with z the
+ * student's n_classes logits, (ids, t) the teacher's k kept classes and their logits, and T the
+ * temperature:
+ *     p = softmax(t / T) over the filled slots,  log q = z / T - logsumexp(z / T),
+ *     loss = T^2 sum_i p_i (log p_i - log q[ids_i]),
+ *     grad_j = weight * d loss / d z_j = weight * T (q_j - sum of the p_i with ids_i = j).
+ * A slot is filled when its id lies in [0, n_classes); others (-1) are ignored.  An id that
+ * stands in several slots gets the sum of their p.  A row without a filled slot, or whose
+ * filled slots are all -infinity, has loss 0 and gradient 0, whatever z holds.  Classes with
+ * z = -infinity have q = 0; a teacher that wants one (p > 0) makes the loss +infinity.  A NaN,
+ * or +infinity, in a row's logits makes its loss and gradient NaN.
+ *   logits       [n_rows, n_classes] of dtype, rows ldl apart; 1 <= n_classes < 2^31
+ *   ids          int32 [n_rows, k];  teacher  [n_rows, k] of teacher_dtype, both without gaps
+ *                (what bridger_top_k writes); 1 <= k <= BRIDGER_MAX_TOP
+ *   temperature  between 1e-6 and 1e6
+ *   weight       float [n_rows]: the derivative of what is trained by each row's loss; NULL = 1
+ *   loss         float [n_rows], or NULL
+ *   stats        float [n_rows, 2] for bridger_distill_backward, or NULL
+ *   grad         [n_rows, n_classes] of dtype, rows ldg apart, or NULL; may be logits itself
+ *                (with ldg = ldl)
+ * With grad, loss and gradient take one pass over the logits where a row fits a workgroup's
+ * registers.  At least one output is given.
+ */
+bridger_status bridger_distill(const void *logits, int64_t ldl, int32_t dtype, const int32_t *ids,
+                               const void *teacher, int32_t teacher_dtype, int64_t n_rows,
+                               int32_t n_classes, int32_t k, float temperature,
+                               const float *weight, float *loss, float *stats, void *grad,
+                               int64_t ldg, void *stream);
+
+/* The gradient alone, from the stats that bridger_distill wrote for the same logits, teacher
+ * and temperature (for callers whose weights are known only after the loss). */
+bridger_status bridger_distill_backward(const void *logits, int64_t ldl, int32_t dtype,
+                                        const int32_t *ids, const void *teacher,
+                                        int32_t teacher_dtype, int64_t n_rows, int32_t n_classes,
+                                        int32_t k, float temperature, const float *stats,
+                                        const float *weight, void *grad, int64_t ldg,
+                                        void *stream);
+
+/*
+ * Root-mean-square norm to 8 bits, with a residual added first:
+ *     s = x + residual,  y_j = s_j weight_j / sqrt(mean_j(s_j^2) + eps),
+ *     scale = max_j |y_j| / 127,  q_j = y_j / scale rounded to nearest even, in [-127, 127].
+ * The norm takes the sums s before their rounding to dtype.  A row of zeros has scale 0 and
+ * q = 0; a row with a NaN or an infinity in s or y (taken in float) has scale NaN and q = 0, so
+ * that a product with it is NaN.
+ *   x         [n_rows, n_features] of dtype, rows ldx apart; 1 <= n_features < 2^31
+ *   residual  as x, rows ldr apart, or NULL (s = x)
+ *   weight    [n_features] of dtype, or NULL (ones);  eps  finite, >= 0
+ *   total     receives s, of dtype, rows ldt apart, or NULL; may be x or residual itself (with
+ *             the same distance of rows)
+ *   q         int8 [n_rows, n_features], rows ldq apart;  scale  float [n_rows]
+ */
+bridger_status bridger_rmsnorm_q8(const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                                  const void *weight, int32_t dtype, int64_t n_rows,
+                                  int32_t n_features, float eps, void *total, int64_t ldt,
+                                  int8_t *q, int64_t ldq, float *scale, void *stream);
+
+/*
+ * Matrix product of 8-bit rows and 8-bit weights, with a scale for each of both (Table 4's
+ * matmul):
+ *     out[r, o] = a_scale[r] * b_scale[o] * sum_j a[r, j] * b[o, j]  (+ bias[o]).
+ * The sum is exact (32-bit integers).
+ *   a  int8 [n_rows, n_features], rows lda apart;  a_scale  float [n_rows]
+ *   b  int8 [n_outputs, n_features], rows ldb apart;  b_scale  float [n_outputs]
+ *   bias  float [n_outputs], or NULL
+ *   out   [n_rows, n_outputs] of dtype, rows ldo apart
+ * 1 <= n_features <= BRIDGER_MATMUL_Q8_MAX_FEATURES, beyond which a sum could leave 32 bits.
+ */
+#define BRIDGER_MATMUL_Q8_MAX_FEATURES 131071
+bridger_status bridger_matmul_q8(const int8_t *a, int64_t lda, const float *a_scale,
+                                 const int8_t *b, int64_t ldb, const float *b_scale,
+                                 const float *bias, int64_t n_rows, int32_t n_outputs,
+                                 int32_t n_features, int32_t dtype, void *out, int64_t ldo,
+                                 void *stream);
+
 /* Message for the calling thread's most recent failed call ("" if none).  The
  * paper states no error interface; this is the library's own, so that nothing
  * throws across the C ABI (thread-local storage, valid until the thread's next

@@ -98,6 +98,7 @@ def load_library(path: Optional[str] = None):
                  "bridger_forest_predict_labels", "bridger_forest_predict_csr",
                  "bridger_forest_predict_csr_leaves"):
         getattr(lib, name).restype = ctypes.c_int
+    operators.declare(lib)
     if path is None:
         _lib = lib
     return lib
@@ -343,6 +344,11 @@ class Forest:
                                       out.data_ptr(), stream)
         return out
 
+    def predict_top(self, X, k: int, values=None, ids=None):
+        """The k largest outputs of every row, largest first, and their classes (predict, then
+        top_k): a teacher's scores for distill.  With the identity transform they are logits."""
+        return operators.top_k(self.predict(X), k, values, ids)
+
     def predict_leaves(self, X, out=None):
         import torch
         self._check_x(X)
@@ -421,3 +427,10 @@ class Forest:
 
     def __exit__(self, *exc):
         self.close()
+
+
+from . import operators  # noqa: E402  (uses load_library and _check)
+from .operators import (  # noqa: E402,F401
+    BRIDGER_BF16, BRIDGER_F16, BRIDGER_F32, BRIDGER_MATMUL_Q8_MAX_FEATURES, BRIDGER_MAX_TOP,
+    bridger_distill, bridger_distill_backward, bridger_matmul_q8, bridger_rmsnorm_q8,
+    bridger_top_k, distill, distill_loss, matmul_q8, rmsnorm_q8, top_k)

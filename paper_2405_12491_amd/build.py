@@ -21,7 +21,8 @@ SOURCES = [os.path.join(CSRC, n) for n in
            ("bridger_host.cpp", "perfect.hip", "perfect_binned.hip", "perfect_fixed.hip",
             "perfect_global.hip", "ragged.hip", "ragged_heap5.hip", "ragged_heap6.hip",
             "ragged_heap7.hip", "direct.hip", "gemm.hip", "bin.hip",
-            "normalize.hip")]
+            "normalize.hip", "operators.cpp", "top_k.hip", "distill.hip", "rmsnorm_q8.hip",
+            "matmul_q8.hip")]
 # Sources compiled once per value of a macro (one trees' depth each: their kernels are many), and
 # once without it; every other source once.
 UNITS = {"perfect_global.hip": ["BRIDGER_DEPTH=%d" % d for d in range(10, 0, -1)]}

@@ -23,12 +23,33 @@
 
 #include "bridger.h"
 #include "internal.h"
+#include "operators.h"
 
 using namespace bridger;
 
 namespace {
 
 thread_local std::string g_last_error;
+
+}  // namespace
+
+namespace bridger {
+
+// operators.cpp reports through the same message (a message that cannot be stored is left out).
+bridger_status report_error(bridger_status s, const char *msg) {
+  try {
+    g_last_error = msg;
+  } catch (const std::bad_alloc &) {
+    g_last_error.clear();
+  }
+  return s;
+}
+
+void clear_error() { g_last_error.clear(); }
+
+}  // namespace bridger
+
+namespace {
 
 bridger_status fail(bridger_status s, const std::string &msg) {
   g_last_error = msg;

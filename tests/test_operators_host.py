@@ -1,0 +1,137 @@
+"""What the row operators refuse, and that they refuse it before any launch: through the C ABI with
+addresses that nothing reads, on a machine without a GPU."""
+import ctypes
+import re
+
+import pytest
+
+import paper_2405_12491_amd as B
+from paper_2405_12491_amd import operators as O
+
+ARG, UNS, DEV = B.BRIDGER_ERR_INVALID_ARGUMENT, B.BRIDGER_ERR_UNSUPPORTED, B.BRIDGER_ERR_DEVICE
+NONE = None
+A = [(i + 1) << 40 for i in range(8)]     # eight far addresses
+
+
+def _status(fn, args, **change):
+    args = dict(args, **change)
+    st = getattr(B.load_library(), fn)(*args.values())
+    return st
+
+
+TOP = dict(scores=A[0], ld=10, dtype=0, n=5, classes=10, k=3, values=A[1], ids=A[2], stream=NONE)
+DIS = dict(logits=A[0], ldl=10, dtype=0, ids=A[1], teacher=A[2], teacher_dtype=0, n=5, classes=10,
+           k=3, temperature=1.0, weight=A[3], loss=A[4], stats=A[5], grad=A[6], ldg=10, stream=NONE)
+BWD = dict(logits=A[0], ldl=10, dtype=0, ids=A[1], teacher=A[2], teacher_dtype=0, n=5, classes=10,
+           k=3, temperature=1.0, stats=A[5], weight=A[3], grad=A[6], ldg=10, stream=NONE)
+NRM = dict(x=A[0], ldx=10, residual=A[1], ldr=10, weight=A[2], dtype=0, n=5, features=10, eps=1e-6,
+           total=A[3], ldt=10, q=A[4], ldq=10, scale=A[5], stream=NONE)
+MUL = dict(a=A[0], lda=10, a_scale=A[1], b=A[2], ldb=10, b_scale=A[3], bias=A[4], n=5, outputs=6,
+           features=10, dtype=0, out=A[5], ldo=6, stream=NONE)
+FNS = {"bridger_top_k": TOP, "bridger_distill": DIS, "bridger_distill_backward": BWD,
+       "bridger_rmsnorm_q8": NRM, "bridger_matmul_q8": MUL}
+inf, nan = float("inf"), float("nan")
+
+REFUSED = [
+    ("bridger_top_k", c, ARG) for c in (
+        dict(scores=NONE), dict(values=NONE, ids=NONE), dict(dtype=3), dict(dtype=-1), dict(n=-1),
+        dict(n=1 << 31), dict(classes=0), dict(classes=-4), dict(k=0), dict(k=257), dict(ld=9),
+        dict(ld=-10), dict(ld=1 << 62), dict(scores=A[0] + 2), dict(scores=A[0] + 1, dtype=1),
+        dict(values=A[1] + 3), dict(ids=A[2] + 2), dict(values=A[0]), dict(ids=A[0] + 4 * 49),
+        dict(values=A[2]), dict(values=A[2] + 4 * 14), dict(n=1 << 30, ld=1 << 60))
+] + [
+    (fn, c, ARG) for fn in ("bridger_distill", "bridger_distill_backward") for c in (
+        dict(logits=NONE), dict(ids=NONE), dict(teacher=NONE), dict(dtype=3), dict(teacher_dtype=9),
+        dict(n=-1), dict(n=1 << 31), dict(classes=0), dict(k=0), dict(k=257), dict(temperature=0.0),
+        dict(temperature=-1.0), dict(temperature=nan), dict(temperature=inf),
+        dict(temperature=1e-7), dict(temperature=1e7), dict(ldl=9), dict(ldg=9),
+        dict(logits=A[0] + 2), dict(ids=A[1] + 1), dict(teacher=A[2] + 1, teacher_dtype=1),
+        dict(weight=A[3] + 1), dict(grad=A[6] + 2), dict(grad=A[0] + 4), dict(grad=A[0], ldg=11),
+        dict(grad=A[1]), dict(grad=A[2] + 8), dict(grad=A[3] + 16), dict(stats=A[5] + 2))
+] + [
+    ("bridger_distill", c, ARG) for c in (
+        dict(loss=NONE, stats=NONE, grad=NONE), dict(loss=A[0]), dict(loss=A[5]), dict(stats=A[6]),
+        dict(loss=A[3]), dict(stats=A[1]))
+] + [
+    ("bridger_distill_backward", c, ARG) for c in (
+        dict(stats=NONE), dict(grad=NONE), dict(grad=A[5]))
+] + [
+    ("bridger_rmsnorm_q8", c, ARG) for c in (
+        dict(x=NONE), dict(q=NONE), dict(scale=NONE), dict(dtype=4), dict(n=-2), dict(features=0),
+        dict(eps=-1e-9), dict(eps=nan), dict(eps=inf), dict(ldx=9), dict(ldr=9), dict(ldt=9),
+        dict(ldq=9), dict(x=A[0] + 1), dict(residual=A[1] + 2), dict(weight=A[2] + 1),
+        dict(total=A[3] + 2), dict(scale=A[5] + 1), dict(total=A[0] + 4), dict(total=A[0], ldt=12),
+        dict(q=A[0]), dict(q=A[0] + 199), dict(q=A[3]), dict(scale=A[4]), dict(q=A[2] + 39),
+        dict(scale=A[1] + 8))
+] + [
+    ("bridger_matmul_q8", c, ARG) for c in (
+        dict(a=NONE), dict(a_scale=NONE), dict(b=NONE), dict(b_scale=NONE), dict(out=NONE),
+        dict(dtype=3), dict(n=-1), dict(outputs=0), dict(features=0), dict(lda=9), dict(ldb=9),
+        dict(ldo=5), dict(a_scale=A[1] + 1), dict(b_scale=A[3] + 2), dict(bias=A[4] + 1),
+        dict(out=A[5] + 2), dict(out=A[0]), dict(out=A[2] + 56), dict(out=A[1] + 16), dict(out=A[4]))
+] + [("bridger_matmul_q8", dict(features=131072, lda=131072, ldb=131072), UNS)]
+
+
+@pytest.mark.parametrize("case", range(len(REFUSED)))
+def test_refused(case):
+    fn, change, status = REFUSED[case]
+    assert _status(fn, FNS[fn], **change) == status, (fn, change)
+    assert B.bridger_last_error(), (fn, change)
+
+
+# sound calls reach the device: without one the answer is DEVICE.  Run where no GPU is present.
+SOUND = [("bridger_top_k", c) for c in (
+    dict(), dict(values=NONE), dict(ids=NONE), dict(k=256), dict(ld=1 << 30), dict(scores=A[0] + 2, dtype=1),
+    dict(n=1, ld=0), dict(ids=A[0] + 4 * 50), dict(scores=A[0], ld=16, values=A[0] + 40, k=16, classes=10, n=1))] + [
+    ("bridger_distill", c) for c in (
+        dict(), dict(weight=NONE), dict(loss=NONE), dict(stats=NONE, grad=NONE), dict(grad=A[0]),
+        dict(ldl=24, grad=A[0] + 48, ldg=24))] + [
+    ("bridger_distill_backward", c) for c in (dict(), dict(weight=NONE), dict(grad=A[0]))] + [
+    ("bridger_rmsnorm_q8", c) for c in (
+        dict(), dict(residual=NONE), dict(weight=NONE), dict(total=NONE), dict(total=A[0]),
+        dict(total=A[1]), dict(eps=0.0), dict(residual=A[0]), dict(ldx=20, total=A[0] + 40, ldt=20))] + [
+    ("bridger_matmul_q8", c) for c in (dict(), dict(bias=NONE), dict(b=A[0], a_scale=A[1]),
+                                       dict(features=131071, lda=131071, ldb=131071))]
+
+
+@pytest.mark.parametrize("case", range(len(SOUND)))
+def test_sound_arguments_pass_the_checks(case):
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("these addresses must not reach a GPU")
+    fn, change = SOUND[case]
+    assert _status(fn, FNS[fn], **change) == DEV, (fn, change, B.bridger_last_error())
+
+
+def test_no_rows_need_no_device():
+    for fn, args in FNS.items():
+        assert _status(fn, args, n=0) == B.BRIDGER_OK
+        assert B.bridger_last_error() == ""
+
+
+def test_constants_are_the_header_s():
+    import os
+    text = open(os.path.join(os.path.dirname(O.__file__), "..", "include", "bridger.h")).read()
+    for name in ("BRIDGER_MAX_TOP", "BRIDGER_MATMUL_Q8_MAX_FEATURES"):
+        assert int(re.search(r"#define %s (\d+)" % name, text).group(1)) == getattr(B, name)
+    assert re.search(r"BRIDGER_F32 = 0, BRIDGER_BF16 = 1, BRIDGER_F16 = 2", text)
+    assert (B.BRIDGER_F32, B.BRIDGER_BF16, B.BRIDGER_F16) == (0, 1, 2)
+
+
+def test_cpu_tensors_are_refused():
+    import torch
+    x = torch.zeros(3, 8)
+    ids, t, v = torch.zeros(3, 2, dtype=torch.int32), torch.zeros(3, 2), torch.ones(3)
+    q = torch.zeros(3, 8, dtype=torch.int8)
+    for call in (lambda: B.top_k(x, 2), lambda: B.distill(x, ids, t), lambda: B.distill_loss(x, ids, t),
+                 lambda: B.rmsnorm_q8(x), lambda: B.matmul_q8(q, v, q, v), lambda: B.top_k([1.0], 1),
+                 lambda: B.distill([[1.0]], ids, t)):
+        with pytest.raises(TypeError):
+            call()
+
+
+def test_raw_call_reports_its_error():
+    with pytest.raises(B.BridgerError) as e:
+        B.bridger_top_k(A[0], 9, 0, 5, 10, 3, A[1], A[2])
+    assert e.value.status == ARG and "distance between rows" in str(e.value)
+    assert isinstance(B.load_library().bridger_top_k, ctypes._CFuncPtr)
