@@ -3,110 +3,381 @@
 
 namespace bridger {
 
-constexpr int kThreads = 256;
+// With M = max z, e_j = exp((z_j - M) / T) and S = sum e_j:  q_j = e_j / S,
+// loss = T^2 sum_i p_i (log p_i - (z_i - M) / T + log S),  grad_j = w T (q_j - p_j).
+// z - M is formed before the division by T, so that neither overflows and exponents are at most 0;
+// exp goes through exp2, 1 / T and log2(e) in one factor that is rounded once.  Every lane keeps the
+// largest of its own logits and the sum relative to it; those pairs are joined across the row's
+// lanes at once.  The gradient is first w T q everywhere; the few kept classes are then written
+// again with their p taken off, by the row's first wave.
+constexpr int kSlots = 4;  // a lane's share of the teacher's slots, lanes of one wave at most
 
-// A row's teacher: p = softmax(t / T) over the filled slots, thread i holding slot i.
-struct Teacher {
-  bool any;       // a filled slot above -infinity
-  int32_t id;     // -1: not filled
-  float p, logp;  // of this thread's slot (p = 0 where not filled)
+template <int G>
+constexpr int kSlotLanes = G < 64 ? G : 64;
+
+struct Slots {
+  int32_t id[kSlots];  // -1: not filled
+  float z[kSlots], p[kSlots];
+  float kl;  // this lane's sum of p log p
+  bool any;  // some slot of the row is filled above -infinity
 };
 
-template <typename U, int WAVES>
-__device__ inline Teacher load_teacher(const DistillArgs &a, int64_t row, float *lds) {
-  Teacher s = {false, -1, 0.0f, 0.0f};
-  const int i = threadIdx.x;
-  float t = -__builtin_inff();
-  if (i < a.k) {
-    const int32_t id = a.ids[row * a.k + i];
-    if (id >= 0 && id < a.n_classes) {
-      s.id = id;
-      t = to_float(((const U *)a.teacher)[row * a.k + i]);
+__device__ inline float teacher_at(const DistillArgs &a, int64_t at) {
+  if (a.teacher_dtype == BRIDGER_F32) return ((const float *)a.teacher)[at];
+  if (a.teacher_dtype == BRIDGER_BF16) return to_float(((const __bf16 *)a.teacher)[at]);
+  return to_float(((const _Float16 *)a.teacher)[at]);
+}
+
+// p = softmax(t / T) over the row's filled slots; slot s L + l is lane l's.
+template <typename T, int G>
+__device__ inline Slots load_slots(const DistillArgs &a, int64_t row, const T *z, int lane) {
+  constexpr int L = kSlotLanes<G>;
+  const float inf = __builtin_inff();
+  Slots s;
+  float t[kSlots], most = -inf;
+  int any = 0;
+#pragma unroll
+  for (int i = 0; i < kSlots; ++i) {
+    const int at = i * L + lane;
+    s.id[i] = -1;
+    s.z[i] = 0.0f;
+    t[i] = -inf;
+    if (at < a.k) {
+      const int32_t id = a.ids[row * a.k + at];
+      const float v = teacher_at(a, row * a.k + at);
+      if (id >= 0 && id < a.n_classes) {
+        s.id[i] = id;
+        s.z[i] = to_float(z[id]);
+        t[i] = v;
+        any |= v != -inf;  // NaN is not
+      }
     }
+    most = fmaxf(most, t[i]);
   }
-  s.any = __syncthreads_or(s.id >= 0 && t != -__builtin_inff());
-  float most = block_reduce<Max, WAVES>(t, lds);
-  if (most == -__builtin_inff()) most = 0.0f;  // nothing but NaN, or an empty row
-  const float u = (t - most) / a.temperature;
-  const float e = s.id >= 0 ? __expf(u) : 0.0f;
-  const float mass = block_reduce<Sum, WAVES>(e, lds);
-  s.p = e / mass;
-  s.logp = u - __logf(mass);
+  s.any = lanes_reduce<Max, L>(any) != 0;
+  most = lanes_reduce<Max, L>(most);
+  if (most == -inf) most = 0.0f;  // an empty row, or nothing but NaN
+  float mass = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kSlots; ++i) {
+    t[i] = (t[i] - most) / a.temperature;
+    s.p[i] = s.id[i] >= 0 ? __expf(t[i]) : 0.0f;
+    mass += s.p[i];
+  }
+  mass = lanes_reduce<Sum, L>(mass);
+  const float log_mass = __logf(mass);
+  s.kl = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kSlots; ++i) {
+    s.p[i] /= mass;
+    if (s.id[i] >= 0 && s.p[i] != 0.0f) s.kl += s.p[i] * (t[i] - log_mass);
+  }
   return s;
 }
 
-// One workgroup a row.  z - max(z) is formed before the division by T, so that neither overflows;
-// exponents are at most 0.
-template <typename T, typename U, bool BACKWARD>
-__global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a) {
-  constexpr int W = kThreads / 64;
-  __shared__ float lds[W];
-  __shared__ int32_t slot_id[BRIDGER_MAX_TOP];
-  __shared__ float slot_p[BRIDGER_MAX_TOP];
-  const float inf = __builtin_inff();
-  const float T_ = a.temperature;
-  for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
-    const T *z = (const T *)a.logits + row * a.ldl;
-    T *grad = a.grad ? (T *)a.grad + row * a.ldg : nullptr;
-    const Teacher s = load_teacher<U, W>(a, row, lds);
-    const int i = threadIdx.x;
-    const float z_id = s.id >= 0 ? to_float(z[s.id]) : 0.0f;
-    float most, mass;
-    if (BACKWARD) {
-      most = a.stats[2 * row];
-      mass = a.stats[2 * row + 1];
-    } else {
-      float v = -inf;
-      for (int64_t j = i; j < a.n_classes; j += kThreads) v = fmaxf(v, to_float(z[j]));
-      most = block_reduce<Max, W>(v, lds);
-      if (most == -inf) most = 0.0f;
-      v = 0.0f;
-      for (int64_t j = i; j < a.n_classes; j += kThreads)
-        v += __expf((to_float(z[j]) - most) / T_);
-      mass = block_reduce<Sum, W>(v, lds);
-      const float log_q = z_id == -inf ? -inf : (z_id - most) / T_ - __logf(mass);
-      v = s.id >= 0 && s.p != 0.0f ? s.p * (s.logp - log_q) : 0.0f;
-      v = block_reduce<Sum, W>(v, lds);
-      if (i == 0) {
-        if (a.loss) a.loss[row] = s.any ? T_ * T_ * v : 0.0f;
-        if (a.stats) {
-          a.stats[2 * row] = most;
-          a.stats[2 * row + 1] = mass;
+// Of slots that hold one class, the first takes the sum of their p, in slot order, and the others
+// are emptied.  `ids` and `ps`: the row's kSlots L slots, written and read by this wave.
+template <int G>
+__device__ inline void join_equal(const DistillArgs &a, Slots &s, int lane, int32_t *ids, float *ps) {
+  constexpr int L = kSlotLanes<G>;
+#pragma unroll
+  for (int i = 0; i < kSlots; ++i) {
+    ids[i * L + lane] = s.id[i];
+    ps[i * L + lane] = s.p[i];
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  int equal[kSlots] = {};
+  for (int q = 0; q < a.k; q += 4) {  // entries past k are -1, as are those not filled
+    const int4 other = *(const int4 *)(ids + q);
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i)
+      equal[i] += (other.x == s.id[i]) + (other.y == s.id[i]) + (other.z == s.id[i]) +
+                  (other.w == s.id[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kSlots; ++i)
+    if (s.id[i] >= 0 && equal[i] > 1) {
+      float p = 0.0f;
+      bool first = true;
+      for (int q = 0; q < a.k; ++q)
+        if (ids[q] == s.id[i]) {
+          p += ps[q];
+          first &= q >= i * L + lane;
         }
-      }
+      s.p[i] = p;
+      if (!first) s.id[i] = -1;
     }
-    if (grad) {
-      const float w = s.any ? T_ * (a.weight ? a.weight[row] : 1.0f) : 0.0f;
-      const float per = mass == 0.0f ? 0.0f : 1.0f / mass;
-      __syncthreads();
-      if (i < a.k) {
-        slot_id[i] = s.id;
-        slot_p[i] = s.p;
-      }
-      __syncthreads();  // also: every slot's logit is read before the gradient may overwrite it
-      for (int64_t j = i; j < a.n_classes; j += kThreads)
-        grad[j] = from_float<T>(s.any ? w * (__expf((to_float(z[j]) - most) / T_) * per) : 0.0f);
-      __syncthreads();
-      if (s.any && s.id >= 0) {  // equal ids: every one of them writes the same value
-        float p = 0.0f;
-        for (int q = 0; q < a.k; ++q)
-          if (slot_id[q] == s.id) p += slot_p[q];
-        grad[s.id] = from_float<T>(w * (__expf((z_id - most) / T_) * per - p));
-      }
+}
+
+// What a row's lanes share: the largest logit, the sum of the exponentials, and whether the row has
+// a teacher.
+struct RowStats {
+  float most, mass;
+  bool any;
+};
+
+// most and mass: a lane's; they are joined over the row.  The barrier between the waves of a row
+// also makes `any`, which the first wave knows, known to all.
+template <int G>
+__device__ inline RowStats join_stats(float most, float mass, bool any, float factor, float2 *lds,
+                                      int *lds_any) {
+  const float inf = __builtin_inff();
+  float all = lanes_reduce<Max, G>(most);
+  float safe = all == -inf ? 0.0f : all;
+  mass = lanes_reduce<Sum, G>(mass * __builtin_amdgcn_exp2f((most - safe) * factor));
+  if constexpr (G > 64) {
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) lds[wave] = make_float2(all, mass);
+    if (threadIdx.x == 0) *lds_any = any;
+    __syncthreads();
+    const float2 w = lds[threadIdx.x & (G / 64 - 1)];
+    all = lanes_reduce<Max, G / 64>(w.x);
+    safe = all == -inf ? 0.0f : all;
+    mass = lanes_reduce<Sum, G / 64>(w.y * __builtin_amdgcn_exp2f((w.x - safe) * factor));
+    any = *lds_any != 0;
+  }
+  return {safe, mass, any};
+}
+
+__device__ inline float factor_of(float temperature) {
+  return (float)(1.4426950408889634 / (double)temperature);
+}
+
+// The first wave's part after the row's sums: the loss, the stats.
+template <int G>
+__device__ inline void store_loss(const DistillArgs &a, int64_t row, const Slots &s,
+                                  const RowStats &r, int lane) {
+  const float inf = __builtin_inff();
+  const float log_mass = __logf(r.mass);
+  float v = s.kl;
+#pragma unroll
+  for (int i = 0; i < kSlots; ++i)
+    if (s.id[i] >= 0 && s.p[i] != 0.0f) {
+      const float log_q = s.z[i] == -inf ? -inf : (s.z[i] - r.most) / a.temperature - log_mass;
+      v -= s.p[i] * log_q;
+    }
+  v = lanes_reduce<Sum, kSlotLanes<G>>(v);
+  if (lane == 0) {
+    if (a.loss) a.loss[row] = s.any ? a.temperature * a.temperature * v : 0.0f;
+    if (a.stats) {
+      a.stats[2 * row] = r.most;
+      a.stats[2 * row + 1] = r.mass;
     }
   }
 }
 
-int launch_distill(const DistillArgs &a, int32_t dtype, int32_t teacher_dtype, bool backward,
-                   void *stream) {
-  static_assert(kThreads >= BRIDGER_MAX_TOP, "a thread for each slot");
+// Gradient of the kept classes, over what the whole row's lanes have written.
+template <typename T>
+__device__ inline void store_kept(T *grad, const Slots &s, const RowStats &r, float factor,
+                                  float weight, float per) {
+#pragma unroll
+  for (int i = 0; i < kSlots; ++i)
+    if (s.any && s.id[i] >= 0) {
+      const float e = __builtin_amdgcn_exp2f((s.z[i] - r.most) * factor);
+      grad[s.id[i]] = from_float<T>(weight * (e * per - s.p[i]));
+    }
+}
+
+// G lanes a row, C loads a lane: the logits stay in registers between the sum and the gradient, so
+// loss and gradient cost one read and one write of the row.
+template <typename T, int G, int C, bool TINY, bool BACKWARD>
+__global__ __launch_bounds__(kRowThreads<G>, C <= 4 ? 8 : 4) void distill_kernel(DistillArgs a) {
+  constexpr int V = kPerLoad<T>, L = kSlotLanes<G>, W = G > 64 ? G / 64 : 1;
+  __shared__ float2 lds[W];
+  __shared__ int lds_any;
+  __shared__ __attribute__((aligned(16))) int32_t slot_id[kRowsAWorkgroup<G> * L * kSlots];
+  __shared__ float slot_p[kRowsAWorkgroup<G> * L * kSlots];
+  const int lane = threadIdx.x & (G - 1), n = a.n_classes;
+  const int64_t row = row_of<G>(a.first);
+  if (row >= a.n_rows) return;
+  const T *z = (const T *)a.logits + row * a.ldl;
+  const float inf = __builtin_inff(), factor = factor_of(a.temperature);
+  RowLoad<T> x[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int j = (c * G + lane) * V;
+    if constexpr (TINY) {
+      x[c].tiny(z, j, n, (T)-inf);
+    } else {
+      x[c].issue(z, j, n);
+    }
+  }
+  const bool first_wave = G <= 64 || threadIdx.x < 64;
+  const int slots_at = threadIdx.x / G * L * kSlots;
+  Slots s;
+  s.any = false;
+  if (first_wave) {
+    s = load_slots<T, G>(a, row, z, lane);
+    join_equal<G>(a, s, lane, slot_id + slots_at, slot_p + slots_at);
+    // the gradient may take the logits' place: they are here before any is stored
+    asm volatile("" ::"v"(s.z[0]), "v"(s.z[1]), "v"(s.z[2]), "v"(s.z[3]));
+  }
+  float most = -inf, mass = 0.0f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    if constexpr (!TINY) x[c].take((c * G + lane) * V, n, fill_of((T)-inf));
+    if constexpr (BACKWARD) forget(x[c].raw);  // here before any gradient is stored
+    if constexpr (!BACKWARD) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) most = fmaxf(most, element<T>(x[c].raw, i));
+    }
+  }
+  RowStats r;
+  if constexpr (BACKWARD) {
+    if constexpr (G > 64) {
+      if (threadIdx.x == 0) lds_any = s.any;
+      __syncthreads();
+      s.any = lds_any != 0;
+    }
+    r = {a.stats[2 * row], a.stats[2 * row + 1], s.any};
+  } else {
+    const float safe = most == -inf ? 0.0f : most;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      forget(x[c].raw);
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        mass += __builtin_amdgcn_exp2f((element<T>(x[c].raw, i) - safe) * factor);
+    }
+    r = join_stats<G>(most, mass, s.any, factor, lds, &lds_any);
+    s.any = r.any;
+    if (first_wave) store_loss<G>(a, row, s, r, lane);
+  }
+  if (!a.grad) return;
+  T *grad = (T *)a.grad + row * a.ldg;
+  const float weight = r.any ? a.temperature * (a.weight ? a.weight[row] : 1.0f) : 0.0f;
+  const float per = r.mass == 0.0f ? 0.0f : 1.0f / r.mass;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int j = (c * G + lane) * V;
+    if (j >= n) break;
+    forget(x[c].raw);
+    float v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float e = __builtin_amdgcn_exp2f((element<T>(x[c].raw, i) - r.most) * factor);
+      v[i] = r.any ? weight * (e * per) : 0.0f;
+    }
+    store16<T>(grad + j, n - j, v);
+  }
+  if constexpr (G > 64) {
+    __syncthreads();
+  } else {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+    __builtin_amdgcn_wave_barrier();
+  }
+  if (first_wave) store_kept<T>(grad, s, r, factor, weight, per);
+}
+
+// Rows that do not fit a workgroup's registers: one walk for the sums, one for the gradient.
+template <typename T, bool BACKWARD>
+__global__ __launch_bounds__(1024) void distill_long_kernel(DistillArgs a) {
+  constexpr int G = 1024, V = kPerLoad<T>, L = 64, U = 4;
+  __shared__ float2 lds[G / 64];
+  __shared__ int lds_any;
+  __shared__ __attribute__((aligned(16))) int32_t slot_id[L * kSlots];
+  __shared__ float slot_p[L * kSlots];
+  const int lane = threadIdx.x, n = a.n_classes;
+  const int64_t row = row_of<G>(a.first);
+  const T *z = (const T *)a.logits + row * a.ldl;
+  const float inf = __builtin_inff(), factor = factor_of(a.temperature);
+  const int whole = n / V * V;  // the row's whole loads; the elements past them are lanes' own
+  Slots s;
+  s.any = false;
+  if (lane < 64) {
+    s = load_slots<T, G>(a, row, z, lane);
+    join_equal<G>(a, s, lane, slot_id, slot_p);
+    asm volatile("" ::"v"(s.z[0]), "v"(s.z[1]), "v"(s.z[2]), "v"(s.z[3]));
+  }
+  RowStats r;
+  if constexpr (BACKWARD) {
+    if (lane == 0) lds_any = s.any;
+    __syncthreads();
+    s.any = lds_any != 0;
+    r = {a.stats[2 * row], a.stats[2 * row + 1], s.any};
+  } else {
+    float most = whole + lane < n ? to_float(z[whole + lane]) : -inf;
+    float mass = most == -inf ? 0.0f : 1.0f;
+    if (most != most || most == inf) mass = __builtin_nanf("");
+    for (int64_t j = (int64_t)lane * V; j < whole; j += (int64_t)G * V * U) {
+      u32x4 raw[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (j + u * G * V < whole) {
+          __builtin_memcpy(&raw[u], z + j + u * G * V, 16);
+        } else {
+          const uint32_t f = fill_of((T)-inf);
+          raw[u] = u32x4{f, f, f, f};
+        }
+      float top = most;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < V; ++i) top = fmaxf(top, element<T>(raw[u], i));
+      const float safe = top == -inf ? 0.0f : top;
+      mass *= __builtin_amdgcn_exp2f((most - safe) * factor);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          mass += __builtin_amdgcn_exp2f((element<T>(raw[u], i) - safe) * factor);
+      most = top;
+    }
+    if (most != most) most = -inf;  // NaN is in the mass
+    r = join_stats<G>(most, mass, s.any, factor, lds, &lds_any);
+    s.any = r.any;
+    if (lane < 64) store_loss<G>(a, row, s, r, lane);
+  }
+  if (!a.grad) return;
+  T *grad = (T *)a.grad + row * a.ldg;
+  const float weight = r.any ? a.temperature * (a.weight ? a.weight[row] : 1.0f) : 0.0f;
+  const float per = r.mass == 0.0f ? 0.0f : 1.0f / r.mass;
+  auto grad_of = [&](float x) {
+    return r.any ? weight * (__builtin_amdgcn_exp2f((x - r.most) * factor) * per) : 0.0f;
+  };
+#pragma unroll 4
+  for (int64_t j = (int64_t)lane * V; j < whole; j += G * V) {
+    u32x4 raw;
+    __builtin_memcpy(&raw, z + j, 16);
+    float v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = grad_of(element<T>(raw, i));
+    store16<T>(grad + j, V, v);
+  }
+  if (whole + lane < n) grad[whole + lane] = from_float<T>(grad_of(to_float(z[whole + lane])));
+  __syncthreads();
+  if (lane < 64) store_kept<T>(grad, s, r, factor, weight, per);
+}
+
+// The fewest lanes that hold a row with few loads each and its slots with four each.
+template <typename T, bool BACKWARD>
+static int launch_pass(const DistillArgs &a, void *stream) {
+  const int64_t bytes = (int64_t)a.n_classes * (int)sizeof(T);
+  auto of = [&](auto k, int lanes) { return launch_rows(k, lanes, a, stream); };
+  if (bytes < 16)
+    return a.k <= 4 ? of(distill_kernel<T, 1, 1, true, BACKWARD>, 1)
+                    : of(distill_kernel<T, 64, 1, true, BACKWARD>, 64);
+  if (bytes <= 64 && a.k <= 16) return of(distill_kernel<T, 4, 1, false, BACKWARD>, 4);
+  if (bytes <= 128 && a.k <= 32) return of(distill_kernel<T, 8, 1, false, BACKWARD>, 8);
+  if (bytes <= 256 && a.k <= 64) return of(distill_kernel<T, 16, 1, false, BACKWARD>, 16);
+  if (bytes <= 512 && a.k <= 64) return of(distill_kernel<T, 16, 2, false, BACKWARD>, 16);
+  if (bytes <= 1024) return of(distill_kernel<T, 64, 1, false, BACKWARD>, 64);
+  if (bytes <= 2048) return of(distill_kernel<T, 64, 2, false, BACKWARD>, 64);
+  if (bytes <= 4096) return of(distill_kernel<T, 64, 4, false, BACKWARD>, 64);
+  if (bytes <= 8192) return of(distill_kernel<T, 256, 2, false, BACKWARD>, 256);
+  if (bytes <= 16384) return of(distill_kernel<T, 256, 4, false, BACKWARD>, 256);
+  if (bytes <= 32768) return of(distill_kernel<T, 256, 8, false, BACKWARD>, 256);
+  if (bytes <= 65536) return of(distill_kernel<T, 1024, 4, false, BACKWARD>, 1024);
+  if (bytes <= 131072) return of(distill_kernel<T, 1024, 8, false, BACKWARD>, 1024);
+  if (bytes <= 262144) return of(distill_kernel<T, 1024, 16, false, BACKWARD>, 1024);
+  return of(distill_long_kernel<T, BACKWARD>, 1024);
+}
+
+int launch_distill(const DistillArgs &a, int32_t dtype, bool backward, void *stream) {
   return with_type(dtype, [&](auto t) {
-    return with_type(teacher_dtype, [&](auto u) {
-      using T = decltype(t);
-      using U = decltype(u);
-      return launch(backward ? distill_kernel<T, U, true> : distill_kernel<T, U, false>,
-                    grid_of(a.n_rows), kThreads, 0, a, stream);
-    });
+    using T = decltype(t);
+    return backward ? launch_pass<T, true>(a, stream) : launch_pass<T, false>(a, stream);
   });
 }
 

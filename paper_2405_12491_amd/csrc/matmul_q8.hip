@@ -47,7 +47,7 @@ __global__ __launch_bounds__(64) void matmul_q8_kernel(MatmulArgs a) {
 int launch_matmul_q8(const MatmulArgs &a, int32_t dtype, void *stream) {
   const int64_t tiles = ((a.n_rows + 15) / 16) * (((int64_t)a.n_outputs + 15) / 16);
   return with_type(dtype, [&](auto t) {
-    return launch(matmul_q8_kernel<decltype(t)>, grid_of(tiles), 64, 0, a, stream);
+    return launch(matmul_q8_kernel<decltype(t)>, (tiles < (1 << 20) ? tiles : 1 << 20), 64, 0, a, stream);
   });
 }
 

@@ -134,7 +134,7 @@ bridger_status bridger_top_k(const void *scores, int64_t ld, int32_t dtype, int6
   const Rows out[] = {{values, n_rows, k, k, size}, {ids, n_rows, k, k, 4}};
   if (const char *f = arrays_fault(in, 1, out, 2, nullptr)) return invalid(f);
   if (bridger_status s = device_ready()) return s;
-  return launched(launch_top_k({scores, ld, n_rows, n_classes, k, values, ids}, dtype, stream));
+  return launched(launch_top_k({scores, ld, n_rows, n_classes, k, values, ids, 0}, dtype, stream));
 }
 
 bridger_status bridger_distill(const void *logits, int64_t ldl, int32_t dtype, const int32_t *ids,
@@ -144,7 +144,7 @@ bridger_status bridger_distill(const void *logits, int64_t ldl, int32_t dtype, c
                                int64_t ldg, void *stream) {
   clear_error();
   const DistillArgs a = {logits, ldl,    ids,  teacher, n_rows, n_classes, k, temperature,
-                         weight, loss, stats, grad,    ldg};
+                         weight, loss, stats, grad,    ldg, teacher_dtype, 0};
   if (const char *f = distill_fault(a, dtype, teacher_dtype)) return invalid(f);
   if (n_rows == 0) return BRIDGER_OK;
   if (!logits || !ids || !teacher) return invalid("null logits, ids or teacher");
@@ -160,7 +160,7 @@ bridger_status bridger_distill(const void *logits, int64_t ldl, int32_t dtype, c
           arrays_fault(in, 4, out, 3, [](int i, int o) { return i == 0 && o == 2; }))
     return invalid(f);
   if (bridger_status s = device_ready()) return s;
-  return launched(launch_distill(a, dtype, teacher_dtype, false, stream));
+  return launched(launch_distill(a, dtype, false, stream));
 }
 
 bridger_status bridger_distill_backward(const void *logits, int64_t ldl, int32_t dtype,
@@ -171,7 +171,7 @@ bridger_status bridger_distill_backward(const void *logits, int64_t ldl, int32_t
                                         void *stream) {
   clear_error();
   const DistillArgs a = {logits, ldl,     ids, teacher, n_rows, n_classes, k, temperature,
-                         weight, nullptr, const_cast<float *>(stats), grad, ldg};
+                         weight, nullptr, const_cast<float *>(stats), grad, ldg, teacher_dtype, 0};
   if (const char *f = distill_fault(a, dtype, teacher_dtype)) return invalid(f);
   if (n_rows == 0) return BRIDGER_OK;
   if (!logits || !ids || !teacher || !stats) return invalid("null logits, ids, teacher or stats");
@@ -186,7 +186,7 @@ bridger_status bridger_distill_backward(const void *logits, int64_t ldl, int32_t
   if (const char *f = arrays_fault(in, 5, out, 1, [](int i, int) { return i == 0; }))
     return invalid(f);
   if (bridger_status s = device_ready()) return s;
-  return launched(launch_distill(a, dtype, teacher_dtype, true, stream));
+  return launched(launch_distill(a, dtype, true, stream));
 }
 
 bridger_status bridger_rmsnorm_q8(const void *x, int64_t ldx, const void *residual, int64_t ldr,
@@ -211,7 +211,7 @@ bridger_status bridger_rmsnorm_q8(const void *x, int64_t ldx, const void *residu
     return invalid(f);
   if (bridger_status s = device_ready()) return s;
   return launched(launch_rmsnorm_q8({x, ldx, residual, ldr, weight, n_rows, n_features, eps, total,
-                                     ldt, q, ldq, scale},
+                                     ldt, q, ldq, scale, 0},
                                     dtype, stream));
 }
 

@@ -20,6 +20,7 @@ struct TopKArgs {
   int32_t k;
   void *values;  // may be null
   int32_t *ids;  // may be null
+  int64_t first;  // the launch's first row
 };
 
 struct DistillArgs {
@@ -36,6 +37,8 @@ struct DistillArgs {
   float *stats;         // written by the forward pass (may be null), read by the backward pass
   void *grad;           // may be null in the forward pass
   int64_t ldg;
+  int32_t teacher_dtype;
+  int64_t first;  // the launch's first row
 };
 
 struct RmsnormArgs {
@@ -52,6 +55,7 @@ struct RmsnormArgs {
   int8_t *q;
   int64_t ldq;
   float *scale;
+  int64_t first;  // the launch's first row
 };
 
 struct MatmulArgs {
@@ -71,8 +75,7 @@ struct MatmulArgs {
 
 // Each returns a hipError_t as int.  Sizes are positive and every argument checked.
 int launch_top_k(const TopKArgs &a, int32_t dtype, void *stream);
-int launch_distill(const DistillArgs &a, int32_t dtype, int32_t teacher_dtype, bool backward,
-                   void *stream);
+int launch_distill(const DistillArgs &a, int32_t dtype, bool backward, void *stream);
 int launch_rmsnorm_q8(const RmsnormArgs &a, int32_t dtype, void *stream);
 int launch_matmul_q8(const MatmulArgs &a, int32_t dtype, void *stream);
 

@@ -1,16 +1,21 @@
 // top_k.hip -- gfx950 kernels of bridger_top_k: the k largest scores of every row.
+#include <utility>
+
 #include "rows.h"
 
 namespace bridger {
 
-// A score's place in the order, with its class: larger is earlier.  The upper word maps floats to
-// unsigned integers of the same order (-0 as +0, NaN below -infinity as 0), the lower word is the
-// class, inverted, so that equal scores rank by the lower class.  Never 0: classes are below 2^31.
+// A score's place in the order: larger is earlier.  Floats map to unsigned integers of the same
+// order, -0 as +0, NaN (below -infinity) as 0.
 __device__ inline uint32_t order_of(float x) {
   if (x != x) return 0;
   const uint32_t b = __float_as_uint(x + 0.0f);
   return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
+__device__ inline float value_of(uint32_t order) {
+  return __uint_as_float(order ^ (order & 0x80000000u ? 0x80000000u : 0xFFFFFFFFu));
+}
+// With its class: of equal scores the lower class is the larger key.  Never 0.
 __device__ inline uint64_t key_of(float x, int32_t cls) {
   return (uint64_t)order_of(x) << 32 | (0xFFFFFFFFu - (uint32_t)cls);
 }
@@ -19,37 +24,312 @@ __device__ inline int32_t class_of(uint64_t key) {
 }
 
 template <typename T>
-__device__ inline T minus_infinity() {
-  return (T)(-__builtin_inff());
+__device__ inline void store_slot(const TopKArgs &a, int64_t row, int at, T value, int32_t id) {
+  if (a.values) ((T *)a.values)[row * a.k + at] = value;
+  if (a.ids) a.ids[row * a.k + at] = id;
 }
 
-// One workgroup a row: k times the largest key below the last one.
-template <typename T>
-__global__ __launch_bounds__(256) void top_k_kernel(TopKArgs a) {
-  __shared__ uint64_t lds[4];
-  const T *scores = (const T *)a.scores;
-  for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
-    const T *x = scores + row * a.ld;
-    uint64_t last = ~uint64_t(0);
-    for (int i = 0; i < a.k; ++i) {
-      uint64_t best = 0;
-      for (int64_t j = threadIdx.x; j < a.n_classes; j += 256) {
-        const uint64_t key = key_of(to_float(x[j]), (int32_t)j);
-        if (key < last && key > best) best = key;
-      }
-      last = block_reduce<Max, 4>(best, lds);
-      if (threadIdx.x == 0) {
-        const int32_t c = last ? class_of(last) : -1;
-        if (a.values) ((T *)a.values)[row * a.k + i] = last ? x[c] : minus_infinity<T>();
-        if (a.ids) a.ids[row * a.k + i] = c;
+// ============================================================================ FEW CLASSES
+// One lane a row: its K best so far stay sorted in registers.  Classes come in ascending order and a
+// score goes behind its equals, so those stay in the order of their classes.
+template <typename T, int K>
+__global__ __launch_bounds__(256) void top_k_lane_kernel(TopKArgs a) {
+  constexpr int V = kPerLoad<T>;
+  const int64_t row = row_of<1>(a.first);
+  if (row >= a.n_rows) return;
+  const int n = a.n_classes;
+  const T *x = (const T *)a.scores + row * a.ld;
+  uint32_t best[K];
+  int32_t id[K];
+#pragma unroll
+  for (int p = 0; p < K; ++p) best[p] = 0, id[p] = -1;
+  for (int j = 0; j < n; j += V) {
+    RowLoad<T> l;
+    if (n < V) {
+      l.tiny(x, j, n, (T)0.0f);
+    } else {
+      l.issue(x, j, n);
+      l.take(j, n, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const uint32_t o = j + i < n ? order_of(element<T>(l.raw, i)) + 1 : 0;  // 0: an empty slot
+#pragma unroll
+      for (int p = K - 1; p >= 0; --p) {
+        // past every slot that is not smaller; the smaller ones move down
+        const bool here = o > best[p], above = p > 0 && o > best[p > 0 ? p - 1 : 0];
+        best[p] = above ? best[p > 0 ? p - 1 : 0] : here ? o : best[p];
+        id[p] = above ? id[p > 0 ? p - 1 : 0] : here ? j + i : id[p];
       }
     }
   }
+#pragma unroll
+  for (int p = 0; p < K; ++p)
+    if (p < a.k) store_slot<T>(a, row, p, id[p] >= 0 ? x[id[p]] : (T)-__builtin_inff(), id[p]);
+}
+
+// =========================================================================== MANY CLASSES
+// One workgroup of G lanes a row.  Every wave takes the j-th largest of its 64 lanes' maxima, j the
+// waves' share of k; the smallest of those bounds the k-th largest score from below, since at least
+// k scores, one a lane, reach it.  The few scores that reach it are collected in LDS and ranked by
+// counting the larger ones.  Rows where too many or too few reach it (many equal scores, masked or
+// broken rows) take the general way below.
+constexpr int kCandidates = 1024;
+
+// Where the row's scores are.  each(f): f(first class, 16 bytes of scores), in ascending order of
+// the classes per lane; NaN past the row's end.  All lanes make the same number of calls.
+template <typename T, int G, int C>
+struct InRegisters {
+  RowLoad<T> x[C];
+  __device__ InRegisters(const T *row, int n) {
+    const uint32_t nan = fill_of((T)__builtin_nanf(""));
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int j = (c * G + (int)threadIdx.x) * kPerLoad<T>;
+      if (n < kPerLoad<T>) {
+        x[c].tiny(row, j, n, (T)__builtin_nanf(""));
+      } else {
+        x[c].issue(row, j, n);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      if (n >= kPerLoad<T>) x[c].take((c * G + (int)threadIdx.x) * kPerLoad<T>, n, nan);
+  }
+  template <typename F>
+  __device__ void each(F f) {
+    each_of(f, std::make_integer_sequence<int, C>());
+  }
+  // written out: a loop that stayed one would index registers
+  template <typename F, int... c>
+  __device__ void each_of(F f, std::integer_sequence<int, c...>) {
+    ((forget(x[c].raw), f((c * G + (int)threadIdx.x) * kPerLoad<T>, x[c].raw)), ...);
+  }
+};
+template <typename T, int G>
+struct InMemory {
+  const T *row;
+  int n;
+  __device__ InMemory(const T *row, int n) : row(row), n(n) {}
+  template <typename F>
+  __device__ void each(F f) {
+    for (int64_t j0 = 0; j0 < n; j0 += G * kPerLoad<T>) {
+      const int64_t j = j0 + (int64_t)threadIdx.x * kPerLoad<T>;
+      const int at = (int)(j < n ? j : n);
+      RowLoad<T> l;
+      l.issue(row, at, n);
+      l.take(at, n, fill_of((T)__builtin_nanf("")));
+      f(at, l.raw);
+    }
+  }
+};
+
+template <int G>
+struct TopKShared {
+  uint64_t key[kCandidates + 2];
+  float value[kCandidates];
+  float bound[G / 64];
+  int wave[2][G / 64];
+  int count;
+};
+
+// The waves' sum of v; all lanes call it.
+template <int G>
+__device__ inline int count_all(int v, TopKShared<G> &s) {
+  v = lanes_reduce<Sum, 64>(v);
+  if constexpr (G > 64) {
+    __syncthreads();  // the last count is read
+    if ((threadIdx.x & 63) == 0) s.wave[0][threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = lanes_reduce<Sum, G / 64>(s.wave[0][threadIdx.x & (G / 64 - 1)]);
+  }
+  return v;
+}
+
+// Scores for which `reach` holds go to the candidates; their number (it may pass kCandidates, whose
+// entries alone are kept).  `top` is the lane's largest score of one load.
+template <typename T, int G, typename Source, typename Reach>
+__device__ inline int collect(Source &x, TopKShared<G> &s, Reach reach) {
+  constexpr int V = kPerLoad<T>;
+  __syncthreads();
+  if (threadIdx.x == 0) s.count = 0;
+  __syncthreads();
+  x.each([&](int j, const u32x4 &raw) {
+    float top = element<T>(raw, 0);
+#pragma unroll
+    for (int i = 1; i < V; ++i) top = fmaxf(top, element<T>(raw, i));
+    if (reach(top)) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float v = element<T>(raw, i);
+        if (reach(v)) {
+          const int at = atomicAdd(&s.count, 1);
+          if (at < kCandidates) {
+            s.key[at] = key_of(v, j + i);
+            s.value[at] = v;
+          }
+        }
+      }
+    }
+  });
+  __syncthreads();
+  return s.count;
+}
+
+// Ranks the first `count` candidates and stores those of rank below k.
+template <typename T, int G>
+__device__ inline void store_ranked(const TopKArgs &a, int64_t row, TopKShared<G> &s, int count,
+                                    int k) {
+  if (threadIdx.x < 2) s.key[count + threadIdx.x] = 0;
+  __syncthreads();
+  for (int t = threadIdx.x; t < count; t += G) {
+    const uint64_t mine = s.key[t];
+    int rank = 0;
+    for (int q = 0; q < count; q += 2) {
+      const ulonglong2 other = *(const ulonglong2 *)&s.key[q];
+      rank += (other.x > mine) + (other.y > mine);
+    }
+    if (rank < k) store_slot<T>(a, row, rank, from_float<T>(s.value[t]), class_of(mine));
+  }
+}
+
+// Stores scores for which `is` holds in ascending class order from slot `at` on; the next free slot.
+template <typename T, int G, typename Source, typename Is>
+__device__ inline int store_in_order(const TopKArgs &a, int64_t row, Source &x, TopKShared<G> &s,
+                                     int at, int k, Is is) {
+  constexpr int V = kPerLoad<T>, W = G / 64;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int turn = 0;
+  x.each([&](int j, const u32x4 &raw) {
+    if (at >= k) return;  // of the whole workgroup
+    int before = 0, all = 0, mine = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const bool yes = j + i < a.n_classes && is(element<T>(raw, i));
+      const uint64_t lanes = __ballot(yes);
+      before += __popcll(lanes & ((uint64_t(1) << lane) - 1));
+      all += __popcll(lanes);
+      mine |= yes << i;
+    }
+    int first = at;
+    if constexpr (G > 64) {
+      if (lane == 0) s.wave[turn][wave] = all;
+      __syncthreads();
+      all = 0;
+      for (int w = 0; w < W; ++w) {
+        if (w < wave) first += s.wave[turn][w];
+        all += s.wave[turn][w];
+      }
+      turn ^= 1;
+    }
+    int slot = first + before;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (mine >> i & 1) {
+        if (slot < k) store_slot<T>(a, row, slot, from_float<T>(element<T>(raw, i)), j + i);
+        ++slot;
+      }
+    at += all;
+  });
+  return at < k ? at : k;
+}
+
+// The j-th largest of a wave's 64 values (-infinity for those without one).
+__device__ inline float wave_jth(float v, int j) {
+  // as many larger ones as there are: the values with fewer than j of them are the j largest
+  int larger = 0;
+#pragma unroll
+  for (int l = 0; l < 64; ++l)
+    larger += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), l)) > v;
+  return -lanes_reduce<Max, 64>(larger < j ? -v : -__builtin_inff());
+}
+
+template <typename T, int G, typename Source>
+__device__ inline void top_k_row(const TopKArgs &a, int64_t row, Source &x, TopKShared<G> &s) {
+  constexpr int V = kPerLoad<T>, W = G / 64;
+  const float inf = __builtin_inff();
+  const int k = a.k < a.n_classes ? a.k : a.n_classes;
+  float top = -inf;
+  x.each([&](int, const u32x4 &raw) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) top = fmaxf(top, element<T>(raw, i));
+  });
+  const int share = (k + W - 1) / W;
+  float bound = wave_jth(top, share < 64 ? share : 64);
+  if constexpr (G > 64) {
+    if ((threadIdx.x & 63) == 0) s.bound[threadIdx.x >> 6] = bound;
+    __syncthreads();
+    bound = -lanes_reduce<Max, W>(-s.bound[threadIdx.x & (W - 1)]);
+  }
+  if (share > 64) bound = -inf;
+  int count = collect<T, G>(x, s, [&](float v) { return v >= bound; });
+  int stored = 0;
+  if (count >= k && count <= kCandidates) {
+    store_ranked<T, G>(a, row, s, count, k);
+    stored = k;
+  } else {
+    // scores above the bound first; where those are too many, the k-th largest becomes the bound
+    count = collect<T, G>(x, s, [&](float v) { return v > bound; });
+    if (count > kCandidates) {
+      uint32_t order = 0;
+      for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
+        int reach = 0;
+        x.each([&](int, const u32x4 &raw) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) reach += order_of(element<T>(raw, i)) >= (order | bit);
+        });
+        if (count_all<G>(reach, s) >= k) order |= bit;
+      }
+      bound = value_of(order);
+      count = collect<T, G>(x, s, [&](float v) { return v > bound; });
+    }
+    store_ranked<T, G>(a, row, s, count, k);
+    stored = count < k ? count : k;
+    if constexpr (G > 64) __syncthreads();
+    stored = store_in_order<T, G>(a, row, x, s, stored, k, [&](float v) { return v == bound; });
+    if constexpr (G > 64) __syncthreads();
+    stored = store_in_order<T, G>(a, row, x, s, stored, k, [&](float v) { return v != v; });
+  }
+  for (int p = k + threadIdx.x; p < a.k; p += G) store_slot<T>(a, row, p, (T)-inf, -1);
+}
+
+template <typename T, int G, int C>
+__global__ __launch_bounds__(G) void top_k_kernel(TopKArgs a) {
+  __shared__ __attribute__((aligned(16))) TopKShared<G> s;
+  const int64_t row = a.first + blockIdx.x;
+  InRegisters<T, G, C> x((const T *)a.scores + row * a.ld, a.n_classes);
+  top_k_row<T, G>(a, row, x, s);
+}
+
+// Rows that do not fit a workgroup's registers: every walk reads them again.
+template <typename T>
+__global__ __launch_bounds__(1024) void top_k_long_kernel(TopKArgs a) {
+  __shared__ __attribute__((aligned(16))) TopKShared<1024> s;
+  const int64_t row = a.first + blockIdx.x;
+  InMemory<T, 1024> x((const T *)a.scores + row * a.ld, a.n_classes);
+  top_k_row<T, 1024>(a, row, x, s);
 }
 
 int launch_top_k(const TopKArgs &a, int32_t dtype, void *stream) {
   return with_type(dtype, [&](auto t) {
-    return launch(top_k_kernel<decltype(t)>, grid_of(a.n_rows), 256, 0, a, stream);
+    using T = decltype(t);
+    const int64_t bytes = (int64_t)a.n_classes * (int)sizeof(T);
+    // a lane's work is classes x k: beyond a few hundred steps it takes many rows to pay
+    if (a.k <= 16 && a.n_classes <= 64 &&
+        ((int64_t)a.n_classes * a.k <= 256 || a.n_rows >= 8192)) {
+      if (a.k == 1) return launch_rows(top_k_lane_kernel<T, 1>, 1, a, stream);
+      if (a.k <= 4) return launch_rows(top_k_lane_kernel<T, 4>, 1, a, stream);
+      return launch_rows(top_k_lane_kernel<T, 16>, 1, a, stream);
+    }
+    auto of = [&](auto k, int threads) { return launch_each_row(k, threads, a, stream); };
+    if (bytes <= 1024 && a.k <= 64) return of(top_k_kernel<T, 64, 1>, 64);
+    if (bytes <= 4096 && a.k <= 64) return of(top_k_kernel<T, 64, 4>, 64);
+    if (bytes <= 16384) return of(top_k_kernel<T, 256, 4>, 256);
+    if (bytes <= 32768) return of(top_k_kernel<T, 256, 8>, 256);
+    if (bytes <= 65536) return of(top_k_kernel<T, 1024, 4>, 1024);
+    if (bytes <= 131072) return of(top_k_kernel<T, 1024, 8>, 1024);
+    if (bytes <= 262144) return of(top_k_kernel<T, 1024, 16>, 1024);
+    return of(top_k_long_kernel<T>, 1024);
   });
 }
 
