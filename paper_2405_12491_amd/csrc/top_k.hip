@@ -74,9 +74,10 @@ __global__ __launch_bounds__(256) void top_k_lane_kernel(TopKArgs a) {
 // k scores, one a lane, reach it.  The few scores that reach it are collected in LDS and ranked by
 // counting the larger ones.  Rows where too many or too few reach it (many equal scores, masked or
 // broken rows) take the general way below.
-constexpr int kCandidates = 1024;
+template <int G>
+constexpr int kCandidates = G == 64 ? 256 : 1024;  // of one wave: little LDS, so that many fit a CU
 
-// Where the row's scores are.  each(f): f(first class, 16 bytes of scores), in ascending order of
+// Where the row's scores are (in registers, C > 1: a row of at least 16 bytes).  each(f): f(first class, 16 bytes of scores), in ascending order of
 // the classes per lane; NaN past the row's end.  All lanes make the same number of calls.
 template <typename T, int G, int C>
 struct InRegisters {
@@ -86,7 +87,7 @@ struct InRegisters {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int j = (c * G + (int)threadIdx.x) * kPerLoad<T>;
-      if (n < kPerLoad<T>) {
+      if (C == 1 && n < kPerLoad<T>) {
         x[c].tiny(row, j, n, (T)__builtin_nanf(""));
       } else {
         x[c].issue(row, j, n);
@@ -94,7 +95,8 @@ struct InRegisters {
     }
 #pragma unroll
     for (int c = 0; c < C; ++c)
-      if (n >= kPerLoad<T>) x[c].take((c * G + (int)threadIdx.x) * kPerLoad<T>, n, nan);
+      if (C > 1 || n >= kPerLoad<T>)
+        x[c].take((c * G + (int)threadIdx.x) * kPerLoad<T>, n, nan);
   }
   template <typename F>
   __device__ void each(F f) {
@@ -117,8 +119,12 @@ struct InMemory {
       const int64_t j = j0 + (int64_t)threadIdx.x * kPerLoad<T>;
       const int at = (int)(j < n ? j : n);
       RowLoad<T> l;
-      l.issue(row, at, n);
-      l.take(at, n, fill_of((T)__builtin_nanf("")));
+      if (n < kPerLoad<T>) {
+        l.tiny(row, at, n, (T)__builtin_nanf(""));
+      } else {
+        l.issue(row, at, n);
+        l.take(at, n, fill_of((T)__builtin_nanf("")));
+      }
       f(at, l.raw);
     }
   }
@@ -126,8 +132,8 @@ struct InMemory {
 
 template <int G>
 struct TopKShared {
-  uint64_t key[kCandidates + 2];
-  float value[kCandidates];
+  uint64_t key[kCandidates<G> + 2];
+  float value[kCandidates<G>];
   float bound[G / 64];
   int wave[2][G / 64];
   int count;
@@ -154,7 +160,7 @@ __device__ inline int collect(Source &x, TopKShared<G> &s, Reach reach) {
   __syncthreads();
   if (threadIdx.x == 0) s.count = 0;
   __syncthreads();
-  x.each([&](int j, const u32x4 &raw) {
+  x.each([&](int j, const u32x4 &raw) __attribute__((always_inline)) {
     float top = element<T>(raw, 0);
 #pragma unroll
     for (int i = 1; i < V; ++i) top = fmaxf(top, element<T>(raw, i));
@@ -164,7 +170,7 @@ __device__ inline int collect(Source &x, TopKShared<G> &s, Reach reach) {
         const float v = element<T>(raw, i);
         if (reach(v)) {
           const int at = atomicAdd(&s.count, 1);
-          if (at < kCandidates) {
+          if (at < kCandidates<G>) {
             s.key[at] = key_of(v, j + i);
             s.value[at] = v;
           }
@@ -200,7 +206,7 @@ __device__ inline int store_in_order(const TopKArgs &a, int64_t row, Source &x, 
   constexpr int V = kPerLoad<T>, W = G / 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int turn = 0;
-  x.each([&](int j, const u32x4 &raw) {
+  x.each([&](int j, const u32x4 &raw) __attribute__((always_inline)) {
     if (at >= k) return;  // of the whole workgroup
     int before = 0, all = 0, mine = 0;
 #pragma unroll
@@ -244,13 +250,44 @@ __device__ inline float wave_jth(float v, int j) {
   return -lanes_reduce<Max, 64>(larger < j ? -v : -__builtin_inff());
 }
 
+// The general way, from any lower bound of the k-th largest score (-infinity where fewer than k are
+// numbers): scores above it first, then those equal to it and at last NaN, in ascending class order.
+// Where too many lie above it, the k-th largest score is found bit by bit and becomes the bound.
+// Its walks read the row from memory again (from the caches): held in registers they would make up
+// most of the kernel's code.
+template <typename T, int G>
+__device__ inline void store_general(const TopKArgs &a, int64_t row, InMemory<T, G> &x,
+                                     TopKShared<G> &s, float bound, int k) {
+  constexpr int V = kPerLoad<T>;
+  int count = collect<T, G>(x, s, [&](float v) { return v > bound; });
+  if (count > kCandidates<G>) {
+    uint32_t order = 0;
+    for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
+      int reach = 0;
+      x.each([&](int, const u32x4 &raw) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) reach += order_of(element<T>(raw, i)) >= (order | bit);
+      });
+      if (count_all<G>(reach, s) >= k) order |= bit;
+    }
+    bound = value_of(order);
+    count = collect<T, G>(x, s, [&](float v) { return v > bound; });
+  }
+  store_ranked<T, G>(a, row, s, count, k);
+  int stored = count < k ? count : k;
+  __syncthreads();
+  stored = store_in_order<T, G>(a, row, x, s, stored, k, [&](float v) { return v == bound; });
+  __syncthreads();
+  store_in_order<T, G>(a, row, x, s, stored, k, [&](float v) { return v != v; });
+}
+
 template <typename T, int G, typename Source>
 __device__ inline void top_k_row(const TopKArgs &a, int64_t row, Source &x, TopKShared<G> &s) {
   constexpr int V = kPerLoad<T>, W = G / 64;
   const float inf = __builtin_inff();
   const int k = a.k < a.n_classes ? a.k : a.n_classes;
   float top = -inf;
-  x.each([&](int, const u32x4 &raw) {
+  x.each([&](int, const u32x4 &raw) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < V; ++i) top = fmaxf(top, element<T>(raw, i));
   });
@@ -263,38 +300,17 @@ __device__ inline void top_k_row(const TopKArgs &a, int64_t row, Source &x, TopK
   }
   if (share > 64) bound = -inf;
   int count = collect<T, G>(x, s, [&](float v) { return v >= bound; });
-  int stored = 0;
-  if (count >= k && count <= kCandidates) {
+  if (count >= k && count <= kCandidates<G>) {
     store_ranked<T, G>(a, row, s, count, k);
-    stored = k;
   } else {
-    // scores above the bound first; where those are too many, the k-th largest becomes the bound
-    count = collect<T, G>(x, s, [&](float v) { return v > bound; });
-    if (count > kCandidates) {
-      uint32_t order = 0;
-      for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
-        int reach = 0;
-        x.each([&](int, const u32x4 &raw) {
-#pragma unroll
-          for (int i = 0; i < V; ++i) reach += order_of(element<T>(raw, i)) >= (order | bit);
-        });
-        if (count_all<G>(reach, s) >= k) order |= bit;
-      }
-      bound = value_of(order);
-      count = collect<T, G>(x, s, [&](float v) { return v > bound; });
-    }
-    store_ranked<T, G>(a, row, s, count, k);
-    stored = count < k ? count : k;
-    if constexpr (G > 64) __syncthreads();
-    stored = store_in_order<T, G>(a, row, x, s, stored, k, [&](float v) { return v == bound; });
-    if constexpr (G > 64) __syncthreads();
-    stored = store_in_order<T, G>(a, row, x, s, stored, k, [&](float v) { return v != v; });
+    InMemory<T, G> m((const T *)a.scores + row * a.ld, a.n_classes);
+    store_general<T, G>(a, row, m, s, bound, k);
   }
   for (int p = k + threadIdx.x; p < a.k; p += G) store_slot<T>(a, row, p, (T)-inf, -1);
 }
 
 template <typename T, int G, int C>
-__global__ __launch_bounds__(G) void top_k_kernel(TopKArgs a) {
+__global__ __launch_bounds__(G, C <= 8 ? 8 : 4) void top_k_kernel(TopKArgs a) {
   __shared__ __attribute__((aligned(16))) TopKShared<G> s;
   const int64_t row = a.first + blockIdx.x;
   InRegisters<T, G, C> x((const T *)a.scores + row * a.ld, a.n_classes);
@@ -322,8 +338,10 @@ int launch_top_k(const TopKArgs &a, int32_t dtype, void *stream) {
       return launch_rows(top_k_lane_kernel<T, 16>, 1, a, stream);
     }
     auto of = [&](auto k, int threads) { return launch_each_row(k, threads, a, stream); };
-    if (bytes <= 1024 && a.k <= 64) return of(top_k_kernel<T, 64, 1>, 64);
-    if (bytes <= 4096 && a.k <= 64) return of(top_k_kernel<T, 64, 4>, 64);
+    // one wave, whose lanes' maxima bound up to 64 scores; rows below 16 bytes are among these
+    const int k = a.k < a.n_classes ? a.k : a.n_classes;
+    if (bytes <= 1024 && k <= 64) return of(top_k_kernel<T, 64, 1>, 64);
+    if (bytes <= 4096 && k <= 64) return of(top_k_kernel<T, 64, 4>, 64);
     if (bytes <= 16384) return of(top_k_kernel<T, 256, 4>, 256);
     if (bytes <= 32768) return of(top_k_kernel<T, 256, 8>, 256);
     if (bytes <= 65536) return of(top_k_kernel<T, 1024, 4>, 1024);
