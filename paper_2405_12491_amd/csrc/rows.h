@@ -281,4 +281,17 @@ int launch_each_row(void (*k)(Args), int threads, const Args &args, void *stream
   return launch_over(k, threads, 1, args, stream);
 }
 
+// A workgroup a tile.
+constexpr int64_t kMaxTiles = int64_t(1) << 23;
+template <typename Args>
+int launch_tiles(void (*k)(Args), int64_t tiles, int threads, int lds_bytes, const Args &args,
+                 void *stream) {
+  if (lds_bytes > 65536) {
+    const hipError_t e = hipFuncSetAttribute(
+        (const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes);
+    if (e != hipSuccess) return (int)e;
+  }
+  return launch(k, tiles, threads, lds_bytes, args, stream);
+}
+
 }  // namespace bridger
