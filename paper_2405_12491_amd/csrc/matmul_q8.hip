@@ -3,6 +3,8 @@
 // The matrix instructions take the weights as their first operand, so that a lane ends with four
 // neighbouring outputs of one row.  Both operands share the order of the features within an
 // instruction, so any fixed order of them gives the same sum.
+#include <type_traits>
+
 #include "rows.h"
 
 namespace bridger {
@@ -36,17 +38,30 @@ __device__ inline i32x4 load_features(const int8_t *row, int j, int n) {
   return v;
 }
 
+// N neighbouring floats from `at` on; what lies past n is not read.
+template <int N>
+__device__ inline void load_floats(const float *p, int64_t at, int64_t n, float (&v)[N]) {
+  if (at + N <= n) {
+    __builtin_memcpy(v, p + at, sizeof(v));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = at + i < n ? p[at + i] : 0.0f;
+  }
+}
+
 // Four neighbouring outputs of a row.
 template <typename T>
 __device__ inline void store_outputs(const MatmulArgs &a, int64_t row, int64_t o, i32x4 sum) {
   if (row >= a.n_rows || o >= a.n_outputs) return;
   const float row_scale = a.a_scale[row];
+  float scale[4], bias[4];
+  load_floats<4>(a.b_scale, o, a.n_outputs, scale);
+  if (a.bias) load_floats<4>(a.bias, o, a.n_outputs, bias);
   T y[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int64_t at = o + i < a.n_outputs ? o + i : o;
-    float v = (float)sum[i] * row_scale * a.b_scale[at];
-    if (a.bias) v += a.bias[at];
+    float v = (float)sum[i] * row_scale * scale[i];
+    if (a.bias) v += bias[i];
     y[i] = from_float<T>(v);
   }
   T *out = (T *)a.out + row * a.ldo + o;
@@ -175,111 +190,174 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
   }
   const int whole = n / kStage;
   uint8_t *lds_a = smem, *lds_b = smem + 2 * B * kStage;
-  i32x4 hold_a[P], hold_b[P];  // a stage on its way through registers
+  i32x4 hold[2 * P];  // a stage on its way through registers
 
-  // starts to bring stage s
-  auto fetch = [&](int s) __attribute__((always_inline)) {
-    const int j = s * kStage + 16 * chunk;
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      if constexpr (ALIGNED) {
-        lds_byte *to = (lds_byte *)smem + (s & 1) * B * kStage + wave * 1024 + p * 4096;
-        __builtin_amdgcn_global_load_lds(
-            (const __attribute__((address_space(1))) void *)(from_a[p] + j),
-            (__attribute__((address_space(3))) void *)to, 16, 0, 0);
-        __builtin_amdgcn_global_load_lds(
-            (const __attribute__((address_space(1))) void *)(from_b[p] + j),
-            (__attribute__((address_space(3))) void *)(to + 2 * B * kStage), 16, 0, 0);
-      } else {
-        __builtin_memcpy(&hold_a[p], from_a[p] + j, 16);
-        __builtin_memcpy(&hold_b[p], from_b[p] + j, 16);
-      }
+  // starts to bring stage s: chunk p of a (p < P) or of b
+  auto fetch = [&](int s, int p) __attribute__((always_inline)) {
+    const int8_t *from = (p < P ? from_a[p % P] : from_b[p % P]) + s * kStage + 16 * chunk;
+    if constexpr (ALIGNED) {
+      lds_byte *to = (lds_byte *)smem + (p < P ? 0 : 2 * B * kStage) + (s & 1) * B * kStage +
+                     wave * 1024 + p % P * 4096;
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                       (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+    } else {
+      __builtin_memcpy(&hold[p], from, 16);
     }
   };
-  // a stage that is held in registers, to LDS
-  auto put = [&](int s) __attribute__((always_inline)) {
-    const int to = (s & 1) * B * kStage + t * 16;
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      *(i32x4 *)(lds_a + to + p * 4096) = hold_a[p];
-      *(i32x4 *)(lds_b + to + p * 4096) = hold_b[p];
-    }
+  // a chunk that is held in registers, to LDS
+  auto put = [&](int s, int p) __attribute__((always_inline)) {
+    *(i32x4 *)((p < P ? lds_a : lds_b) + (s & 1) * B * kStage + t * 16 + p % P * 4096) = hold[p];
   };
   // lane l's operand: row (or output) l & 31, features from 16 (l >> 5) of a step of 32
   const int half = lane >> 5, row32 = lane & 31;
   const int base_a = ((wave >> 1) * (B / 2) + row32) * kStage;
   const int base_b = ((wave & 1) * (B / 2) + row32) * kStage;
-  auto read = [&](int s, int step, i32x4(&x)[C], i32x4(&w)[C]) __attribute__((always_inline)) {
-    const int at = (s & 1) * B * kStage + (((2 * step + half) ^ (row32 & 7)) << 4);
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      x[c] = *(const i32x4 *)(lds_a + base_a + at + c * 32 * kStage);
-      w[c] = *(const i32x4 *)(lds_b + base_b + at + c * 32 * kStage);
+  struct Operands {
+    i32x4 x[C], w[C];
+  };
+  // operand i of a step: w, x in turn
+  auto read = [&](int s, int step, int i, Operands &v) __attribute__((always_inline)) {
+    const int at = (s & 1) * B * kStage + (((2 * step + half) ^ (row32 & 7)) << 4) +
+                   i / 2 * 32 * kStage;
+    if (i % 2) {
+      v.x[i / 2] = *(const i32x4 *)(lds_a + base_a + at);
+    } else {
+      v.w[i / 2] = *(const i32x4 *)(lds_b + base_b + at);
     }
   };
   i32x16 sum[C][C] = {};
-  auto multiply = [&](const i32x4(&x)[C], const i32x4(&w)[C]) __attribute__((always_inline)) {
+  // One step's matrix instructions, with beside(i) in the issue slots behind the i-th.  The order is
+  // pinned: the scheduler would gather the loads ahead of them and leave the matrix cores idle.
+  auto multiply = [&](const Operands &v, auto beside) __attribute__((always_inline)) {
 #pragma unroll
     for (int r = 0; r < C; ++r)
 #pragma unroll
-      for (int o = 0; o < C; ++o)
-        sum[r][o] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[o], x[r], sum[r][o], 0, 0, 0);
+      for (int o = 0; o < C; ++o) {
+        sum[r][o] = __builtin_amdgcn_mfma_i32_32x32x32_i8(v.w[o], v.x[r], sum[r][o], 0, 0, 0);
+        beside(r * C + o);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+  };
+  constexpr int M = C * C;  // matrix instructions of a step
+  // n things spread over a step's first instructions, `many` a time
+  auto spread = [&](int i, int n, int many, auto f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int q = 0; q < many; ++q)
+      if (i * many + q < n) f(i * many + q);
   };
   // Every load to LDS issued so far is done, by all waves, and every read.
   auto meet = [&]() __attribute__((always_inline)) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  i32x4 x0[C], w0[C], x1[C], w1[C];
+  constexpr int kReads = (2 * C + M - 1) / M, kFetches = (2 * P + M - 1) / M;
+  Operands u, v;
+  // stage s, NEXT: with another after it, FETCH: with one more after that
+  auto stage = [&](int s, auto next, auto more) __attribute__((always_inline)) {
+    constexpr bool NEXT = decltype(next)::value, FETCH = decltype(more)::value;
+    multiply(u, [&](int i) {
+      spread(i, 2 * C, kReads, [&](int q) { read(s, 1, q, v); });
+    });
+    multiply(v, [&](int i) {
+      spread(i, 2 * C, kReads, [&](int q) { read(s, 2, q, u); });
+    });
+    multiply(u, [&](int i) {
+      spread(i, 2 * C, kReads, [&](int q) { read(s, 3, q, v); });
+      if (!ALIGNED && NEXT) spread(i, 2 * P, kFetches, [&](int p) { put(s + 1, p); });
+    });
+    if (NEXT) meet();  // stage s + 1 is there, and nobody reads stage s any more
+    multiply(v, [&](int i) {
+      if (NEXT) spread(i, 2 * C, kReads, [&](int q) { read(s + 1, 0, q, u); });
+      if (FETCH) spread(i, 2 * P, kFetches, [&](int p) { fetch(s + 2, p); });
+    });
+  };
   if (whole > 0) {
-    fetch(0);
-    if (!ALIGNED) put(0);
+#pragma unroll
+    for (int p = 0; p < 2 * P; ++p) fetch(0, p);
+    if (!ALIGNED)
+#pragma unroll
+      for (int p = 0; p < 2 * P; ++p) put(0, p);
     meet();
-    read(0, 0, x0, w0);
-    if (whole > 1) fetch(1);
-    for (int s = 0; s < whole; ++s) {
-      read(s, 1, x1, w1);
-      multiply(x0, w0);
-      read(s, 2, x0, w0);
-      multiply(x1, w1);
-      read(s, 3, x1, w1);
-      if (!ALIGNED && s + 1 < whole) put(s + 1);
-      multiply(x0, w0);
-      if (s + 1 < whole) {
-        meet();  // stage s + 1 is there, and nobody reads stage s any more
-        read(s + 1, 0, x0, w0);
-        if (s + 2 < whole) fetch(s + 2);
-      }
-      multiply(x1, w1);
-    }
+#pragma unroll
+    for (int q = 0; q < 2 * C; ++q) read(0, 0, q, u);
+    if (whole > 1)
+#pragma unroll
+      for (int p = 0; p < 2 * P; ++p) fetch(1, p);
+    int s = 0;
+    for (; s + 2 < whole; ++s) stage(s, std::true_type(), std::true_type());
+    if (s + 1 < whole) stage(s++, std::true_type(), std::false_type());
+    stage(s, std::false_type(), std::false_type());
   }
   if (n % kStage) {  // the features past the last whole stage, filled up with zeros
     const int j = whole * kStage + 16 * chunk;
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-      hold_a[p] = load_features<false>(from_a[p], j, n);
-      hold_b[p] = load_features<false>(from_b[p], j, n);
-    }
-    put(whole);  // nobody reads the other stage's place: it was left before the last meeting
+    for (int p = 0; p < 2 * P; ++p)
+      hold[p] = load_features<false>(p < P ? from_a[p % P] : from_b[p % P], j, n);
+#pragma unroll
+    for (int p = 0; p < 2 * P; ++p) put(whole, p);  // not where the last whole stage is read
     meet();
 #pragma unroll 1
     for (int step = 0; step < (n % kStage + 31) / 32; ++step) {
-      read(whole, step, x0, w0);
-      multiply(x0, w0);
+#pragma unroll
+      for (int q = 0; q < 2 * C; ++q) read(whole, step, q, u);
+      multiply(u, [](int) {});
     }
   }
-  // lane l holds row l & 31 and outputs 8 (i / 4) + 4 (l >> 5) + i % 4 of each tile
+
+  // Lane l holds row l & 31 and outputs 8 (i / 4) + 4 (l >> 5) + i % 4 of each tile.  32 rows of a
+  // wave at a time go through LDS, in the type they are stored in, and out as whole runs of a row.
+  meet();
+  float *scales = (float *)smem;  // of the tile's rows, its outputs, and the bias
+  for (int i = t; i < B; i += 256) {
+    scales[i] = r0 + i < a.n_rows ? a.a_scale[r0 + i] : 0.0f;
+    scales[B + i] = o0 + i < a.n_outputs ? a.b_scale[o0 + i] : 0.0f;
+    scales[2 * B + i] = a.bias && o0 + i < a.n_outputs ? a.bias[o0 + i] : 0.0f;
+  }
+  meet();
+  constexpr int kPitch = B / 2 * (int)sizeof(T) + 16;  // of a row of a wave's outputs, in bytes
+  constexpr int kRun = 16 / (int)sizeof(T), kRunsARow = B / 2 / kRun;
+  uint8_t *part = smem + 3 * B * 4 + wave * 32 * kPitch;
+  const int64_t row_first = r0 + (wave >> 1) * (B / 2), out_first = o0 + (wave & 1) * (B / 2);
 #pragma unroll
-  for (int r = 0; r < C; ++r)
+  for (int r = 0; r < C; ++r) {
+    const float row_scale = scales[(wave >> 1) * (B / 2) + 32 * r + row32];
 #pragma unroll
     for (int o = 0; o < C; ++o)
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        store_outputs<T>(a, r0 + (wave >> 1) * (B / 2) + 32 * r + row32,
-                         o0 + (wave & 1) * (B / 2) + 32 * o + 8 * q + 4 * half,
-                         i32x4{sum[r][o][4 * q], sum[r][o][4 * q + 1], sum[r][o][4 * q + 2],
-                               sum[r][o][4 * q + 3]});
+      for (int q = 0; q < 4; ++q) {
+        const int at = 32 * o + 8 * q + 4 * half;
+        const float4 scale = *(const float4 *)&scales[B + (wave & 1) * (B / 2) + at];
+        const float4 bias = *(const float4 *)&scales[2 * B + (wave & 1) * (B / 2) + at];
+        const float f[4] = {scale.x, scale.y, scale.z, scale.w};
+        const float g[4] = {bias.x, bias.y, bias.z, bias.w};
+        T y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float z = (float)sum[r][o][4 * q + i] * row_scale * f[i];
+          if (a.bias) z += g[i];
+          y[i] = from_float<T>(z);
+        }
+        __builtin_memcpy(part + row32 * kPitch + at * sizeof(T), y, sizeof(y));
+      }
+    // only this wave's own part: its LDS instructions are done in order
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < 32 * kRunsARow / 64; ++i) {
+      const int at = i * 64 + lane, in_row = at % kRunsARow * kRun;
+      const int64_t row = row_first + 32 * r + at / kRunsARow, o = out_first + in_row;
+      uint32_t w[4];
+      __builtin_memcpy(w, part + at / kRunsARow * kPitch + in_row * sizeof(T), 16);
+      if (row < a.n_rows && o < a.n_outputs) {
+        const int64_t left = a.n_outputs - o;
+        store_packed<T, kRun>((T *)a.out + row * a.ldo + o, left < kRun ? (int)left : kRun, w);
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
 }
 
 template <typename T, int R, int O, int W, int U>
