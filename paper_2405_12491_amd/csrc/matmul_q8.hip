@@ -75,63 +75,114 @@ __device__ inline void store_outputs(const MatmulArgs &a, int64_t row, int64_t o
 }
 
 // ================================================================================ FEW ROWS
-// A workgroup holds 16 R rows by 16 O outputs; its W waves share the features, each taking every
-// W-th run of U x 64, straight from memory into the matrix instructions' registers (lane l: row or
-// output l & 15, 16 features from 16 (l >> 4)), and join their sums in LDS.  So few rows still put
-// enough waves on the chip to stream the weights, and nothing is shared beyond a workgroup.
-template <typename T, int R, int O, int W, int U>
+// A workgroup holds 16 R rows by 16 O outputs; its W waves share the features, wave w taking stages
+// w, w + W, .. of 64, and join their sums in LDS.  So few rows still put enough waves on the chip to
+// stream the weights, and nothing is shared beyond a workgroup.  Each wave has a ring of S stages of
+// its own in LDS and S - 1 of them on their way, without a barrier.  The detour through LDS is for
+// the loads: an instruction that reads operands in place has neighbouring lanes in 16 different
+// rows, and takes 64 cycles; here four neighbouring lanes read 64 bytes of a row (16 cycles).  A
+// row's four 16-byte chunks stand at chunk ^ (row / 4 & 3): 16 rows of one chunk hit all banks.
+// ALIGNED: rows start at multiples of 16 bytes and go to LDS without passing registers.
+typedef __attribute__((address_space(3))) uint8_t lds_byte;
+
+__device__ inline void load_to_lds(const int8_t *from, lds_byte *to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                   (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+
+// At most V loads (and L LDS instructions) are still on their way.
+template <int V, int L>
+__device__ inline void wait_for() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((V & 15) | 7 << 4 | L << 8 | (V >> 4) << 14);
+  asm volatile("" ::: "memory");
+}
+
+template <typename T, int R, int O, int W, int S, bool ALIGNED>
 __global__ __launch_bounds__(64 * W) void matmul_q8_stream_kernel(MatmulArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = lane & 15;
+  constexpr int N = R + O;  // 16-row parts of a stage, 1 KB and one load of a wave each
+  const int lane = threadIdx.x & 63, at = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = a.n_features;
   const int64_t tiles_o = (a.n_outputs + 16 * O - 1) / (16 * O);
   const int64_t r0 = blockIdx.x / tiles_o * (16 * R), o0 = blockIdx.x % tiles_o * (16 * O);
-  // past the end the last row, or output, stands in; its sums are not stored
-  const int8_t *rows[R], *outs[O];
+  // lane l brings chunk (l & 3) ^ (l / 16) of row l / 4 of each part to slot l & 3 of that row; past
+  // the end the last row, or output, stands in: its sums are not stored
+  auto row_of_part = [&](int p, int i) {
+    const int64_t first = p < R ? r0 + 16 * p : o0 + 16 * (p - R), end = p < R ? a.n_rows : a.n_outputs;
+    const int64_t row = first + i < end ? first + i : end - 1;
+    return p < R ? a.a + row * a.lda : a.b + row * a.ldb;
+  };
+  const int8_t *from[N];
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int64_t row = r0 + 16 * r + at;
-    rows[r] = a.a + (row < a.n_rows ? row : a.n_rows - 1) * a.lda + 16 * (lane >> 4);
-  }
+  for (int p = 0; p < N; ++p)
+    from[p] = row_of_part(p, lane >> 2) + 16 * ((lane & 3) ^ (lane >> 4)) + wave * 64;
+  const int whole = n / 64;                                     // stages without the last, partial one
+  const int count = wave < whole ? (whole - wave + W - 1) / W : 0;  // this wave's
+  constexpr int kRing = ALIGNED ? S : 1;
+  uint8_t *ring = smem + wave * kRing * N * 1024;
+  const uint8_t *operand = ring + at * 64 + (((lane >> 4) ^ (at >> 2)) << 4);
+  i32x4 hold[ALIGNED ? 1 : S][N];
+  auto issue = [&](int i, int slot) __attribute__((always_inline)) {
 #pragma unroll
-  for (int o = 0; o < O; ++o) {
-    const int64_t out = o0 + 16 * o + at;
-    outs[o] = a.b + (out < a.n_outputs ? out : a.n_outputs - 1) * a.ldb + 16 * (lane >> 4);
-  }
+    for (int p = 0; p < N; ++p)
+      if constexpr (ALIGNED) {
+        load_to_lds(from[p] + (int64_t)i * (W * 64), (lds_byte *)ring + (slot * N + p) * 1024);
+      } else {
+        __builtin_memcpy(&hold[slot][p], from[p] + (int64_t)i * (W * 64), 16);
+      }
+  };
   i32x4 sum[R][O] = {};
-  int j = wave * U * 64;
-  for (; j + U * 64 <= n; j += W * U * 64) {
-    i32x4 x[U][R], w[U][O];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+  for (int d = 0; d < S - 1; ++d)
+    if (d < count) issue(d, d);
+  for (int i0 = 0; i0 < count; i0 += S) {
 #pragma unroll
-      for (int o = 0; o < O; ++o) __builtin_memcpy(&w[u][o], outs[o] + j + 64 * u, 16);
+    for (int d = 0; d < S; ++d) {
+      const int i = i0 + d;
+      if (i >= count) break;
+      wait_for<63, 0>();  // the slot that is filled next has been read
+      if (i + S - 1 < count) {
+        issue(i + S - 1, (d + S - 1) % S);
+        if constexpr (ALIGNED) wait_for<(S - 1) * N, 15>();
+      } else {
+        if constexpr (ALIGNED) wait_for<0, 15>();
+      }
+      constexpr int kSlot = ALIGNED ? N * 1024 : 0;
+      if constexpr (!ALIGNED) {
 #pragma unroll
-      for (int r = 0; r < R; ++r) __builtin_memcpy(&x[u][r], rows[r] + j + 64 * u, 16);
-    }
+        for (int p = 0; p < N; ++p) *(i32x4 *)(ring + p * 1024 + lane * 16) = hold[d][p];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+      }
+      i32x4 x[R], w[O];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+      for (int o = 0; o < O; ++o) w[o] = *(const i32x4 *)(operand + d * kSlot + (R + o) * 1024);
+#pragma unroll
+      for (int r = 0; r < R; ++r) x[r] = *(const i32x4 *)(operand + d * kSlot + r * 1024);
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int o = 0; o < O; ++o)
-          sum[r][o] =
-              __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u][o], x[u][r], sum[r][o], 0, 0, 0);
+          sum[r][o] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[o], x[r], sum[r][o], 0, 0, 0);
+    }
   }
-  // the last, partial run of features is one wave's
-  for (const int end = j + U * 64; j < n && j < end; j += 64) {
+  if (n % 64 && wave == whole % W) {  // the features past the last whole stage
+    const int j = whole * 64 + 16 * (lane >> 4);
     i32x4 x[R];
-    const int part = 16 * (lane >> 4);
 #pragma unroll
-    for (int r = 0; r < R; ++r) x[r] = load_features<true>(rows[r] - part, j + part, n);
+    for (int r = 0; r < R; ++r) x[r] = load_features<true>(row_of_part(r, at), j, n);
 #pragma unroll
     for (int o = 0; o < O; ++o) {
-      const i32x4 w = load_features<true>(outs[o] - part, j + part, n);
+      const i32x4 w = load_features<true>(row_of_part(R + o, at), j, n);
 #pragma unroll
       for (int r = 0; r < R; ++r)
         sum[r][o] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x[r], sum[r][o], 0, 0, 0);
     }
   }
+  wait_for<0, 0>();
+  __syncthreads();  // the rings are left
   i32x4 *lds = (i32x4 *)smem;
 #pragma unroll
   for (int r = 0; r < R; ++r)
@@ -156,8 +207,6 @@ constexpr int kStage = 128;
 
 template <int B>
 constexpr int kTileLds = 2 * 2 * B * kStage;
-
-typedef __attribute__((address_space(3))) uint8_t lds_byte;
 
 // ALIGNED: rows of a and b start at multiples of 16 bytes and lie within 2^32 bytes of the tile's
 // first; stages then go to LDS without passing registers.
@@ -198,8 +247,7 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
     if constexpr (ALIGNED) {
       lds_byte *to = (lds_byte *)smem + (p < P ? 0 : 2 * B * kStage) + (s & 1) * B * kStage +
                      wave * 1024 + p % P * 4096;
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
-                                       (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+      load_to_lds(from, to);
     } else {
       __builtin_memcpy(&hold[p], from, 16);
     }
@@ -247,8 +295,7 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
   };
   // Every load to LDS issued so far is done, by all waves, and every read.
   auto meet = [&]() __attribute__((always_inline)) {
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+    wait_for<0, 0>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
@@ -360,19 +407,27 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
   }
 }
 
-template <typename T, int R, int O, int W, int U>
+static bool aligned_rows(const MatmulArgs &a) {
+  return ((uintptr_t)a.a | (uintptr_t)a.b | (uint64_t)a.lda | (uint64_t)a.ldb) % 16 == 0;
+}
+template <typename T, int R, int O, int W, int S>
 static int launch_stream(const MatmulArgs &a, void *stream) {
   const int64_t tiles = ((a.n_rows + 16 * R - 1) / (16 * R)) *
                         (((int64_t)a.n_outputs + 16 * O - 1) / (16 * O));
-  return launch_tiles(matmul_q8_stream_kernel<T, R, O, W, U>, tiles, 64 * W, W * R * O * 1024, a,
-                      stream);
+  constexpr int kSums = W * R * O * 1024, kPart = W * (R + O) * 1024;
+  constexpr int kAligned = S * kPart > kSums ? S * kPart : kSums;
+  constexpr int kOther = kPart > kSums ? kPart : kSums;
+  return aligned_rows(a)
+             ? launch_tiles(matmul_q8_stream_kernel<T, R, O, W, S, true>, tiles, 64 * W, kAligned, a,
+                            stream)
+             : launch_tiles(matmul_q8_stream_kernel<T, R, O, W, S, false>, tiles, 64 * W, kOther, a,
+                            stream);
 }
 template <typename T, int B>
 static int launch_tile(const MatmulArgs &a, void *stream) {
   const int64_t tiles =
       ((a.n_rows + B - 1) / B) * (((int64_t)a.n_outputs + B - 1) / B);
-  const bool aligned = ((uintptr_t)a.a | (uintptr_t)a.b | (uint64_t)a.lda | (uint64_t)a.ldb) % 16 == 0;
-  return aligned ? launch_tiles(matmul_q8_tile_kernel<T, B, true>, tiles, 256, kTileLds<B>, a, stream)
+  return aligned_rows(a) ? launch_tiles(matmul_q8_tile_kernel<T, B, true>, tiles, 256, kTileLds<B>, a, stream)
                  : launch_tiles(matmul_q8_tile_kernel<T, B, false>, tiles, 256, kTileLds<B>, a, stream);
 }
 
@@ -383,12 +438,12 @@ int launch_matmul_q8(const MatmulArgs &a, int32_t dtype, void *stream) {
     if (a.n_features < 16) return launch_stream<T, 1, 1, 8, 4>(a, stream);
     if (m <= 16) return launch_stream<T, 1, 1, 8, 4>(a, stream);
     if (m <= 32) return launch_stream<T, 2, 1, 8, 4>(a, stream);
-    if (m <= 64) return launch_stream<T, 4, 2, 4, 2>(a, stream);
+    if (m <= 64) return launch_stream<T, 4, 2, 8, 3>(a, stream);
     const int64_t wide = ((m + 255) / 256) * ((o + 255) / 256);
     const int64_t middle = ((m + 127) / 128) * ((o + 127) / 128);
     if (wide >= 192) return launch_tile<T, 256>(a, stream);
     if (middle >= 192) return launch_tile<T, 128>(a, stream);
-    return launch_stream<T, 4, 4, 4, 1>(a, stream);
+    return launch_stream<T, 4, 4, 8, 2>(a, stream);
   });
 }
 
