@@ -82,12 +82,24 @@ __device__ inline void store_outputs(const MatmulArgs &a, int64_t row, int64_t o
 // the loads: an instruction that reads operands in place has neighbouring lanes in 16 different
 // rows, and takes 64 cycles; here four neighbouring lanes read 64 bytes of a row (16 cycles).  A
 // row's four 16-byte chunks stand at chunk ^ (row / 4 & 3): 16 rows of one chunk hit all banks.
-// ALIGNED: rows start at multiples of 16 bytes and go to LDS without passing registers.
+// ALIGNED: rows go to LDS without passing registers (aligned_rows).
 typedef __attribute__((address_space(3))) uint8_t lds_byte;
 
-__device__ inline void load_to_lds(const int8_t *from, lds_byte *to) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
-                                   (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+// Rows [first, n) of a matrix, `ld` apart, for loads by 32-bit offsets from row `first`; what lies
+// behind the matrix is out of its bounds.
+__device__ inline __amdgpu_buffer_rsrc_t rows_from(const int8_t *p, int64_t ld, int64_t first,
+                                                   int64_t n, int width) {
+  const int64_t bytes = (n - 1 - first) * ld + width;
+  return __builtin_amdgcn_make_buffer_rsrc((void *)(p + first * ld), 0,
+                                           (int)(bytes < 0xFFFFFFFFll ? bytes : 0xFFFFFFFFll),
+                                           0x27000);
+}
+// 16 bytes a lane to LDS, lane after lane from `to`.  (The buffer form: the compiler counts the
+// global form among the LDS instructions too, and waits for all of those at every use of one.)
+__device__ inline void load_to_lds(__amdgpu_buffer_rsrc_t rows, int lane_offset, int offset,
+                                   lds_byte *to) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(
+      rows, (__attribute__((address_space(3))) void *)to, 16, lane_offset, offset, 0, 0);
 }
 
 // At most V loads (and L LDS instructions) are still on their way.
@@ -114,10 +126,15 @@ __global__ __launch_bounds__(64 * W) void matmul_q8_stream_kernel(MatmulArgs a) 
     const int64_t row = first + i < end ? first + i : end - 1;
     return p < R ? a.a + row * a.lda : a.b + row * a.ldb;
   };
+  const auto rows_a = rows_from(a.a, a.lda, r0, a.n_rows, n);
+  const auto rows_b = rows_from(a.b, a.ldb, o0, a.n_outputs, n);
   const int8_t *from[N];
+  int offset[N];
 #pragma unroll
-  for (int p = 0; p < N; ++p)
+  for (int p = 0; p < N; ++p) {
     from[p] = row_of_part(p, lane >> 2) + 16 * ((lane & 3) ^ (lane >> 4)) + wave * 64;
+    offset[p] = (int)(from[p] - (p < R ? a.a + r0 * a.lda : a.b + o0 * a.ldb));
+  }
   const int whole = n / 64;                                     // stages without the last, partial one
   const int count = wave < whole ? (whole - wave + W - 1) / W : 0;  // this wave's
   constexpr int kRing = ALIGNED ? S : 1;
@@ -128,7 +145,8 @@ __global__ __launch_bounds__(64 * W) void matmul_q8_stream_kernel(MatmulArgs a) 
 #pragma unroll
     for (int p = 0; p < N; ++p)
       if constexpr (ALIGNED) {
-        load_to_lds(from[p] + (int64_t)i * (W * 64), (lds_byte *)ring + (slot * N + p) * 1024);
+        load_to_lds(p < R ? rows_a : rows_b, offset[p], i * (W * 64),
+                    (lds_byte *)ring + (slot * N + p) * 1024);
       } else {
         __builtin_memcpy(&hold[slot][p], from[p] + (int64_t)i * (W * 64), 16);
       }
@@ -199,21 +217,21 @@ __global__ __launch_bounds__(64 * W) void matmul_q8_stream_kernel(MatmulArgs a) 
 
 // =============================================================================== MANY ROWS
 // A workgroup of 2 x 2 waves holds B x B outputs, each wave (B / 2) x (B / 2) in tiles of 32 x 32
-// (v_mfma_i32_32x32x32_i8).  Stages of 128 features of its rows and weights go to LDS, two stages
-// in turn, one being filled while the other is multiplied; a wave reads the operands of a step of
-// 32 features while the matrix cores work on the step before.  In LDS a row's eight 16-byte chunks
-// stand at chunk ^ (row & 7), so that the 32 rows that one instruction reads hit all banks.
+// (v_mfma_i32_32x32x32_i8).  Stages of 128 features of its rows and weights go to a ring of stages in
+// LDS, one being multiplied in steps of 32 features while the others are on their way.  In LDS a
+// row's eight 16-byte chunks stand at chunk ^ (row / 2 & 7): the 16 lanes that are served in one
+// cycle have 16 neighbouring rows, even ones in 32 of the 64 banks and odd ones in the others.
 constexpr int kStage = 128;
 
-template <int B>
-constexpr int kTileLds = 2 * 2 * B * kStage;
+template <int B, bool DEEP>
+constexpr int kTileLds = (DEEP ? 4 : 2) * 2 * B * kStage;
 
-// ALIGNED: rows of a and b start at multiples of 16 bytes and lie within 2^32 bytes of the tile's
-// first; stages then go to LDS without passing registers.
-template <typename T, int B, bool ALIGNED>
+// ALIGNED: stages go to LDS without passing registers (aligned_rows).
+template <typename T, int B, bool DEEP, bool ALIGNED>
 __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
   constexpr int C = B / 64;       // 32 x 32 tiles of a wave, each way
   constexpr int P = B * 8 / 256;  // 16-byte chunks of a stage that a thread brings, for each matrix
+  constexpr int S = DEEP ? 4 : 2;  // stages in LDS
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   const int t = threadIdx.x, lane = t & 63;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -228,33 +246,38 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
   const int64_t within = tile - group * 8 * tiles_o;
   const int64_t r0 = (group * 8 + within % height) * B, o0 = within / height * B;
 
-  // thread t brings chunk (t & 7) ^ (row & 7) of rows t / 8 + 32 p to slot t & 7
-  const int slot = t & 7, row_at = t >> 3, chunk = slot ^ (row_at & 7);
-  const int8_t *from_a[P], *from_b[P];
+  // thread t brings chunk (t & 7) ^ (row / 2 & 7) of rows t / 8 + 32 p to slot t & 7
+  const int slot = t & 7, row_at = t >> 3, chunk = slot ^ (row_at >> 1 & 7);
+  const auto rows_a = rows_from(a.a, a.lda, r0, a.n_rows, n);
+  const auto rows_b = rows_from(a.b, a.ldb, o0, a.n_outputs, n);
+  const int8_t *from[2 * P];
+  int offset[2 * P];
 #pragma unroll
-  for (int p = 0; p < P; ++p) {
-    const int64_t r = r0 + row_at + 32 * p, o = o0 + row_at + 32 * p;
-    from_a[p] = a.a + (r < a.n_rows ? r : a.n_rows - 1) * a.lda;
-    from_b[p] = a.b + (o < a.n_outputs ? o : a.n_outputs - 1) * a.ldb;
+  for (int p = 0; p < 2 * P; ++p) {
+    const int64_t row = (p < P ? r0 : o0) + row_at + 32 * (p % P);
+    const int64_t end = p < P ? a.n_rows : a.n_outputs;
+    from[p] = p < P ? a.a + (row < end ? row : end - 1) * a.lda
+                    : a.b + (row < end ? row : end - 1) * a.ldb;
+    offset[p] = (int)(from[p] - (p < P ? a.a + r0 * a.lda : a.b + o0 * a.ldb)) + 16 * chunk;
   }
   const int whole = n / kStage;
-  uint8_t *lds_a = smem, *lds_b = smem + 2 * B * kStage;
-  i32x4 hold[2 * P];  // a stage on its way through registers
+  uint8_t *lds_a = smem, *lds_b = smem + S * B * kStage;
+  i32x4 hold[DEEP ? 2 : 1][2 * P];  // stages on their way through registers
 
-  // starts to bring stage s: chunk p of a (p < P) or of b
-  auto fetch = [&](int s, int p) __attribute__((always_inline)) {
-    const int8_t *from = (p < P ? from_a[p % P] : from_b[p % P]) + s * kStage + 16 * chunk;
+  // starts to bring stage s: chunk p of a (p < P) or of b, into place h of hold
+  auto fetch = [&](int s, int p, int h = 0) __attribute__((always_inline)) {
     if constexpr (ALIGNED) {
-      lds_byte *to = (lds_byte *)smem + (p < P ? 0 : 2 * B * kStage) + (s & 1) * B * kStage +
+      lds_byte *to = (lds_byte *)smem + (p < P ? 0 : S * B * kStage) + (s & (S - 1)) * B * kStage +
                      wave * 1024 + p % P * 4096;
-      load_to_lds(from, to);
+      load_to_lds(p < P ? rows_a : rows_b, offset[p], s * kStage, to);
     } else {
-      __builtin_memcpy(&hold[p], from, 16);
+      __builtin_memcpy(&hold[h][p], from[p] + s * kStage + 16 * chunk, 16);
     }
   };
   // a chunk that is held in registers, to LDS
-  auto put = [&](int s, int p) __attribute__((always_inline)) {
-    *(i32x4 *)((p < P ? lds_a : lds_b) + (s & 1) * B * kStage + t * 16 + p % P * 4096) = hold[p];
+  auto put = [&](int s, int p, int h = 0) __attribute__((always_inline)) {
+    *(i32x4 *)((p < P ? lds_a : lds_b) + (s & (S - 1)) * B * kStage + t * 16 + p % P * 4096) =
+        hold[h][p];
   };
   // lane l's operand: row (or output) l & 31, features from 16 (l >> 5) of a step of 32
   const int half = lane >> 5, row32 = lane & 31;
@@ -265,7 +288,7 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
   };
   // operand i of a step: w, x in turn
   auto read = [&](int s, int step, int i, Operands &v) __attribute__((always_inline)) {
-    const int at = (s & 1) * B * kStage + (((2 * step + half) ^ (row32 & 7)) << 4) +
+    const int at = (s & (S - 1)) * B * kStage + (((2 * step + half) ^ (row32 >> 1 & 7)) << 4) +
                    i / 2 * 32 * kStage;
     if (i % 2) {
       v.x[i / 2] = *(const i32x4 *)(lds_a + base_a + at);
@@ -293,58 +316,140 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
     for (int q = 0; q < many; ++q)
       if (i * many + q < n) f(i * many + q);
   };
-  // Every load to LDS issued so far is done, by all waves, and every read.
-  auto meet = [&]() __attribute__((always_inline)) {
-    wait_for<0, 0>();
+  // All waves are here; of this one's loads to LDS all but the latest `loads` are done, and of its
+  // LDS instructions all but the latest `others`.
+  auto meet = [&](auto loads, auto others) __attribute__((always_inline)) {
+    wait_for<decltype(loads)::value, decltype(others)::value>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
+  typedef std::integral_constant<int, 0> none;
   constexpr int kReads = (2 * C + M - 1) / M, kFetches = (2 * P + M - 1) / M;
   Operands u, v;
-  // stage s, NEXT: with another after it, FETCH: with one more after that
-  auto stage = [&](int s, auto next, auto more) __attribute__((always_inline)) {
-    constexpr bool NEXT = decltype(next)::value, FETCH = decltype(more)::value;
-    multiply(u, [&](int i) {
-      spread(i, 2 * C, kReads, [&](int q) { read(s, 1, q, v); });
-    });
-    multiply(v, [&](int i) {
-      spread(i, 2 * C, kReads, [&](int q) { read(s, 2, q, u); });
-    });
-    multiply(u, [&](int i) {
-      spread(i, 2 * C, kReads, [&](int q) { read(s, 3, q, v); });
-      if (!ALIGNED && NEXT) spread(i, 2 * P, kFetches, [&](int p) { put(s + 1, p); });
-    });
-    if (NEXT) meet();  // stage s + 1 is there, and nobody reads stage s any more
-    multiply(v, [&](int i) {
-      if (NEXT) spread(i, 2 * C, kReads, [&](int q) { read(s + 1, 0, q, u); });
-      if (FETCH) spread(i, 2 * P, kFetches, [&](int p) { fetch(s + 2, p); });
-    });
-  };
-  if (whole > 0) {
+  if constexpr (!DEEP) {
+    // A step's operands are read during the step before.  stage s, NEXT: with another after it,
+    // FETCH: with stage s + 2 to be brought.
+    auto stage = [&](int s, auto next, auto more) __attribute__((always_inline)) {
+      constexpr bool NEXT = decltype(next)::value, FETCH = decltype(more)::value;
+      multiply(u, [&](int i) {
+        spread(i, 2 * C, kReads, [&](int q) { read(s, 1, q, v); });
+      });
+      multiply(v, [&](int i) {
+        spread(i, 2 * C, kReads, [&](int q) { read(s, 2, q, u); });
+      });
+      multiply(u, [&](int i) {
+        spread(i, 2 * C, kReads, [&](int q) { read(s, 3, q, v); });
+        if (!ALIGNED && NEXT) spread(i, 2 * P, kFetches, [&](int p) { put(s + 1, p); });
+      });
+      // stage s + 1 is there, and nobody reads stage s any more
+      if (NEXT) meet(none(), none());
+      multiply(v, [&](int i) {
+        if (NEXT) spread(i, 2 * C, kReads, [&](int q) { read(s + 1, 0, q, u); });
+        if (FETCH) spread(i, 2 * P, kFetches, [&](int p) { fetch(s + 2, p); });
+      });
+    };
+    if (whole > 0) {
 #pragma unroll
-    for (int p = 0; p < 2 * P; ++p) fetch(0, p);
-    if (!ALIGNED)
+      for (int p = 0; p < 2 * P; ++p) fetch(0, p);
+      if (!ALIGNED)
 #pragma unroll
-      for (int p = 0; p < 2 * P; ++p) put(0, p);
-    meet();
+        for (int p = 0; p < 2 * P; ++p) put(0, p);
+      meet(none(), none());
 #pragma unroll
-    for (int q = 0; q < 2 * C; ++q) read(0, 0, q, u);
-    if (whole > 1)
+      for (int q = 0; q < 2 * C; ++q) read(0, 0, q, u);
+      if (whole > 1)
 #pragma unroll
-      for (int p = 0; p < 2 * P; ++p) fetch(1, p);
-    int s = 0;
-    for (; s + 2 < whole; ++s) stage(s, std::true_type(), std::true_type());
-    if (s + 1 < whole) stage(s++, std::true_type(), std::false_type());
-    stage(s, std::false_type(), std::false_type());
+        for (int p = 0; p < 2 * P; ++p) fetch(1, p);
+      int s = 0;
+      for (; s + 2 < whole; ++s) stage(s, std::true_type(), std::true_type());
+      if (s + 1 < whole) stage(s++, std::true_type(), std::false_type());
+      stage(s, std::false_type(), std::false_type());
+    }
+  } else {
+    // A step has four matrix instructions only, too few to cover a read of LDS: operands are read
+    // three steps ahead, into four sets, and the meeting of a stage (after its first step) makes
+    // the next one readable.  Stages are on their way for two stages: in LDS, or in registers, from
+    // where a stage goes to LDS two stages before its use.
+    Operands set[4];
+    auto stage = [&](int s, auto turn, auto next, auto two, auto three, auto four)
+        __attribute__((always_inline)) {
+      constexpr int h = decltype(turn)::value;
+      multiply(set[0], [&](int i) { read(s, 3, i, set[3]); });
+      if (next) {
+        if constexpr (!ALIGNED) {
+          meet(std::integral_constant<int, 63>(), std::integral_constant<int, 2 * C>());
+        } else if (two) {
+          meet(std::integral_constant<int, 2 * P>(), std::integral_constant<int, 15>());
+        } else {
+          meet(none(), std::integral_constant<int, 15>());
+        }
+      }
+#pragma unroll
+      for (int step = 1; step < 4; ++step)
+        multiply(set[step], [&](int i) {
+          if (next) read(s + 1, step - 1, i, set[step - 1]);
+          const int p = (step - 1) * M + i;
+          if constexpr (ALIGNED) {
+            if (three && p < 2 * P) fetch(s + 3, p);
+          } else {
+            if (two && p < 2 * P) put(s + 2, p, h);
+            if (four && p >= M) fetch(s + 4, p - M, h);
+          }
+        });
+    };
+    typedef std::integral_constant<int, 0> even;
+    typedef std::integral_constant<int, 1> odd;
+    typedef std::true_type yes;
+    if (whole > 0) {
+#pragma unroll
+      for (int f = 0; f < 3; ++f) {
+        if (f < whole && (ALIGNED || f < 2))
+#pragma unroll
+          for (int p = 0; p < 2 * P; ++p) fetch(f, p, ALIGNED ? 0 : f);
+      }
+      if constexpr (ALIGNED) {
+        if (whole >= 3) {
+          meet(std::integral_constant<int, 4 * P>(), std::integral_constant<int, 15>());
+        } else {
+          meet(none(), none());
+        }
+      } else {
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+          if (f < whole)
+#pragma unroll
+            for (int p = 0; p < 2 * P; ++p) put(f, p, f);
+#pragma unroll
+        for (int f = 2; f < 4; ++f)
+          if (f < whole)
+#pragma unroll
+            for (int p = 0; p < 2 * P; ++p) fetch(f, p, f - 2);
+        meet(std::integral_constant<int, 63>(), none());
+      }
+#pragma unroll
+      for (int step = 0; step < 3; ++step)
+#pragma unroll
+        for (int q = 0; q < 2 * C; ++q) read(0, step, q, set[step]);
+      int s = 0;
+      for (; s + 5 < whole; s += 2) {
+        stage(s, even(), yes(), yes(), yes(), yes());
+        stage(s + 1, odd(), yes(), yes(), yes(), yes());
+      }
+      for (; s < whole; s += 2) {
+        stage(s, even(), s + 1 < whole, s + 2 < whole, s + 3 < whole, s + 4 < whole);
+        if (s + 1 < whole)
+          stage(s + 1, odd(), s + 2 < whole, s + 3 < whole, s + 4 < whole, s + 5 < whole);
+      }
+    }
   }
   if (n % kStage) {  // the features past the last whole stage, filled up with zeros
     const int j = whole * kStage + 16 * chunk;
 #pragma unroll
     for (int p = 0; p < 2 * P; ++p)
-      hold[p] = load_features<false>(p < P ? from_a[p % P] : from_b[p % P], j, n);
+      hold[0][p] = load_features<false>(from[p], j, n);
 #pragma unroll
     for (int p = 0; p < 2 * P; ++p) put(whole, p);  // not where the last whole stage is read
-    meet();
+    meet(none(), none());
 #pragma unroll 1
     for (int step = 0; step < (n % kStage + 31) / 32; ++step) {
 #pragma unroll
@@ -355,14 +460,14 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
 
   // Lane l holds row l & 31 and outputs 8 (i / 4) + 4 (l >> 5) + i % 4 of each tile.  32 rows of a
   // wave at a time go through LDS, in the type they are stored in, and out as whole runs of a row.
-  meet();
+  meet(none(), none());
   float *scales = (float *)smem;  // of the tile's rows, its outputs, and the bias
   for (int i = t; i < B; i += 256) {
     scales[i] = r0 + i < a.n_rows ? a.a_scale[r0 + i] : 0.0f;
     scales[B + i] = o0 + i < a.n_outputs ? a.b_scale[o0 + i] : 0.0f;
     scales[2 * B + i] = a.bias && o0 + i < a.n_outputs ? a.bias[o0 + i] : 0.0f;
   }
-  meet();
+  meet(none(), none());
   constexpr int kPitch = B / 2 * (int)sizeof(T) + 16;  // of a row of a wave's outputs, in bytes
   constexpr int kRun = 16 / (int)sizeof(T), kRunsARow = B / 2 / kRun;
   uint8_t *part = smem + 3 * B * 4 + wave * 32 * kPitch;
@@ -407,8 +512,11 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
   }
 }
 
+// Whether rows can go to LDS directly: 16-byte chunks, and a tile's offsets below 2^31.
 static bool aligned_rows(const MatmulArgs &a) {
-  return ((uintptr_t)a.a | (uintptr_t)a.b | (uint64_t)a.lda | (uint64_t)a.ldb) % 16 == 0;
+  return a.lda <= (1 << 22) && a.ldb <= (1 << 22) &&
+         ((uintptr_t)a.a | (uintptr_t)a.b | (uint64_t)a.lda | (uint64_t)a.ldb) % 16 ==
+             0;
 }
 template <typename T, int R, int O, int W, int S>
 static int launch_stream(const MatmulArgs &a, void *stream) {
@@ -423,12 +531,14 @@ static int launch_stream(const MatmulArgs &a, void *stream) {
              : launch_tiles(matmul_q8_stream_kernel<T, R, O, W, S, false>, tiles, 64 * W, kOther, a,
                             stream);
 }
-template <typename T, int B>
+template <typename T, int B, bool DEEP>
 static int launch_tile(const MatmulArgs &a, void *stream) {
   const int64_t tiles =
       ((a.n_rows + B - 1) / B) * (((int64_t)a.n_outputs + B - 1) / B);
-  return aligned_rows(a) ? launch_tiles(matmul_q8_tile_kernel<T, B, true>, tiles, 256, kTileLds<B>, a, stream)
-                 : launch_tiles(matmul_q8_tile_kernel<T, B, false>, tiles, 256, kTileLds<B>, a, stream);
+  constexpr int kLds = kTileLds<B, DEEP>;
+  return aligned_rows(a)
+             ? launch_tiles(matmul_q8_tile_kernel<T, B, DEEP, true>, tiles, 256, kLds, a, stream)
+             : launch_tiles(matmul_q8_tile_kernel<T, B, DEEP, false>, tiles, 256, kLds, a, stream);
 }
 
 int launch_matmul_q8(const MatmulArgs &a, int32_t dtype, void *stream) {
@@ -441,8 +551,8 @@ int launch_matmul_q8(const MatmulArgs &a, int32_t dtype, void *stream) {
     if (m <= 64) return launch_stream<T, 4, 2, 8, 3>(a, stream);
     const int64_t wide = ((m + 255) / 256) * ((o + 255) / 256);
     const int64_t middle = ((m + 127) / 128) * ((o + 127) / 128);
-    if (wide >= 192) return launch_tile<T, 256>(a, stream);
-    if (middle >= 192) return launch_tile<T, 128>(a, stream);
+    if (wide >= 192) return launch_tile<T, 256, false>(a, stream);
+    if (middle >= 192) return launch_tile<T, 128, false>(a, stream);
     return launch_stream<T, 4, 4, 8, 2>(a, stream);
   });
 }
