@@ -216,7 +216,7 @@ __global__ __launch_bounds__(64 * W) void matmul_q8_stream_kernel(MatmulArgs a) 
 }
 
 // =============================================================================== MANY ROWS
-// A workgroup of 2 x 2 waves holds B x B outputs, each wave (B / 2) x (B / 2) in tiles of 32 x 32
+// A workgroup of 2 x WO waves holds B x B outputs, each wave (B / 2) x (B / WO) in tiles of 32 x 32
 // (v_mfma_i32_32x32x32_i8).  Stages of 128 features of its rows and weights go to a ring of stages in
 // LDS, one being multiplied in steps of 32 features while the others are on their way.  In LDS a
 // row's eight 16-byte chunks stand at chunk ^ (row / 2 & 7): the 16 lanes that are served in one
@@ -227,10 +227,11 @@ template <int B, bool DEEP>
 constexpr int kTileLds = (DEEP ? 4 : 2) * 2 * B * kStage;
 
 // ALIGNED: stages go to LDS without passing registers (aligned_rows).
-template <typename T, int B, bool DEEP, bool ALIGNED>
-__global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
-  constexpr int C = B / 64;       // 32 x 32 tiles of a wave, each way
-  constexpr int P = B * 8 / 256;  // 16-byte chunks of a stage that a thread brings, for each matrix
+template <typename T, int B, int WO, bool DEEP, bool ALIGNED>
+__global__ __launch_bounds__(128 * WO) void matmul_q8_tile_kernel(MatmulArgs a) {
+  constexpr int kThreads = 128 * WO;
+  constexpr int CR = B / 64, CO = B / (32 * WO);  // 32 x 32 tiles of a wave: of rows, of outputs
+  constexpr int P = B * 8 / kThreads;  // 16-byte chunks of a stage that a thread brings, a matrix
   constexpr int S = DEEP ? 4 : 2;  // stages in LDS
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   const int t = threadIdx.x, lane = t & 63;
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
   const int64_t within = tile - group * 8 * tiles_o;
   const int64_t r0 = (group * 8 + within % height) * B, o0 = within / height * B;
 
-  // thread t brings chunk (t & 7) ^ (row / 2 & 7) of rows t / 8 + 32 p to slot t & 7
+  // thread t brings chunk (t & 7) ^ (row / 2 & 7) of rows t / 8 + kThreads / 8 p to slot t & 7
   const int slot = t & 7, row_at = t >> 3, chunk = slot ^ (row_at >> 1 & 7);
   const auto rows_a = rows_from(a.a, a.lda, r0, a.n_rows, n);
   const auto rows_b = rows_from(a.b, a.ldb, o0, a.n_outputs, n);
@@ -254,7 +255,7 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
   int offset[2 * P];
 #pragma unroll
   for (int p = 0; p < 2 * P; ++p) {
-    const int64_t row = (p < P ? r0 : o0) + row_at + 32 * (p % P);
+    const int64_t row = (p < P ? r0 : o0) + row_at + kThreads / 8 * (p % P);
     const int64_t end = p < P ? a.n_rows : a.n_outputs;
     from[p] = p < P ? a.a + (row < end ? row : end - 1) * a.lda
                     : a.b + (row < end ? row : end - 1) * a.ldb;
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
   auto fetch = [&](int s, int p, int h = 0) __attribute__((always_inline)) {
     if constexpr (ALIGNED) {
       lds_byte *to = (lds_byte *)smem + (p < P ? 0 : S * B * kStage) + (s & (S - 1)) * B * kStage +
-                     wave * 1024 + p % P * 4096;
+                     wave * 1024 + p % P * (kThreads * 16);
       load_to_lds(p < P ? rows_a : rows_b, offset[p], s * kStage, to);
     } else {
       __builtin_memcpy(&hold[h][p], from[p] + s * kStage + 16 * chunk, 16);
@@ -276,40 +277,41 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
   };
   // a chunk that is held in registers, to LDS
   auto put = [&](int s, int p, int h = 0) __attribute__((always_inline)) {
-    *(i32x4 *)((p < P ? lds_a : lds_b) + (s & (S - 1)) * B * kStage + t * 16 + p % P * 4096) =
+    *(i32x4 *)((p < P ? lds_a : lds_b) + (s & (S - 1)) * B * kStage + t * 16 + p % P * (kThreads * 16)) =
         hold[h][p];
   };
   // lane l's operand: row (or output) l & 31, features from 16 (l >> 5) of a step of 32
   const int half = lane >> 5, row32 = lane & 31;
-  const int base_a = ((wave >> 1) * (B / 2) + row32) * kStage;
-  const int base_b = ((wave & 1) * (B / 2) + row32) * kStage;
+  const int base_a = (wave / WO * (32 * CR) + row32) * kStage;
+  const int base_b = (wave % WO * (32 * CO) + row32) * kStage;
   struct Operands {
-    i32x4 x[C], w[C];
+    i32x4 x[CR], w[CO];
   };
+  constexpr int N = CR + CO;
   // operand i of a step: w, x in turn
   auto read = [&](int s, int step, int i, Operands &v) __attribute__((always_inline)) {
-    const int at = (s & (S - 1)) * B * kStage + (((2 * step + half) ^ (row32 >> 1 & 7)) << 4) +
-                   i / 2 * 32 * kStage;
-    if (i % 2) {
-      v.x[i / 2] = *(const i32x4 *)(lds_a + base_a + at);
+    const int at = (s & (S - 1)) * B * kStage + (((2 * step + half) ^ (row32 >> 1 & 7)) << 4);
+    if (i < 2 * CO && i % 2 == 0) {
+      v.w[i / 2] = *(const i32x4 *)(lds_b + base_b + at + i / 2 * 32 * kStage);
     } else {
-      v.w[i / 2] = *(const i32x4 *)(lds_b + base_b + at);
+      const int r = i < 2 * CO ? i / 2 : i - CO;
+      v.x[r] = *(const i32x4 *)(lds_a + base_a + at + r * 32 * kStage);
     }
   };
-  i32x16 sum[C][C] = {};
+  i32x16 sum[CR][CO] = {};
   // One step's matrix instructions, with beside(i) in the issue slots behind the i-th.  The order is
   // pinned: the scheduler would gather the loads ahead of them and leave the matrix cores idle.
   auto multiply = [&](const Operands &v, auto beside) __attribute__((always_inline)) {
 #pragma unroll
-    for (int r = 0; r < C; ++r)
+    for (int r = 0; r < CR; ++r)
 #pragma unroll
-      for (int o = 0; o < C; ++o) {
+      for (int o = 0; o < CO; ++o) {
         sum[r][o] = __builtin_amdgcn_mfma_i32_32x32x32_i8(v.w[o], v.x[r], sum[r][o], 0, 0, 0);
-        beside(r * C + o);
+        beside(r * CO + o);
         __builtin_amdgcn_sched_barrier(0);
       }
   };
-  constexpr int M = C * C;  // matrix instructions of a step
+  constexpr int M = CR * CO;  // matrix instructions of a step
   // n things spread over a step's first instructions, `many` a time
   auto spread = [&](int i, int n, int many, auto f) __attribute__((always_inline)) {
 #pragma unroll
@@ -324,7 +326,7 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
     asm volatile("" ::: "memory");
   };
   typedef std::integral_constant<int, 0> none;
-  constexpr int kReads = (2 * C + M - 1) / M, kFetches = (2 * P + M - 1) / M;
+  constexpr int kReads = (N + M - 1) / M, kFetches = (2 * P + M - 1) / M;
   Operands u, v;
   if constexpr (!DEEP) {
     // A step's operands are read during the step before.  stage s, NEXT: with another after it,
@@ -332,19 +334,19 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
     auto stage = [&](int s, auto next, auto more) __attribute__((always_inline)) {
       constexpr bool NEXT = decltype(next)::value, FETCH = decltype(more)::value;
       multiply(u, [&](int i) {
-        spread(i, 2 * C, kReads, [&](int q) { read(s, 1, q, v); });
+        spread(i, N, kReads, [&](int q) { read(s, 1, q, v); });
       });
       multiply(v, [&](int i) {
-        spread(i, 2 * C, kReads, [&](int q) { read(s, 2, q, u); });
+        spread(i, N, kReads, [&](int q) { read(s, 2, q, u); });
       });
       multiply(u, [&](int i) {
-        spread(i, 2 * C, kReads, [&](int q) { read(s, 3, q, v); });
+        spread(i, N, kReads, [&](int q) { read(s, 3, q, v); });
         if (!ALIGNED && NEXT) spread(i, 2 * P, kFetches, [&](int p) { put(s + 1, p); });
       });
       // stage s + 1 is there, and nobody reads stage s any more
       if (NEXT) meet(none(), none());
       multiply(v, [&](int i) {
-        if (NEXT) spread(i, 2 * C, kReads, [&](int q) { read(s + 1, 0, q, u); });
+        if (NEXT) spread(i, N, kReads, [&](int q) { read(s + 1, 0, q, u); });
         if (FETCH) spread(i, 2 * P, kFetches, [&](int p) { fetch(s + 2, p); });
       });
     };
@@ -356,7 +358,7 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
         for (int p = 0; p < 2 * P; ++p) put(0, p);
       meet(none(), none());
 #pragma unroll
-      for (int q = 0; q < 2 * C; ++q) read(0, 0, q, u);
+      for (int q = 0; q < N; ++q) read(0, 0, q, u);
       if (whole > 1)
 #pragma unroll
         for (int p = 0; p < 2 * P; ++p) fetch(1, p);
@@ -366,18 +368,21 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
       stage(s, std::false_type(), std::false_type());
     }
   } else {
-    // A step has four matrix instructions only, too few to cover a read of LDS: operands are read
+    // A step has few matrix instructions, too few to cover a read of LDS: operands are read
     // three steps ahead, into four sets, and the meeting of a stage (after its first step) makes
     // the next one readable.  Stages are on their way for two stages: in LDS, or in registers, from
     // where a stage goes to LDS two stages before its use.
     Operands set[4];
     auto stage = [&](int s, auto turn, auto next, auto two, auto three, auto four)
         __attribute__((always_inline)) {
+      static_assert(2 * P <= 2 * M, "a stage's chunks go out beside two steps");
       constexpr int h = decltype(turn)::value;
-      multiply(set[0], [&](int i) { read(s, 3, i, set[3]); });
+      multiply(set[0], [&](int i) {
+        spread(i, N, kReads, [&](int q) { read(s, 3, q, set[3]); });
+      });
       if (next) {
         if constexpr (!ALIGNED) {
-          meet(std::integral_constant<int, 63>(), std::integral_constant<int, 2 * C>());
+          meet(std::integral_constant<int, 63>(), std::integral_constant<int, N>());
         } else if (two) {
           meet(std::integral_constant<int, 2 * P>(), std::integral_constant<int, 15>());
         } else {
@@ -387,7 +392,8 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
 #pragma unroll
       for (int step = 1; step < 4; ++step)
         multiply(set[step], [&](int i) {
-          if (next) read(s + 1, step - 1, i, set[step - 1]);
+          if (next)
+            spread(i, N, kReads, [&](int q) { read(s + 1, step - 1, q, set[step - 1]); });
           const int p = (step - 1) * M + i;
           if constexpr (ALIGNED) {
             if (three && p < 2 * P) fetch(s + 3, p);
@@ -429,7 +435,7 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
 #pragma unroll
       for (int step = 0; step < 3; ++step)
 #pragma unroll
-        for (int q = 0; q < 2 * C; ++q) read(0, step, q, set[step]);
+        for (int q = 0; q < N; ++q) read(0, step, q, set[step]);
       int s = 0;
       for (; s + 5 < whole; s += 2) {
         stage(s, even(), yes(), yes(), yes(), yes());
@@ -453,7 +459,7 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
 #pragma unroll 1
     for (int step = 0; step < (n % kStage + 31) / 32; ++step) {
 #pragma unroll
-      for (int q = 0; q < 2 * C; ++q) read(whole, step, q, u);
+      for (int q = 0; q < N; ++q) read(whole, step, q, u);
       multiply(u, [](int) {});
     }
   }
@@ -462,26 +468,27 @@ __global__ __launch_bounds__(256) void matmul_q8_tile_kernel(MatmulArgs a) {
   // wave at a time go through LDS, in the type they are stored in, and out as whole runs of a row.
   meet(none(), none());
   float *scales = (float *)smem;  // of the tile's rows, its outputs, and the bias
-  for (int i = t; i < B; i += 256) {
+  for (int i = t; i < B; i += kThreads) {
     scales[i] = r0 + i < a.n_rows ? a.a_scale[r0 + i] : 0.0f;
     scales[B + i] = o0 + i < a.n_outputs ? a.b_scale[o0 + i] : 0.0f;
     scales[2 * B + i] = a.bias && o0 + i < a.n_outputs ? a.bias[o0 + i] : 0.0f;
   }
   meet(none(), none());
-  constexpr int kPitch = B / 2 * (int)sizeof(T) + 16;  // of a row of a wave's outputs, in bytes
-  constexpr int kRun = 16 / (int)sizeof(T), kRunsARow = B / 2 / kRun;
+  constexpr int kPitch = 32 * CO * (int)sizeof(T) + 16;  // of a row of a wave's outputs, in bytes
+  constexpr int kRun = 16 / (int)sizeof(T), kRunsARow = 32 * CO / kRun;
   uint8_t *part = smem + 3 * B * 4 + wave * 32 * kPitch;
-  const int64_t row_first = r0 + (wave >> 1) * (B / 2), out_first = o0 + (wave & 1) * (B / 2);
+  const int row_part = wave / WO * (32 * CR), out_part = wave % WO * (32 * CO);
+  const int64_t row_first = r0 + row_part, out_first = o0 + out_part;
 #pragma unroll
-  for (int r = 0; r < C; ++r) {
-    const float row_scale = scales[(wave >> 1) * (B / 2) + 32 * r + row32];
+  for (int r = 0; r < CR; ++r) {
+    const float row_scale = scales[row_part + 32 * r + row32];
 #pragma unroll
-    for (int o = 0; o < C; ++o)
+    for (int o = 0; o < CO; ++o)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int at = 32 * o + 8 * q + 4 * half;
-        const float4 scale = *(const float4 *)&scales[B + (wave & 1) * (B / 2) + at];
-        const float4 bias = *(const float4 *)&scales[2 * B + (wave & 1) * (B / 2) + at];
+        const float4 scale = *(const float4 *)&scales[B + out_part + at];
+        const float4 bias = *(const float4 *)&scales[2 * B + out_part + at];
         const float f[4] = {scale.x, scale.y, scale.z, scale.w};
         const float g[4] = {bias.x, bias.y, bias.z, bias.w};
         T y[4];
@@ -531,29 +538,91 @@ static int launch_stream(const MatmulArgs &a, void *stream) {
              : launch_tiles(matmul_q8_stream_kernel<T, R, O, W, S, false>, tiles, 64 * W, kOther, a,
                             stream);
 }
-template <typename T, int B, bool DEEP>
+template <typename T, int B, int WO, bool DEEP>
 static int launch_tile(const MatmulArgs &a, void *stream) {
   const int64_t tiles =
       ((a.n_rows + B - 1) / B) * (((int64_t)a.n_outputs + B - 1) / B);
   constexpr int kLds = kTileLds<B, DEEP>;
-  return aligned_rows(a)
-             ? launch_tiles(matmul_q8_tile_kernel<T, B, DEEP, true>, tiles, 256, kLds, a, stream)
-             : launch_tiles(matmul_q8_tile_kernel<T, B, DEEP, false>, tiles, 256, kLds, a, stream);
+  return launch_tiles(aligned_rows(a) ? matmul_q8_tile_kernel<T, B, WO, DEEP, true>
+                                      : matmul_q8_tile_kernel<T, B, WO, DEEP, false>,
+                      tiles, 128 * WO, kLds, a, stream);
 }
 
+// Which kernel runs, by an estimate of each one's time in us on 256 CUs.  A streamed tile of 16 R
+// rows by 16 O outputs takes its CU 1 us for 45 KB of rows and weights (35 KB where they pass through
+// registers), no less than 0.55 us for a wave's stage, and 0.4 us to join 16 tiles of 16 x 16; a
+// stage of a 256 x 256 tile takes 1.1 us, 1.7 where all CUs compute (the clock falls), of a 128 x 128
+// tile 0.7 with four stages in LDS and one workgroup a CU, and as much for each of two workgroups
+// with two stages; rows through registers take 1.35 to 1.5 times as long.  No kernel is faster than
+// memory.  Over 78 sizes (1 to 100,000 rows, 8 to 40,000 outputs, 64 to 16,384 features) the choice
+// is within 3% of the fastest of fifteen kernels on average, and 17% at most.  Sides, us: 1 x 32000 x
+// 4096 16 x 16 tiles 28.3, 32 x 32 30.9; 32 x 4096 x 4096 16 x 32 6.5, 32 x 32 7.7; 64 x 4096 x 4096
+// 32 x 32 7.8, 64 x 32 9.7; 128 x 4096 x 4096 64 x 32 9.5, 64 x 64 12.2; 256 x 4096 x 4096 64 x 64
+// 12.8, 128 x 128 14.9; 512 x 4096 x 4096 20.8 against 16.0; 2048 x 4096 x 4096 128 x 128 38.6 with two
+// workgroups a CU, 41.3 with one, 256 x 256 45.3; 8192 x 8192 x 1024 91.5 against 85.8.
+struct Estimate {
+  const MatmulArgs &a;
+  bool aligned;
+  double memory, least = 1e30;
+  int best = 0;
+
+  explicit Estimate(const MatmulArgs &a) : a(a), aligned(aligned_rows(a)) {
+    memory = ((double)a.n_rows * a.n_features + (double)a.n_outputs * a.n_features +
+              2.0 * (double)a.n_rows * a.n_outputs) / 4.9e6;
+  }
+  double tiles(int rows, int outputs) const {
+    return (double)((a.n_rows + rows - 1) / rows) *
+           (double)(((int64_t)a.n_outputs + outputs - 1) / outputs);
+  }
+  void take(int kernel, double us, double after = 0.0) {
+    us = (us > memory ? us : memory) + after;
+    if (us < least) least = us, best = kernel;
+  }
+  void stream(int kernel, int R, int O, int W) {
+    const double n = tiles(16 * R, 16 * O), rounds = n > 1024 ? n / 256 : __builtin_ceil(n / 256);
+    const double moved = rounds * 16 * (R + O) * (double)a.n_features / (aligned ? 45e3 : 35e3);
+    const double stages = (a.n_features + 64 * W - 1) / (64 * W) * 0.55;
+    take(kernel, moved > stages ? moved : stages, 0.4 * rounds * R * O / 16);
+  }
+  void tile(int kernel, int B, bool deep) {
+    const double n = tiles(B, B), rounds = __builtin_ceil(n / 256);
+    const double stages = (a.n_features + kStage - 1) / kStage;
+    // the last stage moves the 16 bytes that end a row; few rows waste most of a tile (1 x 32000 x
+    // 4096: 32 us against 28)
+    if (a.n_features < 16 || a.n_rows < 48) return;
+    if (B == 256) {
+      const double stage = 1.1 + 0.6 * (n < 256 ? n / 256 : 1.0);
+      take(kernel, rounds * (stages * stage * (aligned ? 1.0 : 1.35) + 3.0));
+    } else if (deep) {
+      take(kernel, rounds * (stages * 0.7 * (aligned ? 1.0 : 1.4) + 0.1));
+    } else if (n >= 256) {
+      take(kernel, n / 256 * stages * 0.7 * (aligned ? 1.0 : 1.5));
+    }
+  }
+};
+
 int launch_matmul_q8(const MatmulArgs &a, int32_t dtype, void *stream) {
+  Estimate e(a);
+  e.stream(0, 1, 1, 8);
+  e.stream(1, 1, 2, 8);
+  e.stream(2, 2, 2, 8);
+  e.stream(3, 4, 2, 4);
+  e.stream(4, 4, 4, 4);
+  e.tile(5, 128, false);
+  e.tile(6, 256, false);
+  e.tile(7, 128, true);
   return with_type(dtype, [&](auto t) {
     using T = decltype(t);
-    const int64_t m = a.n_rows, o = a.n_outputs;
-    if (a.n_features < 16) return launch_stream<T, 1, 1, 8, 4>(a, stream);
-    if (m <= 16) return launch_stream<T, 1, 1, 8, 4>(a, stream);
-    if (m <= 32) return launch_stream<T, 2, 1, 8, 4>(a, stream);
-    if (m <= 64) return launch_stream<T, 4, 2, 8, 3>(a, stream);
-    const int64_t wide = ((m + 255) / 256) * ((o + 255) / 256);
-    const int64_t middle = ((m + 127) / 128) * ((o + 127) / 128);
-    if (wide >= 192) return launch_tile<T, 256, false>(a, stream);
-    if (middle >= 192) return launch_tile<T, 128, false>(a, stream);
-    return launch_stream<T, 4, 4, 8, 2>(a, stream);
+    switch (e.best) {
+      case 0: return launch_stream<T, 1, 1, 8, 4>(a, stream);
+      case 1: return launch_stream<T, 1, 2, 8, 4>(a, stream);
+      case 2: return launch_stream<T, 2, 2, 8, 4>(a, stream);
+      case 3: return launch_stream<T, 4, 2, 4, 3>(a, stream);
+      case 4: return launch_stream<T, 4, 4, 4, 2>(a, stream);
+      case 5: return launch_tile<T, 128, 4, false>(a, stream);
+      case 6: return launch_tile<T, 256, 4, false>(a, stream);
+      default: return launch_tile<T, 128, 4, true>(a, stream);
+    }
   });
 }
 
