@@ -63,9 +63,22 @@ __global__ __launch_bounds__(256) void top_k_lane_kernel(TopKArgs a) {
       }
     }
   }
+  T value[K];
 #pragma unroll
-  for (int p = 0; p < K; ++p)
-    if (p < a.k) store_slot<T>(a, row, p, id[p] >= 0 ? x[id[p]] : (T)-__builtin_inff(), id[p]);
+  for (int p = 0; p < K; ++p) {
+    const float v = value_of(best[p] - 1);
+    // the order holds a score's value, but not which zero or NaN it was
+    value[p] = id[p] < 0 ? (T)-__builtin_inff()
+               : v == 0.0f || v != v ? x[id[p]] : from_float<T>(v);
+  }
+  if (a.k == K) {  // whole slots of a lane in one store: a store of one slot each takes 64 cycles
+    if (a.values) __builtin_memcpy((T *)a.values + row * K, value, sizeof(value));
+    if (a.ids) __builtin_memcpy(a.ids + row * K, id, sizeof(id));
+  } else {
+#pragma unroll
+    for (int p = 0; p < K; ++p)
+      if (p < a.k) store_slot<T>(a, row, p, value[p], id[p]);
+  }
 }
 
 // =========================================================================== MANY CLASSES
@@ -334,7 +347,9 @@ int launch_top_k(const TopKArgs &a, int32_t dtype, void *stream) {
     if (a.k <= 16 && a.n_classes <= 64 &&
         ((int64_t)a.n_classes * a.k <= 256 || a.n_rows >= 8192)) {
       if (a.k == 1) return launch_rows(top_k_lane_kernel<T, 1>, 1, a, stream);
+      if (a.k == 2) return launch_rows(top_k_lane_kernel<T, 2>, 1, a, stream);
       if (a.k <= 4) return launch_rows(top_k_lane_kernel<T, 4>, 1, a, stream);
+      if (a.k <= 8) return launch_rows(top_k_lane_kernel<T, 8>, 1, a, stream);
       return launch_rows(top_k_lane_kernel<T, 16>, 1, a, stream);
     }
     auto of = [&](auto k, int threads) { return launch_each_row(k, threads, a, stream); };

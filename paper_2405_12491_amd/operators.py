@@ -73,55 +73,65 @@ def bridger_matmul_q8(a_ptr, lda, a_scale_ptr, b_ptr, ldb, b_scale_ptr, bias_ptr
 
 
 # ---------------------------------------------------------------- convenience
+# A call on few rows is bound by its way to the launch: torch and its types are looked up once, a
+# tensor's properties read once, and the entry points called without the functions above.
+_torch = None
 _codes = {}  # torch dtype -> BRIDGER_*
 
 
+def _setup():
+    global _torch
+    import torch
+    _codes.update({torch.float32: BRIDGER_F32, torch.bfloat16: BRIDGER_BF16,
+                   torch.float16: BRIDGER_F16})
+    _torch = torch
+    _B.load_library()
+
+
 def _code(dtype) -> int:
-    if not _codes:
-        import torch
-        _codes.update({torch.float32: BRIDGER_F32, torch.bfloat16: BRIDGER_BF16,
-                       torch.float16: BRIDGER_F16})
     code = _codes.get(dtype)
     if code is None:
         raise TypeError(f"{dtype} rows: float32, bfloat16 or float16 are supported")
     return code
 
 
-def _rows(t, name, width=None, n=None, dtype=None, device=None):
-    """Checks a 2-D tensor with contiguous rows; the distance between its rows in elements."""
-    import torch
-    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+def _rows(t, name, width, n, dtype, device):
+    """Checks a 2-D tensor with contiguous rows (None: any): (rows, width, the distance between rows
+    in elements)."""
+    if not (isinstance(t, _torch.Tensor) and t.is_cuda):
         raise TypeError(f"{name} must be a CUDA tensor")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must be of type {dtype}")
-    if device is not None and t.device != device:
+    if device is not None and t.get_device() != device:
         raise ValueError(f"{name} is on another device")
-    if t.dim() != 2 or (width is not None and t.shape[1] != width) or \
-            (n is not None and t.shape[0] != n):
+    shape = t.shape
+    if len(shape) != 2 or (width is not None and shape[1] != width) or \
+            (n is not None and shape[0] != n):
         raise ValueError(f"{name} must be [{'n' if n is None else n}, "
                          f"{'width' if width is None else width}]")
-    w = t.shape[1]
-    if w > 1 and t.stride(1) != 1:
+    rows, w = shape
+    step, inner = t.stride()
+    if w > 1 and inner != 1:
         raise ValueError(f"{name}'s rows must be contiguous")
-    if t.shape[0] <= 1:
-        return w
-    if t.stride(0) < w:
+    if rows <= 1:
+        return rows, w, w
+    if step < w:
         raise ValueError(f"{name}'s rows overlap")
-    return t.stride(0)
+    return rows, w, step
 
 
 def _vector(t, name, n, dtype, device):
-    import torch
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype):
+    if not (isinstance(t, _torch.Tensor) and t.is_cuda and t.dtype == dtype):
         raise TypeError(f"{name} must be a {dtype} CUDA tensor")
-    if t.device != device:
+    if t.get_device() != device:
         raise ValueError(f"{name} is on another device")
-    if t.dim() != 1 or t.shape[0] != n or not (n <= 1 or t.stride(0) == 1):
+    shape = t.shape
+    if len(shape) != 1 or shape[0] != n or not (n <= 1 or t.stride(0) == 1):
         raise ValueError(f"{name} must be contiguous [{n}]")
 
 
 def _dense(t, name, n, width, dtype, device):
-    if _rows(t, name, width, n, dtype, device) != width:
+    if _rows(t, name, width, n, dtype, device)[2] != width:
         raise ValueError(f"{name} must be contiguous")
 
 
@@ -129,74 +139,72 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _call(fn, device, *args):
-    """Calls an entry point on the current stream of `device`, with that device current."""
-    import torch
-    stream = _B._launch_stream(device)
-    if torch.cuda.current_device() == device.index:
-        fn(*args, stream)
+def _call(name, like, *args):
+    """Calls an entry point on the current stream of `like`'s device, with that device current."""
+    stream = _B._launch_stream(like.device)
+    fn = getattr(_B._lib, name)
+    if _torch.cuda.current_device() == like.get_device():
+        st = fn(*args, stream)
     else:
-        with torch.cuda.device(device):
-            fn(*args, stream)
+        with _torch.cuda.device(like.device):
+            st = fn(*args, stream)
+    if st != _B.BRIDGER_OK:
+        _B._check(st, name)
 
 
 def top_k(scores, k: int, values=None, ids=None):
     """The k largest of every row's scores, largest first (equal scores: the lower class first),
     and their class ids: (values [n, k] of scores' dtype, ids int32 [n, k]).  Slots beyond the
     number of classes hold -infinity and -1."""
-    import torch
-    ld = _rows(scores, "scores")
-    n, c = scores.shape
-    dev = scores.device
+    if _torch is None:
+        _setup()
+    n, c, ld = _rows(scores, "scores", None, None, None, None)
+    dev = scores.get_device()
     if values is None:
         values = scores.new_empty((n, k))
     else:
         _dense(values, "values", n, k, scores.dtype, dev)
     if ids is None:
-        ids = scores.new_empty((n, k), dtype=torch.int32)
+        ids = scores.new_empty((n, k), dtype=_torch.int32)
     else:
-        _dense(ids, "ids", n, k, torch.int32, dev)
-    _call(bridger_top_k, dev, scores.data_ptr(), ld, _code(scores.dtype), n, c, k,
+        _dense(ids, "ids", n, k, _torch.int32, dev)
+    _call("bridger_top_k", scores, scores.data_ptr(), ld, _code(scores.dtype), n, c, k,
           values.data_ptr(), ids.data_ptr())
     return values, ids
 
 
 def _check_distill(logits, ids, teacher, weight):
-    import torch
-    ld = _rows(logits, "logits")
-    n, dev = logits.shape[0], logits.device
-    if _rows(ids, "ids", None, n, torch.int32, dev) != ids.shape[1]:
+    """What both passes take first, from checked tensors: (rows, classes, first arguments)."""
+    n, c, ld = _rows(logits, "logits", None, None, None, None)
+    dev = logits.get_device()
+    _, k, step = _rows(ids, "ids", None, n, _torch.int32, dev)
+    if step != k:
         raise ValueError("ids must be contiguous")
-    _dense(teacher, "teacher", n, ids.shape[1], teacher.dtype, dev)
+    _dense(teacher, "teacher", n, k, None, dev)
     if weight is not None:
-        _vector(weight, "weight", n, torch.float32, dev)
-    return ld, _code(logits.dtype), _code(teacher.dtype)
-
-
-def _forward(logits, ids, teacher, temperature, weight, loss, stats, grad):
-    ld, code, teacher_code = _check_distill(logits, ids, teacher, weight)
-    ldg = 0 if grad is None else _rows(grad, "grad", logits.shape[1], logits.shape[0],
-                                       logits.dtype, logits.device)
-    _call(bridger_distill, logits.device, logits.data_ptr(), ld, code, ids.data_ptr(),
-          teacher.data_ptr(), teacher_code, logits.shape[0], logits.shape[1], ids.shape[1],
-          float(temperature), _ptr(weight), _ptr(loss), _ptr(stats), _ptr(grad), ldg)
+        _vector(weight, "weight", n, _torch.float32, dev)
+    return n, c, (logits.data_ptr(), ld, _code(logits.dtype), ids.data_ptr(), teacher.data_ptr(),
+                  _code(teacher.dtype), n, c, k)
 
 
 def distill(logits, ids, teacher, temperature: float = 1.0, weight=None, grad=None, loss=None):
     """Loss of every row [n] (float32) and its gradient [n, classes] (of logits' dtype), times
     ``weight`` [n] (float32), in one pass over the logits.  ``ids`` int32 and ``teacher`` [n, k]
     are the teacher's kept classes and their logits, as top_k gives them; ids outside the classes
-    are empty slots.  ``grad`` may be ``logits`` itself."""
-    import torch
-    z = logits.detach() if isinstance(logits, torch.Tensor) else logits
-    _rows(z, "logits")
+    are empty slots.  ``grad`` may be ``logits`` itself.  Autograd does not see the call."""
+    if _torch is None:
+        _setup()
+    n, c, args = _check_distill(logits, ids, teacher, weight)
     if loss is None:
-        loss = z.new_empty((z.shape[0],), dtype=torch.float32)
+        loss = teacher.new_empty((n,), dtype=_torch.float32)
     else:
-        _vector(loss, "loss", z.shape[0], torch.float32, z.device)
+        _vector(loss, "loss", n, _torch.float32, logits.get_device())
     if grad is None:
-        grad = torch.empty(z.shape, dtype=z.dtype, device=z.device)
-    _forward(z, ids, teacher, temperature, weight, loss, None, grad)
+        grad, ldg = ids.new_empty((n, c), dtype=logits.dtype), c
+    else:
+        ldg = _rows(grad, "grad", c, n, logits.dtype, logits.get_device())[2]
+    _call("bridger_distill", logits, *args, temperature, _ptr(weight), loss.data_ptr(), None,
+          grad.data_ptr(), ldg)
     return loss, grad
 
 
@@ -204,14 +212,16 @@ _distill_function = None
 
 
 def _make_distill_function():
-    import torch
+    torch = _torch
 
     class Distill(torch.autograd.Function):
         @staticmethod
         def forward(ctx, logits, ids, teacher, temperature):
-            loss = logits.new_empty((logits.shape[0],), dtype=torch.float32)
-            stats = logits.new_empty((logits.shape[0], 2), dtype=torch.float32)
-            _forward(logits, ids, teacher, temperature, None, loss, stats, None)
+            n, c, args = _check_distill(logits, ids, teacher, None)
+            loss = ids.new_empty((n,), dtype=torch.float32)
+            stats = ids.new_empty((n, 2), dtype=torch.float32)
+            _call("bridger_distill", logits, *args, temperature, None, loss.data_ptr(),
+                  stats.data_ptr(), None, 0)
             ctx.save_for_backward(logits, ids, teacher, stats)
             ctx.temperature = temperature
             return loss
@@ -221,12 +231,10 @@ def _make_distill_function():
         def backward(ctx, grad_loss):
             logits, ids, teacher, stats = ctx.saved_tensors
             weight = grad_loss.contiguous()
-            grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-            ld, code, teacher_code = _check_distill(logits, ids, teacher, weight)
-            _call(bridger_distill_backward, logits.device, logits.data_ptr(), ld, code,
-                  ids.data_ptr(), teacher.data_ptr(), teacher_code, logits.shape[0],
-                  logits.shape[1], ids.shape[1], ctx.temperature, stats.data_ptr(),
-                  weight.data_ptr(), grad.data_ptr(), logits.shape[1])
+            n, c, args = _check_distill(logits, ids, teacher, weight)
+            grad = ids.new_empty((n, c), dtype=logits.dtype)
+            _call("bridger_distill_backward", logits, *args, ctx.temperature, stats.data_ptr(),
+                  weight.data_ptr(), grad.data_ptr(), c)
             return grad, None, None, None
 
     return Distill
@@ -234,8 +242,11 @@ def _make_distill_function():
 
 def distill_loss(logits, ids, teacher, temperature: float = 1.0):
     """distill's loss of every row [n], differentiable in ``logits`` (once; the teacher is taken
-    as constant)."""
+    as constant).  In a training step that is captured into a graph, take distill: it gives the
+    gradient without autograd, whose nodes stay with the streams they were made on."""
     global _distill_function
+    if _torch is None:
+        _setup()
     if _distill_function is None:
         _distill_function = _make_distill_function()
     return _distill_function.apply(logits, ids, teacher, float(temperature))
@@ -246,45 +257,52 @@ def rmsnorm_q8(x, weight=None, residual=None, eps: float = 1e-6, q=None, scale=N
     (q int8 [n, f], scale float32 [n], total), q * scale[:, None] being the norm and total
     x + residual in x's dtype (None without a residual or a ``total`` to write).  ``total`` may be
     x or residual itself."""
-    import torch
-    ldx = _rows(x, "x")
-    n, f = x.shape
-    dev = x.device
-    code = _code(x.dtype)
-    ldr = 0 if residual is None else _rows(residual, "residual", f, n, x.dtype, dev)
+    if _torch is None:
+        _setup()
+    n, f, ldx = _rows(x, "x", None, None, None, None)
+    dev, dtype = x.get_device(), x.dtype
+    code = _code(dtype)
+    ldr = 0 if residual is None else _rows(residual, "residual", f, n, dtype, dev)[2]
     if weight is not None:
-        _vector(weight, "weight", f, x.dtype, dev)
+        _vector(weight, "weight", f, dtype, dev)
     if q is None:
-        q = torch.empty((n, f), dtype=torch.int8, device=dev)
-    if scale is None:
-        scale = torch.empty((n,), dtype=torch.float32, device=dev)
+        q, ldq = x.new_empty((n, f), dtype=_torch.int8), f
     else:
-        _vector(scale, "scale", n, torch.float32, dev)
-    if total is None and residual is not None:
-        total = torch.empty((n, f), dtype=x.dtype, device=dev)
-    ldt = 0 if total is None else _rows(total, "total", f, n, x.dtype, dev)
-    ldq = _rows(q, "q", f, n, torch.int8, dev)
-    _call(bridger_rmsnorm_q8, dev, x.data_ptr(), ldx, _ptr(residual), ldr, _ptr(weight), code, n, f,
-          float(eps), _ptr(total), ldt, q.data_ptr(), ldq, scale.data_ptr())
+        ldq = _rows(q, "q", f, n, _torch.int8, dev)[2]
+    if scale is None:
+        scale = x.new_empty((n,), dtype=_torch.float32)
+    else:
+        _vector(scale, "scale", n, _torch.float32, dev)
+    ldt = f
+    if total is not None:
+        ldt = _rows(total, "total", f, n, dtype, dev)[2]
+    elif residual is not None:
+        total = x.new_empty((n, f))
+    _call("bridger_rmsnorm_q8", x, x.data_ptr(), ldx, _ptr(residual), ldr, _ptr(weight), code, n, f,
+          eps, _ptr(total), ldt, q.data_ptr(), ldq, scale.data_ptr())
     return q, scale, total
 
 
 def matmul_q8(a, a_scale, b, b_scale, bias=None, dtype=None, out=None):
     """a [n, f] times b [m, f] transposed, both int8 with float32 scales for each row of a [n] and
     of b [m], plus ``bias`` [m] (float32): [n, m] of ``dtype`` (bfloat16 unless given, or out's)."""
-    import torch
-    lda = _rows(a, "a", dtype=torch.int8)
-    n, f = a.shape
-    dev = a.device
-    ldb = _rows(b, "b", f, None, torch.int8, dev)
-    m = b.shape[0]
-    _vector(a_scale, "a_scale", n, torch.float32, dev)
-    _vector(b_scale, "b_scale", m, torch.float32, dev)
+    if _torch is None:
+        _setup()
+    f32 = _torch.float32
+    n, f, lda = _rows(a, "a", None, None, _torch.int8, None)
+    dev = a.get_device()
+    m, _, ldb = _rows(b, "b", f, None, _torch.int8, dev)
+    _vector(a_scale, "a_scale", n, f32, dev)
+    _vector(b_scale, "b_scale", m, f32, dev)
     if bias is not None:
-        _vector(bias, "bias", m, torch.float32, dev)
+        _vector(bias, "bias", m, f32, dev)
     if out is None:
-        out = torch.empty((n, m), dtype=dtype or torch.bfloat16, device=dev)
-    ldo = _rows(out, "out", m, n, dtype, dev)
-    _call(bridger_matmul_q8, dev, a.data_ptr(), lda, a_scale.data_ptr(), b.data_ptr(), ldb,
-          b_scale.data_ptr(), _ptr(bias), n, m, f, _code(out.dtype), out.data_ptr(), ldo)
+        dtype = dtype or _torch.bfloat16
+        code = _code(dtype)
+        out, ldo = a.new_empty((n, m), dtype=dtype), m
+    else:
+        ldo = _rows(out, "out", m, n, dtype, dev)[2]
+        code = _code(out.dtype)
+    _call("bridger_matmul_q8", a, a.data_ptr(), lda, a_scale.data_ptr(), b.data_ptr(), ldb,
+          b_scale.data_ptr(), _ptr(bias), n, m, f, code, out.data_ptr(), ldo)
     return out
