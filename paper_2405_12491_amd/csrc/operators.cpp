@@ -211,7 +211,7 @@ bridger_status bridger_rmsnorm_q8(const void *x, int64_t ldx, const void *residu
     return invalid(f);
   if (bridger_status s = device_ready()) return s;
   return launched(launch_rmsnorm_q8({x, ldx, residual, ldr, weight, n_rows, n_features, eps, total,
-                                     ldt, q, ldq, scale, 0},
+                                     ldt, q, ldq, scale, 1.0 / n_features, 0},
                                     dtype, stream));
 }
 

@@ -55,6 +55,7 @@ struct RmsnormArgs {
   int8_t *q;
   int64_t ldq;
   float *scale;
+  double per_feature;  // 1 / n_features
   int64_t first;  // the launch's first row
 };
 

@@ -152,11 +152,19 @@ __global__ __launch_bounds__(kRowThreads<G>) void rmsnorm_q8_kernel(RmsnormArgs 
     walk_row<T, G, 1>(a, row, lane, lds_sum2, lds_max2, lds_again);
     return;
   }
-  const double top = (double)__uint_as_float(most) * inverse_rms(squares, n, a.eps);
+  // in float where the mean square lies in its middle: half the instructions of a short row were
+  // those of the double root and quotient (1M x 28 float: 48 -> 38 us)
+  const double mean = squares * a.per_feature + (double)a.eps;
+  double top;
+  if (mean > 0x1p-100 && mean < 0x1p100) {
+    top = (double)(__uint_as_float(most) / __builtin_sqrtf((float)mean));
+  } else {
+    top = (double)__uint_as_float(most) * inverse_rms(squares, n, a.eps);
+  }
   const bool fine = top <= (double)__FLT_MAX__;
   const float steps = fine && most ? 127.0f / __uint_as_float(most) : 0.0f;
   int8_t *q = a.q + row * a.ldq;
-  if (lane == 0) a.scale[row] = fine ? (float)(top / 127.0) : __builtin_nanf("");
+  if (lane == 0) a.scale[row] = fine ? (float)top * (1.0f / 127.0f) : __builtin_nanf("");
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int j = (c * G + lane) * V;
