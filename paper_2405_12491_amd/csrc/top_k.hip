@@ -88,28 +88,21 @@ __global__ __launch_bounds__(256) void top_k_lane_kernel(TopKArgs a) {
 // counting the larger ones.  Rows where too many or too few reach it (many equal scores, masked or
 // broken rows) take the general way below.
 template <int G>
-constexpr int kCandidates = G == 64 ? 256 : 1024;  // of one wave: little LDS, so that many fit a CU
+constexpr int kCandidates = G == 64 ? 512 : 1024;  // of one wave: less LDS, so that many fit a CU
 
-// Where the row's scores are (in registers, C > 1: a row of at least 16 bytes).  each(f): f(first class, 16 bytes of scores), in ascending order of
-// the classes per lane; NaN past the row's end.  All lanes make the same number of calls.
+// Where the row's scores are.  each(f): f(first class, 16 bytes of scores), the classes kStep apart,
+// in ascending order per lane; NaN past the row's end.  All lanes make the same number of calls.
+// In registers, lane after lane with whole loads: rows of at least 16 bytes.
 template <typename T, int G, int C>
 struct InRegisters {
+  static constexpr int kStep = 1;
   RowLoad<T> x[C];
   __device__ InRegisters(const T *row, int n) {
     const uint32_t nan = fill_of((T)__builtin_nanf(""));
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int j = (c * G + (int)threadIdx.x) * kPerLoad<T>;
-      if (C == 1 && n < kPerLoad<T>) {
-        x[c].tiny(row, j, n, (T)__builtin_nanf(""));
-      } else {
-        x[c].issue(row, j, n);
-      }
-    }
+    for (int c = 0; c < C; ++c) x[c].issue(row, (c * G + (int)threadIdx.x) * kPerLoad<T>, n);
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-      if (C > 1 || n >= kPerLoad<T>)
-        x[c].take((c * G + (int)threadIdx.x) * kPerLoad<T>, n, nan);
+    for (int c = 0; c < C; ++c) x[c].take((c * G + (int)threadIdx.x) * kPerLoad<T>, n, nan);
   }
   template <typename F>
   __device__ void each(F f) {
@@ -121,8 +114,30 @@ struct InRegisters {
     ((forget(x[c].raw), f((c * G + (int)threadIdx.x) * kPerLoad<T>, x[c].raw)), ...);
   }
 };
+// In registers, class after class on neighbouring lanes: short rows, whose whole loads would leave
+// most lanes without a score, and their maxima without a bound.
+template <typename T, int G>
+struct InLanes {
+  static constexpr int kStep = G;
+  u32x4 raw;
+  __device__ InLanes(const T *row, int n) {
+    T e[kPerLoad<T>];
+#pragma unroll
+    for (int i = 0; i < kPerLoad<T>; ++i) {
+      const int j = i * G + (int)threadIdx.x;
+      e[i] = j < n ? row[j] : (T)__builtin_nanf("");
+    }
+    __builtin_memcpy(&raw, e, 16);
+  }
+  template <typename F>
+  __device__ void each(F f) {
+    f((int)threadIdx.x, raw);
+  }
+};
+// In memory: every walk reads the row again.
 template <typename T, int G>
 struct InMemory {
+  static constexpr int kStep = 1;
   const T *row;
   int n;
   __device__ InMemory(const T *row, int n) : row(row), n(n) {}
@@ -145,7 +160,7 @@ struct InMemory {
 
 template <int G>
 struct TopKShared {
-  uint64_t key[kCandidates<G> + 2];
+  uint64_t key[kCandidates<G> + 8];
   float value[kCandidates<G>];
   float bound[G / 64];
   int wave[2][G / 64];
@@ -184,7 +199,7 @@ __device__ inline int collect(Source &x, TopKShared<G> &s, Reach reach) {
         if (reach(v)) {
           const int at = atomicAdd(&s.count, 1);
           if (at < kCandidates<G>) {
-            s.key[at] = key_of(v, j + i);
+            s.key[at] = key_of(v, j + i * Source::kStep);
             s.value[at] = v;
           }
         }
@@ -199,14 +214,17 @@ __device__ inline int collect(Source &x, TopKShared<G> &s, Reach reach) {
 template <typename T, int G>
 __device__ inline void store_ranked(const TopKArgs &a, int64_t row, TopKShared<G> &s, int count,
                                     int k) {
-  if (threadIdx.x < 2) s.key[count + threadIdx.x] = 0;
+  if (threadIdx.x < 8) s.key[count + threadIdx.x] = 0;
   __syncthreads();
   for (int t = threadIdx.x; t < count; t += G) {
     const uint64_t mine = s.key[t];
     int rank = 0;
-    for (int q = 0; q < count; q += 2) {
-      const ulonglong2 other = *(const ulonglong2 *)&s.key[q];
-      rank += (other.x > mine) + (other.y > mine);
+    for (int q = 0; q < count; q += 8) {  // four loads on their way at once
+      ulonglong2 other[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) other[i] = *(const ulonglong2 *)&s.key[q + 2 * i];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) rank += (other[i].x > mine) + (other[i].y > mine);
     }
     if (rank < k) store_slot<T>(a, row, rank, from_float<T>(s.value[t]), class_of(mine));
   }
@@ -330,7 +348,15 @@ __global__ __launch_bounds__(G, C <= 8 ? 8 : 4) void top_k_kernel(TopKArgs a) {
   top_k_row<T, G>(a, row, x, s);
 }
 
-// Rows that do not fit a workgroup's registers: every walk reads them again.
+template <typename T, int G>
+__global__ __launch_bounds__(G, 8) void top_k_short_kernel(TopKArgs a) {
+  __shared__ __attribute__((aligned(16))) TopKShared<G> s;
+  const int64_t row = a.first + blockIdx.x;
+  InLanes<T, G> x((const T *)a.scores + row * a.ld, a.n_classes);
+  top_k_row<T, G>(a, row, x, s);
+}
+
+// Rows that do not fit a workgroup's registers.
 template <typename T>
 __global__ __launch_bounds__(1024) void top_k_long_kernel(TopKArgs a) {
   __shared__ __attribute__((aligned(16))) TopKShared<1024> s;
@@ -343,24 +369,36 @@ int launch_top_k(const TopKArgs &a, int32_t dtype, void *stream) {
   return with_type(dtype, [&](auto t) {
     using T = decltype(t);
     const int64_t bytes = (int64_t)a.n_classes * (int)sizeof(T);
-    // a lane's work is classes x k: beyond a few hundred steps it takes many rows to pay
-    if (a.k <= 16 && a.n_classes <= 64 &&
-        ((int64_t)a.n_classes * a.k <= 256 || a.n_rows >= 8192)) {
-      if (a.k == 1) return launch_rows(top_k_lane_kernel<T, 1>, 1, a, stream);
-      if (a.k == 2) return launch_rows(top_k_lane_kernel<T, 2>, 1, a, stream);
-      if (a.k <= 4) return launch_rows(top_k_lane_kernel<T, 4>, 1, a, stream);
-      if (a.k <= 8) return launch_rows(top_k_lane_kernel<T, 8>, 1, a, stream);
-      return launch_rows(top_k_lane_kernel<T, 16>, 1, a, stream);
+    // a lane's work is classes x k: beyond a few steps it takes many rows to pay (64 classes, k = 16,
+    // us, a lane / a wave a row: 8192 rows 16 / 8, 100,000 27 / 56)
+    if (a.k <= 32 && a.n_classes <= 64 &&
+        ((int64_t)a.n_classes * a.k <= 64 || a.n_rows >= 32768)) {
+      auto lane = [&](auto k) { return launch_rows(k, 1, a, stream); };
+      return a.k == 1   ? lane(top_k_lane_kernel<T, 1>)
+             : a.k == 2 ? lane(top_k_lane_kernel<T, 2>)
+             : a.k <= 4 ? lane(top_k_lane_kernel<T, 4>)
+             : a.k <= 8 ? lane(top_k_lane_kernel<T, 8>)
+             : a.k <= 16 ? lane(top_k_lane_kernel<T, 16>)
+                         : lane(top_k_lane_kernel<T, 32>);
     }
     auto of = [&](auto k, int threads) { return launch_each_row(k, threads, a, stream); };
-    // one wave, whose lanes' maxima bound up to 64 scores; rows below 16 bytes are among these
     const int k = a.k < a.n_classes ? a.k : a.n_classes;
-    if (bytes <= 1024 && k <= 64) return of(top_k_kernel<T, 64, 1>, 64);
-    if (bytes <= 4096 && k <= 64) return of(top_k_kernel<T, 64, 4>, 64);
+    // Few waves a row, each of which pays for its bound and its meetings, but so many that about half
+    // of their lanes hold one of the k (bfloat16, us, one / two / four waves: 100,000 x 1000, k = 10 82
+    // / 133 / 216, k = 64 647 / 209 / 289; 10,000 x 8000, k = 20 37 / 36 / 40, k = 64 309 / 55 / 55).
+    const bool small = a.n_classes <= 128;
+    if (bytes <= 1024 && (k <= 32 || (small && k <= 64))) return of(top_k_short_kernel<T, 64>, 64);
+    if (bytes <= 2048 && k > 32 && k <= 64) return of(top_k_short_kernel<T, 128>, 128);
+    if (bytes <= 4096 && k > 64) return of(top_k_short_kernel<T, 256>, 256);
+    if (bytes <= 2048 && k <= 32) return of(top_k_kernel<T, 64, 2>, 64);
+    if (bytes <= 4096 && k <= 32) return of(top_k_kernel<T, 64, 4>, 64);
+    if (bytes <= 8192 && k <= 32) return of(top_k_kernel<T, 64, 8>, 64);
+    if (bytes <= 8192 && k <= 64) return of(top_k_kernel<T, 128, 4>, 128);
+    if (bytes <= 16384 && k <= 32) return of(top_k_kernel<T, 128, 8>, 128);
     if (bytes <= 16384) return of(top_k_kernel<T, 256, 4>, 256);
     if (bytes <= 32768) return of(top_k_kernel<T, 256, 8>, 256);
-    if (bytes <= 65536) return of(top_k_kernel<T, 1024, 4>, 1024);
-    if (bytes <= 131072) return of(top_k_kernel<T, 1024, 8>, 1024);
+    if (bytes <= 65536) return of(top_k_kernel<T, 512, 8>, 512);
+    if (bytes <= 131072) return of(top_k_kernel<T, 512, 16>, 512);
     if (bytes <= 262144) return of(top_k_kernel<T, 1024, 16>, 1024);
     return of(top_k_long_kernel<T>, 1024);
   });
