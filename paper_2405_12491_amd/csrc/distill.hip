@@ -297,7 +297,7 @@ __global__ __launch_bounds__(1024) void distill_long_kernel(DistillArgs a) {
     s.any = lds_any != 0;
     r = {a.stats[2 * row], a.stats[2 * row + 1], s.any};
   } else {
-    float most = whole + lane < n ? to_float(z[whole + lane]) : -inf;
+    float most = lane < n - whole ? to_float(z[whole + lane]) : -inf;
     float mass = most == -inf ? 0.0f : 1.0f;
     if (most != most || most == inf) mass = __builtin_nanf("");
     for (int64_t j = (int64_t)lane * V; j < whole; j += (int64_t)G * V * U) {
@@ -345,7 +345,7 @@ __global__ __launch_bounds__(1024) void distill_long_kernel(DistillArgs a) {
     for (int i = 0; i < V; ++i) v[i] = grad_of(element<T>(raw, i));
     store16<T>(grad + j, V, v);
   }
-  if (whole + lane < n) grad[whole + lane] = from_float<T>(grad_of(to_float(z[whole + lane])));
+  if (lane < n - whole) grad[whole + lane] = from_float<T>(grad_of(to_float(z[whole + lane])));
   __syncthreads();
   if (lane < 64) store_kept<T>(grad, s, r, factor, weight, per);
 }

@@ -3,6 +3,7 @@
 // The matrix instructions take the weights as their first operand, so that a lane ends with four
 // neighbouring outputs of one row.  Both operands share the order of the features within an
 // instruction, so any fixed order of them gives the same sum.
+#include <mutex>
 #include <type_traits>
 
 #include "rows.h"
@@ -519,6 +520,34 @@ __global__ __launch_bounds__(128 * WO) void matmul_q8_tile_kernel(MatmulArgs a) 
   }
 }
 
+// A workgroup a tile, at most 2^22 of them.  More than 64 KB of LDS are allowed once per kernel (each
+// has one size) and device.
+static int launch_tiles(void (*k)(MatmulArgs), int64_t tiles, int threads, int lds_bytes,
+                        const MatmulArgs &args, void *stream) {
+  if (lds_bytes > 65536) {
+    constexpr int kMost = 256;
+    static std::mutex mu;
+    static struct {
+      void (*kernel)(MatmulArgs);
+      int device;
+    } allowed[kMost];
+    static int count = 0;
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess) return (int)e;
+    std::lock_guard<std::mutex> lock(mu);
+    int at = 0;
+    while (at < count && !(allowed[at].kernel == k && allowed[at].device == device)) ++at;
+    if (at == count) {
+      e = hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize,
+                              lds_bytes);
+      if (e != hipSuccess) return (int)e;
+      if (count < kMost) allowed[count++] = {k, device};
+    }
+  }
+  return launch(k, tiles, threads, lds_bytes, args, stream);
+}
+
 // Whether rows can go to LDS directly: 16-byte chunks, and a tile's offsets below 2^31.
 static bool aligned_rows(const MatmulArgs &a) {
   return a.lda <= (1 << 22) && a.ldb <= (1 << 22) &&
@@ -601,7 +630,7 @@ struct Estimate {
   }
 };
 
-int launch_matmul_q8(const MatmulArgs &a, int32_t dtype, void *stream) {
+static int launch_part(const MatmulArgs &a, int32_t dtype, void *stream) {
   Estimate e(a);
   e.stream(0, 1, 1, 8);
   e.stream(1, 1, 2, 8);
@@ -624,6 +653,29 @@ int launch_matmul_q8(const MatmulArgs &a, int32_t dtype, void *stream) {
       default: return launch_tile<T, 128, 4, true>(a, stream);
     }
   });
+}
+
+// A dispatch counts its work-items in 32 bits: no more than 2^22 tiles of 16 x 16 a launch.
+int launch_matmul_q8(const MatmulArgs &a, int32_t dtype, void *stream) {
+  constexpr int64_t kOutputs = int64_t(1) << 20, kSums = int64_t(1) << 30;
+  const int64_t outputs = a.n_outputs < kOutputs ? a.n_outputs : kOutputs;
+  const int64_t rows = kSums / ((outputs + 255) / 256 * 256) / 256 * 256;
+  const int size = dtype == BRIDGER_F32 ? 4 : 2;
+  for (int64_t o = 0; o < a.n_outputs; o += outputs)
+    for (int64_t r = 0; r < a.n_rows; r += rows) {
+      MatmulArgs part = a;
+      part.a += r * a.lda;
+      part.a_scale += r;
+      part.b += o * a.ldb;
+      part.b_scale += o;
+      if (a.bias) part.bias += o;
+      part.out = (uint8_t *)a.out + (r * a.ldo + o) * size;
+      part.n_rows = a.n_rows - r < rows ? a.n_rows - r : rows;
+      part.n_outputs = (int32_t)(a.n_outputs - o < outputs ? a.n_outputs - o : outputs);
+      const int err = launch_part(part, dtype, stream);
+      if (err) return err;
+    }
+  return 0;
 }
 
 }  // namespace bridger

@@ -82,7 +82,15 @@ bridger_status device_ready() {
   return BRIDGER_OK;
 }
 
-bridger_status launched(int err) {
+// Runs a launcher; nothing throws across the interface.
+template <typename F>
+bridger_status launched(F f) {
+  int err;
+  try {
+    err = f();
+  } catch (...) {
+    return report_error(BRIDGER_ERR_OUT_OF_MEMORY, "host allocation failed");
+  }
   if (err == 0) return BRIDGER_OK;
   (void)hipGetLastError();
   return report_error(BRIDGER_ERR_DEVICE, hipGetErrorString((hipError_t)err));
@@ -134,7 +142,9 @@ bridger_status bridger_top_k(const void *scores, int64_t ld, int32_t dtype, int6
   const Rows out[] = {{values, n_rows, k, k, size}, {ids, n_rows, k, k, 4}};
   if (const char *f = arrays_fault(in, 1, out, 2, nullptr)) return invalid(f);
   if (bridger_status s = device_ready()) return s;
-  return launched(launch_top_k({scores, ld, n_rows, n_classes, k, values, ids, 0}, dtype, stream));
+  return launched([&] {
+    return launch_top_k({scores, ld, n_rows, n_classes, k, values, ids, 0}, dtype, stream);
+  });
 }
 
 bridger_status bridger_distill(const void *logits, int64_t ldl, int32_t dtype, const int32_t *ids,
@@ -160,7 +170,9 @@ bridger_status bridger_distill(const void *logits, int64_t ldl, int32_t dtype, c
           arrays_fault(in, 4, out, 3, [](int i, int o) { return i == 0 && o == 2; }))
     return invalid(f);
   if (bridger_status s = device_ready()) return s;
-  return launched(launch_distill(a, dtype, false, stream));
+  return launched([&] {
+    return launch_distill(a, dtype, false, stream);
+  });
 }
 
 bridger_status bridger_distill_backward(const void *logits, int64_t ldl, int32_t dtype,
@@ -186,7 +198,9 @@ bridger_status bridger_distill_backward(const void *logits, int64_t ldl, int32_t
   if (const char *f = arrays_fault(in, 5, out, 1, [](int i, int) { return i == 0; }))
     return invalid(f);
   if (bridger_status s = device_ready()) return s;
-  return launched(launch_distill(a, dtype, true, stream));
+  return launched([&] {
+    return launch_distill(a, dtype, true, stream);
+  });
 }
 
 bridger_status bridger_rmsnorm_q8(const void *x, int64_t ldx, const void *residual, int64_t ldr,
@@ -210,9 +224,11 @@ bridger_status bridger_rmsnorm_q8(const void *x, int64_t ldx, const void *residu
           arrays_fault(in, 3, out, 3, [](int i, int o) { return i < 2 && o == 0; }))
     return invalid(f);
   if (bridger_status s = device_ready()) return s;
-  return launched(launch_rmsnorm_q8({x, ldx, residual, ldr, weight, n_rows, n_features, eps, total,
+  return launched([&] {
+    return launch_rmsnorm_q8({x, ldx, residual, ldr, weight, n_rows, n_features, eps, total,
                                      ldt, q, ldq, scale, 1.0 / n_features, 0},
-                                    dtype, stream));
+                                    dtype, stream);
+  });
 }
 
 bridger_status bridger_matmul_q8(const int8_t *a, int64_t lda, const float *a_scale,
@@ -238,9 +254,11 @@ bridger_status bridger_matmul_q8(const int8_t *a, int64_t lda, const float *a_sc
   const Rows o[] = {{out, n_rows, n_outputs, ldo, size}};
   if (const char *f = arrays_fault(in, 5, o, 1, nullptr)) return invalid(f);
   if (bridger_status s = device_ready()) return s;
-  return launched(launch_matmul_q8({a, lda, a_scale, b, ldb, b_scale, bias, n_rows, n_outputs,
+  return launched([&] {
+    return launch_matmul_q8({a, lda, a_scale, b, ldb, b_scale, bias, n_rows, n_outputs,
                                     n_features, out, ldo},
-                                   dtype, stream));
+                                   dtype, stream);
+  });
 }
 
 }  // extern "C"

@@ -63,7 +63,7 @@ struct RowLoad {
     __builtin_memcpy(&raw, row + (j < n - kPerLoad<T> ? j : n - kPerLoad<T>), 16);
   }
   __device__ void take(int j, int n, uint32_t fill) {
-    const int d = j + kPerLoad<T> - n;  // elements to move down, all of them from kPerLoad on
+    const int d = j - n + kPerLoad<T>;  // elements to move down, all of them from kPerLoad on
     if (d > 0) {
       const int words = sizeof(T) == 4 ? d : d >> 1;
       if (words >= 4) raw = u32x4{fill, fill, fill, fill};
@@ -279,19 +279,6 @@ int launch_rows(void (*k)(Args), int lanes, const Args &args, void *stream) {
 template <typename Args>
 int launch_each_row(void (*k)(Args), int threads, const Args &args, void *stream) {
   return launch_over(k, threads, 1, args, stream);
-}
-
-// A workgroup a tile.
-constexpr int64_t kMaxTiles = int64_t(1) << 23;
-template <typename Args>
-int launch_tiles(void (*k)(Args), int64_t tiles, int threads, int lds_bytes, const Args &args,
-                 void *stream) {
-  if (lds_bytes > 65536) {
-    const hipError_t e = hipFuncSetAttribute(
-        (const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes);
-    if (e != hipSuccess) return (int)e;
-  }
-  return launch(k, tiles, threads, lds_bytes, args, stream);
 }
 
 }  // namespace bridger

@@ -159,7 +159,7 @@ def top_k(scores, k: int, values=None, ids=None):
     if _torch is None:
         _setup()
     n, c, ld = _rows(scores, "scores", None, None, None, None)
-    dev = scores.get_device()
+    k, dev = int(k), scores.get_device()
     if values is None:
         values = scores.new_empty((n, k))
     else:
@@ -203,7 +203,7 @@ def distill(logits, ids, teacher, temperature: float = 1.0, weight=None, grad=No
         grad, ldg = ids.new_empty((n, c), dtype=logits.dtype), c
     else:
         ldg = _rows(grad, "grad", c, n, logits.dtype, logits.get_device())[2]
-    _call("bridger_distill", logits, *args, temperature, _ptr(weight), loss.data_ptr(), None,
+    _call("bridger_distill", logits, *args, float(temperature), _ptr(weight), loss.data_ptr(), None,
           grad.data_ptr(), ldg)
     return loss, grad
 
@@ -279,7 +279,7 @@ def rmsnorm_q8(x, weight=None, residual=None, eps: float = 1e-6, q=None, scale=N
     elif residual is not None:
         total = x.new_empty((n, f))
     _call("bridger_rmsnorm_q8", x, x.data_ptr(), ldx, _ptr(residual), ldr, _ptr(weight), code, n, f,
-          eps, _ptr(total), ldt, q.data_ptr(), ldq, scale.data_ptr())
+          float(eps), _ptr(total), ldt, q.data_ptr(), ldq, scale.data_ptr())
     return q, scale, total
 
 

@@ -708,3 +708,50 @@ def test_numbers_of_slots():
         ids = torch.randint(-1, c, (5, k), generator=_gen(k), device="cuda", dtype=torch.int32)
         _check_distill(z, ids, _normal(k, 5, k), 1.5, None, f"c={c} k={k}")
     assert math.isfinite(float(B.distill(z, torch.zeros_like(ids), _normal(1, 5, 129))[0].sum()))
+
+
+def test_more_rows_than_a_launch_takes():
+    """Rows, and tiles, beyond what one dispatch counts go out as several launches."""
+    n = (1 << 20) + 1234
+    s = _normal(1, n, 70, dtype=torch.bfloat16)
+    values, ids = B.top_k(s, 3)                                    # a workgroup a row
+    for part in (slice(0, 300), slice((1 << 20) - 150, (1 << 20) + 150), slice(n - 300, n)):
+        _check_top(s[part], 3, values[part], ids[part])
+    rows, outputs = (1 << 20) + 70, 1100                           # 2^22.5 tiles of 16 x 16
+    a, b = _int8(2, rows, 33), _int8(3, outputs, 33)
+    sa, sb = torch.rand(rows, device="cuda", generator=_gen(4)), torch.rand(outputs, device="cuda", generator=_gen(5))
+    v = _normal(6, outputs)
+    out = B.matmul_q8(a, sa, b, sb, v, torch.float32)
+    cut = (1 << 30) // 1280 // 256 * 256                           # where the second launch starts
+    for part in (slice(0, 100), slice(cut - 100, cut + 100), slice(rows - 100, rows)):
+        R.check_matmul(a[part], sa[part], b, sb, v, out[part])
+    del a, out
+    outputs = (1 << 20) + 33
+    a, b = _int8(7, 20, 40), _int8(8, outputs, 40)
+    sa, sb = torch.rand(20, device="cuda", generator=_gen(9)), torch.rand(outputs, device="cuda", generator=_gen(10))
+    v = _normal(11, outputs)
+    R.check_matmul(a, sa, b, sb, v, B.matmul_q8(a, sa, b, sb, v, torch.float32))
+
+
+@pytest.mark.parametrize("n,m,f", [(600, 600, 256), (64, 512, 4096), (4096, 4100, 200)])
+def test_products_in_a_graph(n, m, f):
+    """Kernels of more than 64 KB of LDS, captured and replayed."""
+    a, b = _int8(1, n, f), _int8(2, m, f)
+    sa, sb = torch.rand(n, device="cuda", generator=_gen(3)), torch.rand(m, device="cuda", generator=_gen(4)) * 1e-3
+    out = torch.empty(n, m, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        B.matmul_q8(a, sa, b, sb, out=out)
+    s.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        B.matmul_q8(a, sa, b, sb, out=out)
+    for rep in range(3):
+        a.copy_(_int8(10 + rep, n, f))
+        sa.mul_(0.5)
+        torch.cuda.synchronize()
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        R.check_matmul(a, sa, b, sb, None, out, f"replay {rep}")
