@@ -38,10 +38,15 @@ __device__ inline Slots load_slots(const DistillArgs &a, int64_t row, const T *z
   int any = 0;
 #pragma unroll
   for (int i = 0; i < kSlots; ++i) {
-    const int at = i * L + lane;
     s.id[i] = -1;
-    s.z[i] = 0.0f;
+    s.z[i] = s.p[i] = 0.0f;
     t[i] = -inf;
+  }
+  // in this and the loops below: no work for the slots that no lane has
+#pragma unroll
+  for (int i = 0; i < kSlots; ++i) {
+    if (i * L >= a.k) break;
+    const int at = i * L + lane;
     if (at < a.k) {
       const int32_t id = a.ids[row * a.k + at];
       const float v = teacher_at(a, row * a.k + at);
@@ -60,6 +65,7 @@ __device__ inline Slots load_slots(const DistillArgs &a, int64_t row, const T *z
   float mass = 0.0f;
 #pragma unroll
   for (int i = 0; i < kSlots; ++i) {
+    if (i * L >= a.k) break;
     t[i] = (t[i] - most) / a.temperature;
     s.p[i] = s.id[i] >= 0 ? __expf(t[i]) : 0.0f;
     mass += s.p[i];
@@ -69,35 +75,58 @@ __device__ inline Slots load_slots(const DistillArgs &a, int64_t row, const T *z
   s.kl = 0.0f;
 #pragma unroll
   for (int i = 0; i < kSlots; ++i) {
+    if (i * L >= a.k) break;
     s.p[i] /= mass;
     if (s.id[i] >= 0 && s.p[i] != 0.0f) s.kl += s.p[i] * (t[i] - log_mass);
   }
   return s;
 }
 
+// How many pairs (slot of this wave's rows in groups below N, filled entry of the row's `ids`) hold
+// one class.  A slot meets itself: no class is there twice where this is the number of filled slots.
+template <int N>
+__device__ inline int count_equal(const Slots &s, const int32_t *ids, int k) {
+  int32_t id[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) id[i] = s.id[i] < 0 ? -2 : s.id[i];  // entries not filled are -1
+  int equal = 0;
+  for (int q = 0; q < k; q += 4) {
+    const int4 other = *(const int4 *)(ids + q);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      equal += __popcll(__ballot(other.x == id[i])) + __popcll(__ballot(other.y == id[i])) +
+               __popcll(__ballot(other.z == id[i])) + __popcll(__ballot(other.w == id[i]));
+  }
+  return equal;
+}
+
 // Of slots that hold one class, the first takes the sum of their p, in slot order, and the others
-// are emptied.  `ids` and `ps`: the row's kSlots L slots, written and read by this wave.
+// are emptied.  `ids` and `ps`: the row's kSlots L slots, written and read by this wave.  All pairs
+// are compared, and counted by the scalar unit; only rows that have such slots go on to find them.
 template <int G>
 __device__ inline void join_equal(const DistillArgs &a, Slots &s, int lane, int32_t *ids, float *ps) {
   constexpr int L = kSlotLanes<G>;
+  int filled = 0;
 #pragma unroll
   for (int i = 0; i < kSlots; ++i) {
+    if (i * L >= a.k) break;
     ids[i * L + lane] = s.id[i];
     ps[i * L + lane] = s.p[i];
+    filled += __popcll(__ballot(s.id[i] >= 0));
+  }
+  if constexpr (L < 4) {  // the last of four entries read at once
+    if (lane == 0)
+      for (int q = a.k; q < kSlots * L; ++q) ids[q] = -1;
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
-  int equal[kSlots] = {};
-  for (int q = 0; q < a.k; q += 4) {  // entries past k are -1, as are those not filled
-    const int4 other = *(const int4 *)(ids + q);
-#pragma unroll
-    for (int i = 0; i < kSlots; ++i)
-      equal[i] += (other.x == s.id[i]) + (other.y == s.id[i]) + (other.z == s.id[i]) +
-                  (other.w == s.id[i]);
-  }
+  const int equal = a.k <= L ? count_equal<1>(s, ids, a.k)
+                             : a.k <= 2 * L ? count_equal<2>(s, ids, a.k)
+                                            : count_equal<kSlots>(s, ids, a.k);
+  if (equal == filled) return;
 #pragma unroll
   for (int i = 0; i < kSlots; ++i)
-    if (s.id[i] >= 0 && equal[i] > 1) {
+    if (s.id[i] >= 0) {
       float p = 0.0f;
       bool first = true;
       for (int q = 0; q < a.k; ++q)
@@ -140,10 +169,6 @@ __device__ inline RowStats join_stats(float most, float mass, bool any, float fa
   return {safe, mass, any};
 }
 
-__device__ inline float factor_of(float temperature) {
-  return (float)(1.4426950408889634 / (double)temperature);
-}
-
 // The first wave's part after the row's sums: the loss, the stats.
 template <int G>
 __device__ inline void store_loss(const DistillArgs &a, int64_t row, const Slots &s,
@@ -152,11 +177,13 @@ __device__ inline void store_loss(const DistillArgs &a, int64_t row, const Slots
   const float log_mass = __logf(r.mass);
   float v = s.kl;
 #pragma unroll
-  for (int i = 0; i < kSlots; ++i)
+  for (int i = 0; i < kSlots; ++i) {
+    if (i * kSlotLanes<G> >= a.k) break;
     if (s.id[i] >= 0 && s.p[i] != 0.0f) {
       const float log_q = s.z[i] == -inf ? -inf : (s.z[i] - r.most) / a.temperature - log_mass;
       v -= s.p[i] * log_q;
     }
+  }
   v = lanes_reduce<Sum, kSlotLanes<G>>(v);
   if (lane == 0) {
     if (a.loss) a.loss[row] = s.any ? a.temperature * a.temperature * v : 0.0f;
@@ -192,7 +219,7 @@ __global__ __launch_bounds__(kRowThreads<G>, C <= 4 ? 8 : 4) void distill_kernel
   const int64_t row = row_of<G>(a.first);
   if (row >= a.n_rows) return;
   const T *z = (const T *)a.logits + row * a.ldl;
-  const float inf = __builtin_inff(), factor = factor_of(a.temperature);
+  const float inf = __builtin_inff(), factor = a.factor;
   RowLoad<T> x[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
@@ -281,7 +308,7 @@ __global__ __launch_bounds__(1024) void distill_long_kernel(DistillArgs a) {
   const int lane = threadIdx.x, n = a.n_classes;
   const int64_t row = row_of<G>(a.first);
   const T *z = (const T *)a.logits + row * a.ldl;
-  const float inf = __builtin_inff(), factor = factor_of(a.temperature);
+  const float inf = __builtin_inff(), factor = a.factor;
   const int whole = n / V * V;  // the row's whole loads; the elements past them are lanes' own
   Slots s;
   s.any = false;
@@ -374,7 +401,9 @@ static int launch_pass(const DistillArgs &a, void *stream) {
   return of(distill_long_kernel<T, BACKWARD>, 1024);
 }
 
-int launch_distill(const DistillArgs &a, int32_t dtype, bool backward, void *stream) {
+int launch_distill(const DistillArgs &args, int32_t dtype, bool backward, void *stream) {
+  DistillArgs a = args;
+  a.factor = (float)(1.4426950408889634 / (double)a.temperature);
   return with_type(dtype, [&](auto t) {
     using T = decltype(t);
     return backward ? launch_pass<T, true>(a, stream) : launch_pass<T, false>(a, stream);

@@ -3,7 +3,6 @@
 #pragma once
 #include <stdint.h>
 
-
 #include "bridger.h"
 
 namespace bridger {
@@ -39,6 +38,7 @@ struct DistillArgs {
   int64_t ldg;
   int32_t teacher_dtype;
   int64_t first;  // the launch's first row
+  float factor;   // log2(e) / temperature, rounded once
 };
 
 struct RmsnormArgs {
