@@ -242,7 +242,7 @@ __device__ inline int store_in_order(const TopKArgs &a, int64_t row, Source &x, 
     int before = 0, all = 0, mine = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const bool yes = j + i < a.n_classes && is(element<T>(raw, i));
+      const bool yes = i < a.n_classes - j && is(element<T>(raw, i));
       const uint64_t lanes = __ballot(yes);
       before += __popcll(lanes & ((uint64_t(1) << lane) - 1));
       all += __popcll(lanes);

@@ -16,6 +16,7 @@ import paper_2405_12491_amd as _B
 BRIDGER_F32, BRIDGER_BF16, BRIDGER_F16 = 0, 1, 2
 BRIDGER_MAX_TOP = 256
 BRIDGER_MATMUL_Q8_MAX_FEATURES = 131071
+_MOST = 0x7FFFFFFF
 
 _P, _I32, _I64, _F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 _ARGTYPES = {
@@ -110,6 +111,8 @@ def _rows(t, name, width, n, dtype, device):
         raise ValueError(f"{name} must be [{'n' if n is None else n}, "
                          f"{'width' if width is None else width}]")
     rows, w = shape
+    if w > _MOST or rows > _MOST:  # more than the entry points' 32 bits hold
+        raise ValueError(f"{name} has 2^31 or more rows or elements a row")
     step, inner = t.stride()
     if w > 1 and inner != 1:
         raise ValueError(f"{name}'s rows must be contiguous")
@@ -160,6 +163,8 @@ def top_k(scores, k: int, values=None, ids=None):
         _setup()
     n, c, ld = _rows(scores, "scores", None, None, None, None)
     k, dev = int(k), scores.get_device()
+    if not 1 <= k <= BRIDGER_MAX_TOP:
+        raise ValueError("k must be between 1 and BRIDGER_MAX_TOP")
     if values is None:
         values = scores.new_empty((n, k))
     else:
@@ -242,13 +247,19 @@ def _make_distill_function():
 
 def distill_loss(logits, ids, teacher, temperature: float = 1.0):
     """distill's loss of every row [n], differentiable in ``logits`` (once; the teacher is taken
-    as constant).  In a training step that is captured into a graph, take distill: it gives the
-    gradient without autograd, whose nodes stay with the streams they were made on."""
+    as constant).  Where logits need a gradient, a stream that is being captured is refused: autograd
+    keeps nodes on the streams they were made on, and a captured backward pass that meets one of an
+    eager graph ends the process.  There take distill and hand its gradient on
+    (``logits.backward(grad)``)."""
     global _distill_function
     if _torch is None:
         _setup()
     if _distill_function is None:
         _distill_function = _make_distill_function()
+    if getattr(logits, "requires_grad", False) and _torch.is_grad_enabled() and \
+            _torch.cuda.is_current_stream_capturing():
+        raise RuntimeError("distill_loss with a gradient on a stream that is being captured: "
+                           "take distill")
     return _distill_function.apply(logits, ids, teacher, float(temperature))
 
 

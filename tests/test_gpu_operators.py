@@ -593,6 +593,26 @@ def test_backward_in_a_graph_beside_an_eager_one():
     R.assert_near(z.grad, ref, tol, torch.float32)
 
 
+def test_loss_with_a_gradient_is_refused_in_a_graph():
+    x = _normal(1, 6, 8).requires_grad_()
+    ids, t = _teacher(2, 6, 8, 3)
+    eager = B.distill_loss(x, ids, t)
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        with pytest.raises(RuntimeError):
+            B.distill_loss(x, ids, t)
+        with torch.no_grad():
+            loss = B.distill_loss(x, ids, t)
+    for _ in range(3):
+        loss.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(loss, eager.detach())
+    eager.sum().backward()
+    assert bool(torch.isfinite(x.grad).all())
+
+
 def test_far_offsets():
     """Rows whose offsets pass 2^31 elements (and 2^32 bytes)."""
     far = (1 << 31) + 24
@@ -658,6 +678,22 @@ def test_refused_tensors():
                  lambda: B.top_k(torch.empty(4, 0, device="cuda"), 1),
                  lambda: B.rmsnorm_q8(x[:5], total=x.view(-1)[4:44].view(5, 8))):
         with pytest.raises((B.BridgerError, ValueError)):
+            call()
+
+
+def test_refused_counts_past_32_bits():
+    """A count that would lose its upper bits on the way: 2^32 + 3 classes are not 3 classes."""
+    wide = torch.empty(1, 2**32 + 3, dtype=torch.bfloat16, device="cuda")
+    ids, t = _teacher(1, 1, 3, 2)
+    one = torch.ones(1, device="cuda")
+    q = torch.zeros(1, 1, dtype=torch.int8, device="cuda")
+    many = wide.view(torch.int8).view(-1, 1)
+    for call in (lambda: B.top_k(wide, 2), lambda: B.distill(wide, ids, t),
+                 lambda: B.distill_loss(wide, ids, t), lambda: B.rmsnorm_q8(wide),
+                 lambda: B.matmul_q8(q, one, many, one), lambda: B.matmul_q8(many, one, q, one),
+                 lambda: B.matmul_q8(many.view(1, -1), one, many.view(1, -1), one),
+                 lambda: B.top_k(wide[:, :8], 2**32 + 2), lambda: B.top_k(wide[:, :8], -1)):
+        with pytest.raises(ValueError):
             call()
 
 
