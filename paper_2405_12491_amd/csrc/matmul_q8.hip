@@ -13,29 +13,31 @@ namespace bridger {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 
-// 16 features of a row from j on; zeros from n on.  SHORT: n may be below 16.
-template <bool SHORT>
-__device__ inline i32x4 load_features(const int8_t *row, int j, int n) {
+// 16 features of a row (n of them, 16 at least) from j on; those that end the row where less is
+// left.  move_down() brings the latter into place, zeros behind them.
+__device__ inline i32x4 load_raw(const int8_t *row, int j, int n) {
   i32x4 v;
-  if (!SHORT || n >= 16) {  // the 16 bytes that end the row, moved down
-    const int at = j < n - 16 ? j : n - 16;
-    __builtin_memcpy(&v, row + at, 16);
-    const int d = j - at;
-    if (d > 0) {
-      uint64_t lo = (uint32_t)v[0] | (uint64_t)(uint32_t)v[1] << 32;
-      uint64_t hi = (uint32_t)v[2] | (uint64_t)(uint32_t)v[3] << 32;
-      if (d >= 8) lo = hi, hi = 0;
-      if (d >= 16) lo = 0;
-      const int bits = 8 * (d & 7);
-      if (bits) lo = lo >> bits | hi << (64 - bits), hi >>= bits;
-      v = i32x4{(int)lo, (int)(lo >> 32), (int)hi, (int)(hi >> 32)};
-    }
-  } else {
-    int8_t b[16];
+  __builtin_memcpy(&v, row + (j < n - 16 ? j : n - 16), 16);
+  return v;
+}
+__device__ inline i32x4 move_down(i32x4 v, int j, int n) {
+  const int d = j - n + 16;
+  if (d <= 0) return v;
+  uint64_t lo = (uint32_t)v[0] | (uint64_t)(uint32_t)v[1] << 32;
+  uint64_t hi = (uint32_t)v[2] | (uint64_t)(uint32_t)v[3] << 32;
+  if (d >= 8) lo = hi, hi = 0;
+  if (d >= 16) lo = 0;
+  const int bits = 8 * (d & 7);
+  if (bits) lo = lo >> bits | hi << (64 - bits), hi >>= bits;
+  return i32x4{(int)lo, (int)(lo >> 32), (int)hi, (int)(hi >> 32)};
+}
+// A row below 16 features: j = 0 holds all of it.
+__device__ inline i32x4 load_tiny(const int8_t *row, int j, int n) {
+  i32x4 v;
+  int8_t b[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) b[i] = j + i < n ? row[j + i] : (int8_t)0;
-    __builtin_memcpy(&v, b, 16);
-  }
+  for (int i = 0; i < 16; ++i) b[i] = j + i < n ? row[j + i] : (int8_t)0;
+  __builtin_memcpy(&v, b, 16);
   return v;
 }
 
@@ -50,19 +52,27 @@ __device__ inline void load_floats(const float *p, int64_t at, int64_t n, float 
   }
 }
 
-// Four neighbouring outputs of a row.
+// What four neighbouring outputs of a row take besides their sums.  Read ahead of the sums, so that
+// a short call does not wait for memory twice.
+struct Scales {
+  float row, output[4], bias[4];
+
+  __device__ void load(const MatmulArgs &a, int64_t r, int64_t o) {
+    row = r < a.n_rows ? a.a_scale[r] : 0.0f;
+    load_floats<4>(a.b_scale, o, a.n_outputs, output);
+    if (a.bias) load_floats<4>(a.bias, o, a.n_outputs, bias);
+  }
+};
+
 template <typename T>
-__device__ inline void store_outputs(const MatmulArgs &a, int64_t row, int64_t o, i32x4 sum) {
+__device__ inline void store_outputs(const MatmulArgs &a, int64_t row, int64_t o, i32x4 sum,
+                                     const Scales &s) {
   if (row >= a.n_rows || o >= a.n_outputs) return;
-  const float row_scale = a.a_scale[row];
-  float scale[4], bias[4];
-  load_floats<4>(a.b_scale, o, a.n_outputs, scale);
-  if (a.bias) load_floats<4>(a.bias, o, a.n_outputs, bias);
   T y[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float v = (float)sum[i] * row_scale * scale[i];
-    if (a.bias) v += bias[i];
+    float v = (float)sum[i] * s.row * s.output[i];
+    if (a.bias) v += s.bias[i];
     y[i] = from_float<T>(v);
   }
   T *out = (T *)a.out + row * a.ldo + o;
@@ -156,6 +166,27 @@ __global__ __launch_bounds__(64 * W) void matmul_q8_stream_kernel(MatmulArgs a) 
 #pragma unroll
   for (int d = 0; d < S - 1; ++d)
     if (d < count) issue(d, d);
+  // The features past the last whole stage, and what this wave's tiles take besides their sums:
+  // asked for behind the first stages, where those do not fill the registers themselves.
+  const bool tail = n % 64 && wave == whole % W;
+  i32x4 last[N];
+  const int last_at = whole * 64 + 16 * (lane >> 4);
+  auto load_last = [&]() __attribute__((always_inline)) {
+    if (tail && n >= 16) {
+#pragma unroll
+      for (int p = 0; p < N; ++p) last[p] = load_raw(row_of_part(p, at), last_at, n);
+    }
+  };
+  constexpr int kTiles = (R * O + W - 1) / W;
+  Scales scales[kTiles];
+  auto load_scales = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int q = 0; q < kTiles; ++q) {
+      const int t = wave + q * W;
+      if (t < R * O) scales[q].load(a, r0 + 16 * (t / O) + at, o0 + 16 * (t % O) + 4 * (lane >> 4));
+    }
+  };
+  if constexpr (ALIGNED) load_last(), load_scales();
   for (int i0 = 0; i0 < count; i0 += S) {
 #pragma unroll
     for (int d = 0; d < S; ++d) {
@@ -187,18 +218,17 @@ __global__ __launch_bounds__(64 * W) void matmul_q8_stream_kernel(MatmulArgs a) 
           sum[r][o] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[o], x[r], sum[r][o], 0, 0, 0);
     }
   }
-  if (n % 64 && wave == whole % W) {  // the features past the last whole stage
-    const int j = whole * 64 + 16 * (lane >> 4);
-    i32x4 x[R];
+  if constexpr (!ALIGNED) load_last(), load_scales();
+  if (tail) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) x[r] = load_features<true>(row_of_part(r, at), j, n);
+    for (int p = 0; p < N; ++p)
+      last[p] = n >= 16 ? move_down(last[p], last_at, n) : load_tiny(row_of_part(p, at), last_at, n);
 #pragma unroll
-    for (int o = 0; o < O; ++o) {
-      const i32x4 w = load_features<true>(row_of_part(R + o, at), j, n);
+    for (int o = 0; o < O; ++o)
 #pragma unroll
       for (int r = 0; r < R; ++r)
-        sum[r][o] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x[r], sum[r][o], 0, 0, 0);
-    }
+        sum[r][o] =
+            __builtin_amdgcn_mfma_i32_16x16x64_i8(last[R + o], last[r], sum[r][o], 0, 0, 0);
   }
   wait_for<0, 0>();
   __syncthreads();  // the rings are left
@@ -208,11 +238,14 @@ __global__ __launch_bounds__(64 * W) void matmul_q8_stream_kernel(MatmulArgs a) 
 #pragma unroll
     for (int o = 0; o < O; ++o) lds[((wave * R + r) * O + o) * 64 + lane] = sum[r][o];
   __syncthreads();
-  for (int t = wave; t < R * O; t += W) {
+#pragma unroll
+  for (int q = 0; q < kTiles; ++q) {
+    const int t = wave + q * W;
+    if (t >= R * O) break;
     i32x4 all = lds[t * 64 + lane];
 #pragma unroll
     for (int w = 1; w < W; ++w) all += lds[(w * R * O + t) * 64 + lane];
-    store_outputs<T>(a, r0 + 16 * (t / O) + at, o0 + 16 * (t % O) + 4 * (lane >> 4), all);
+    store_outputs<T>(a, r0 + 16 * (t / O) + at, o0 + 16 * (t % O) + 4 * (lane >> 4), all, scales[q]);
   }
 }
 
@@ -453,7 +486,7 @@ __global__ __launch_bounds__(128 * WO) void matmul_q8_tile_kernel(MatmulArgs a) 
     const int j = whole * kStage + 16 * chunk;
 #pragma unroll
     for (int p = 0; p < 2 * P; ++p)
-      hold[0][p] = load_features<false>(from[p], j, n);
+      hold[0][p] = move_down(load_raw(from[p], j, n), j, n);
 #pragma unroll
     for (int p = 0; p < 2 * P; ++p) put(whole, p);  // not where the last whole stage is read
     meet(none(), none());
