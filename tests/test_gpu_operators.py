@@ -746,6 +746,20 @@ def test_numbers_of_slots():
     assert math.isfinite(float(B.distill(z, torch.zeros_like(ids), _normal(1, 5, 129))[0].sum()))
 
 
+@pytest.mark.parametrize("c,k", [(3, 4), (9, 16), (15, 17), (50, 33), (60, 64), (127, 65), (200, 100),
+                                 (255, 128), (255, 129), (350, 128), (400, 129), (1100, 70)])
+@pytest.mark.parametrize("dtype", TYPES, ids=ids_of)
+def test_lanes_and_slots(c, k, dtype):
+    """Slots in each of a lane's places; one row of several in a wave holds a class twice."""
+    n = 70
+    z = _normal(c, n, c, scale=2, dtype=dtype)
+    ids, t = _teacher(k, n, c, min(c, k), empty=0.0)
+    ids, t = (torch.nn.functional.pad(x, (0, k - x.shape[1]), value=-1) for x in (ids, t))
+    ids[5, -1] = ids[5, 0]
+    ids[66, : k // 2 + 1] = ids[66, 0]
+    _check_distill(z, ids, t, 1.5, None, f"c={c} k={k}")
+
+
 def test_more_rows_than_a_launch_takes():
     """Rows, and tiles, beyond what one dispatch counts go out as several launches."""
     n = (1 << 20) + 1234
