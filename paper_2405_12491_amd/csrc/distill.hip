@@ -6,14 +6,14 @@ namespace bridger {
 // With M = max z, e_j = exp((z_j - M) / T) and S = sum e_j:  q_j = e_j / S,
 // loss = T^2 sum_i p_i (log p_i - (z_i - M) / T + log S),  grad_j = w T (q_j - p_j).
 // z - M is formed before the division by T, so that neither overflows and exponents are at most 0;
-// exp goes through exp2, 1 / T and log2(e) in one factor that is rounded once.  Every lane keeps the
-// largest of its own logits and the sum relative to it; those pairs are joined across the row's
-// lanes at once.  The gradient is first w T q everywhere; the few kept classes are then written
-// again with their p taken off, by the row's first wave.
+// exp goes through exp2, 1 / T and log2(e) in one factor that is rounded once.  Every lane keeps the largest
+// of its own logits and the sum relative to it; those pairs are joined across the row's lanes at
+// once.  The gradient is first w T q everywhere; the few kept classes are then written again with
+// their p taken off, by the row's first wave.
 // Bound by memory from about 300 bytes a row on: 4096 x 32,000 bfloat16, loss and gradient from one
 // read and one write of 262 MB, take 106 us (5.0 TB/s, a large copy's rate); 2048 x 50,257 float 92
-// us for the loss and 138 for the gradient later.  Shorter rows are bound by their instructions, which
-// a row's slots and reductions are most of: 1M x 10 float, k = 4, 144 MB in 29 us.
+// us for the loss and 138 for the gradient later.  Shorter rows are bound by their instructions,
+// which a row's slots and reductions are most of: 1M x 10 float, k = 4, 144 MB in 29 us.
 constexpr int kSlots = 4;  // a lane's share of the teacher's slots, lanes of one wave at most
 
 template <int G>
@@ -87,7 +87,8 @@ __device__ inline Slots load_slots(const DistillArgs &a, int64_t row, const T *z
 }
 
 // How many pairs (slot of this wave's rows in groups below N, filled entry of the row's `ids`) hold
-// one class.  A slot meets itself: no class is there twice where this is the number of filled slots.
+// one class.  A slot meets itself: no class is there twice where this is the number of filled
+// slots.
 template <int N>
 __device__ inline int count_equal(const Slots &s, const int32_t *ids, int k) {
   int32_t id[N];
@@ -382,13 +383,13 @@ __global__ __launch_bounds__(1024) void distill_long_kernel(DistillArgs a) {
 }
 
 // Few lanes a row, so that a wave's reductions and slots serve many rows, but enough for its slots
-// (four a lane), and no more loads a lane than leave the registers for many waves.  Loss and gradient,
-// us, lanes x loads: 1M x 10 float (k = 4) 4 x 1 30, 8 x 1 58, 16 x 1 112; 1M x 64 (8) 8 x 2 108, 16 x 1
-// 148; 200,000 x 200 (10) 32 x 2 68, 16 x 4 74, 64 x 1 111; 100,000 x 347 (10) 32 x 4 55, 64 x 2 64;
-// 100,000 x 500 (10) 64 x 2 74, 32 x 4 81; 20,000 x 1500 (20) 64 x 8 43, 256 x 2 44; 20,000 x 1700 (20)
-// 256 x 2 47, 64 x 8 50; 20,000 x 4836 bfloat16 (84) 256 x 4 104, 512 x 2 161; 8192 x 12,000 (32) 512
-// x 4 75, 256 x 8 79, 1024 x 2 87; 4096 x 32,000 (64) 1024 x 4 100, 512 x 8 107; 2048 x 128,000 (32)
-// 1024 x 16 218, two walks over memory 257.
+// (four a lane), and no more loads a lane than leave the registers for many waves.  Loss and
+// gradient, us, lanes x loads: 1M x 10 float (k = 4) 4 x 1 30, 8 x 1 58, 16 x 1 112; 1M x 64 (8) 8
+// x 2 108, 16 x 1 148; 200,000 x 200 (10) 32 x 2 68, 16 x 4 74, 64 x 1 111; 100,000 x 347 (10) 32 x
+// 4 55, 64 x 2 64; 100,000 x 500 (10) 64 x 2 74, 32 x 4 81; 20,000 x 1500 (20) 64 x 8 43, 256 x 2
+// 44; 20,000 x 1700 (20) 256 x 2 47, 64 x 8 50; 20,000 x 4836 bfloat16 (84) 256 x 4 104, 512 x 2
+// 161; 8192 x 12,000 (32) 512 x 4 75, 256 x 8 79, 1024 x 2 87; 4096 x 32,000 (64) 1024 x 4 100, 512
+// x 8 107; 2048 x 128,000 (32) 1024 x 16 218, two walks over memory 257.
 template <typename T, bool BACKWARD>
 static int launch_pass(const DistillArgs &a, void *stream) {
   const int64_t bytes = (int64_t)a.n_classes * (int)sizeof(T);

@@ -87,15 +87,17 @@ __device__ inline void store_outputs(const MatmulArgs &a, int64_t row, int64_t o
 
 // ================================================================================ FEW ROWS
 // A workgroup holds 16 R rows by 16 O outputs; its W waves share the features, wave w taking stages
-// w, w + W, .. of 64, and join their sums in LDS.  So few rows still put enough waves on the chip to
-// stream the weights, and nothing is shared beyond a workgroup.  Each wave has a ring of S stages of
-// its own in LDS and S - 1 of them on their way, without a barrier.  The detour through LDS is for
-// the loads: an instruction that reads operands in place has neighbouring lanes in 16 different
-// rows, and takes 64 cycles; here four neighbouring lanes read 64 bytes of a row (16 cycles).  A
-// row's four 16-byte chunks stand at chunk ^ (row / 4 & 3): 16 rows of one chunk hit all banks.
+// w, w + W, .. of 64, and join their sums in LDS.  So few rows still put enough waves on the chip
+// to stream the weights, and nothing is shared beyond a workgroup.  Each wave has a ring of S
+// stages of its own in LDS and S - 1 of them on their way, without a barrier.  The detour through
+// LDS is for the loads: an instruction that reads operands in place has neighbouring lanes in 16
+// different rows, and takes 64 cycles; here four neighbouring lanes read 64 bytes of a row (16
+// cycles).  A row's four 16-byte chunks stand at chunk ^ (row / 4 & 3): 16 rows of one chunk hit
+// all banks.
 // ALIGNED: rows go to LDS without passing registers (aligned_rows).
-// One row is bound by memory: 1 x 32,000 x 4096, 131 MB in 25 to 27 us (4.9 to 5.2 TB/s).  Small products
-// are bound by their chain of launch, first loads, stages and join: 77 x 4099 x 2047, 9 MB, in 10.7.
+// One row is bound by memory: 1 x 32,000 x 4096, 131 MB in 25 to 27 us (4.9 to 5.2 TB/s).  Small
+// products are bound by their chain of launch, first loads, stages and join: 77 x 4099 x 2047, 9
+// MB, in 10.7.
 typedef __attribute__((address_space(3))) uint8_t lds_byte;
 
 // Rows [first, n) of a matrix, `ld` apart, for loads by 32-bit offsets from row `first`; what lies
@@ -132,8 +134,8 @@ __global__ __launch_bounds__(64 * W) void matmul_q8_stream_kernel(MatmulArgs a) 
   const int n = a.n_features;
   const int64_t tiles_o = (a.n_outputs + 16 * O - 1) / (16 * O);
   const int64_t r0 = blockIdx.x / tiles_o * (16 * R), o0 = blockIdx.x % tiles_o * (16 * O);
-  // lane l brings chunk (l & 3) ^ (l / 16) of row l / 4 of each part to slot l & 3 of that row; past
-  // the end the last row, or output, stands in: its sums are not stored
+  // lane l brings chunk (l & 3) ^ (l / 16) of row l / 4 of each part to slot l & 3 of that row;
+  // past the end the last row, or output, stands in: its sums are not stored
   auto row_of_part = [&](int p, int i) {
     const int64_t first = p < R ? r0 + 16 * p : o0 + 16 * (p - R), end = p < R ? a.n_rows : a.n_outputs;
     const int64_t row = first + i < end ? first + i : end - 1;
@@ -253,13 +255,13 @@ __global__ __launch_bounds__(64 * W) void matmul_q8_stream_kernel(MatmulArgs a) 
 
 // =============================================================================== MANY ROWS
 // A workgroup of 2 x WO waves holds B x B outputs, each wave (B / 2) x (B / WO) in tiles of 32 x 32
-// (v_mfma_i32_32x32x32_i8).  Stages of 128 features of its rows and weights go to a ring of stages in
-// LDS, one being multiplied in steps of 32 features while the others are on their way.  In LDS a
+// (v_mfma_i32_32x32x32_i8).  Stages of 128 features of its rows and weights go to a ring of stages
+// in LDS, one being multiplied in steps of 32 features while the others are on their way.  In LDS a
 // row's eight 16-byte chunks stand at chunk ^ (row / 2 & 7): the 16 lanes that are served in one
 // cycle have 16 neighbouring rows, even ones in 32 of the 64 banks and odd ones in the others.
 // 8192 x 8192 x 8192 in 443 to 452 us (2.43 to 2.48e15 operations/s).  The matrix cores are busy 76% of
-// the cycles, and the clock falls to 1.6 GHz under random operands (2.2 with zeros, at the same count
-// of cycles): power bounds it.
+// the cycles, and the clock falls to 1.6 GHz under random operands (2.2 with zeros, at the same
+// count of cycles): power bounds it.
 constexpr int kStage = 128;
 
 template <int B, bool DEEP>
@@ -338,8 +340,8 @@ __global__ __launch_bounds__(128 * WO) void matmul_q8_tile_kernel(MatmulArgs a) 
     }
   };
   i32x16 sum[CR][CO] = {};
-  // One step's matrix instructions, with beside(i) in the issue slots behind the i-th.  The order is
-  // pinned: the scheduler would gather the loads ahead of them and leave the matrix cores idle.
+  // One step's matrix instructions, with beside(i) in the issue slots behind the i-th.  The order
+  // is pinned: the scheduler would gather the loads ahead of them and leave the matrix cores idle.
   auto multiply = [&](const Operands &v, auto beside) __attribute__((always_inline)) {
 #pragma unroll
     for (int r = 0; r < CR; ++r)
@@ -558,8 +560,8 @@ __global__ __launch_bounds__(128 * WO) void matmul_q8_tile_kernel(MatmulArgs a) 
   }
 }
 
-// A workgroup a tile, at most 2^22 of them.  More than 64 KB of LDS are allowed once per kernel (each
-// has one size) and device.
+// A workgroup a tile, at most 2^22 of them.  More than 64 KB of LDS are allowed once per kernel
+// (each has one size) and device.
 static int launch_tiles(void (*k)(MatmulArgs), int64_t tiles, int threads, int lds_bytes,
                         const MatmulArgs &args, void *stream) {
   if (lds_bytes > 65536) {
@@ -616,19 +618,20 @@ static int launch_tile(const MatmulArgs &a, void *stream) {
 }
 
 // Which kernel runs, by an estimate of each one's time in us on 256 CUs.  A streamed tile of 16 R
-// rows by 16 O outputs takes its CU 1 us for 45 KB of rows and weights (35 KB where they pass through
-// registers), no less than 0.55 us for a wave's stage, 0.2 us to begin, and 0.4 us to join 16 tiles of
-// 16 x 16.  A stage of a 256 x 256 tile takes 1.1 us, 1.7 where all CUs compute (the clock falls), of
-// a 128 x 128 tile with four stages in LDS and one workgroup a CU 0.4, and 0.7 where all compute, and
-// 0.7 for each of two workgroups a CU with two stages; rows through registers take 1.35 to 1.5 times
-// as long.  No kernel is faster than memory.  Over 168 sizes (1 to 100,000 rows, 8 to 40,000 outputs,
-// 64 to 16,384 features) the choice is within 3% of the fastest of eleven kernels on average; the
-// worst is 1.34 times as long (70 x 6739 x 7644, where tiles of 80 rows would fit).  Sides, us: 1 x
-// 32000 x 4096 16 x 16 tiles 27.3, 32 x 32 31.2; 32 x 4096 x 4096 16 x 32 6.5, 32 x 32 7.7; 64 x 4096
-// x 4096 32 x 32 7.8, 64 x 32 9.7; 128 x 4096 x 4096 64 x 32 9.5, 64 x 64 12.2; 256 x 4096 x 4096 64 x
-// 64 12.8, 128 x 128 14.9; 512 x 4096 x 4096 20.8 against 16.0; 281 x 3520 x 13696 62.4 against 40.2 (weights in the last cache);
-// 2048 x 4096 x 4096 128 x 128 38.6 with two workgroups a CU, 41.3 with one, 256 x 256 45.3; 8192 x
-// 8192 x 1024 91.5 against 85.8.
+// rows by 16 O outputs takes its CU 1 us for 45 KB of rows and weights (35 KB where they pass
+// through registers), no less than 0.55 us for a wave's stage, 0.2 us to begin, and 0.4 us to join
+// 16 tiles of 16 x 16.  A stage of a 256 x 256 tile takes 1.1 us, 1.7 where all CUs compute (the
+// clock falls), of a 128 x 128 tile with four stages in LDS and one workgroup a CU 0.4, and 0.7
+// where all compute, and 0.7 for each of two workgroups a CU with two stages; rows through
+// registers take 1.35 to 1.5 times as long.  No kernel is faster than memory.  Over 168 sizes (1 to
+// 100,000 rows, 8 to 40,000 outputs, 64 to 16,384 features) the choice is within 3% of the fastest
+// of eleven kernels on average; the worst is 1.34 times as long (70 x 6739 x 7644, where tiles of
+// 80 rows would fit).  Sides, us: 1 x 32000 x 4096 16 x 16 tiles 27.3, 32 x 32 31.2; 32 x 4096 x
+// 4096 16 x 32 6.5, 32 x 32 7.7; 64 x 4096 x 4096 32 x 32 7.8, 64 x 32 9.7; 128 x 4096 x 4096 64 x
+// 32 9.5, 64 x 64 12.2; 256 x 4096 x 4096 64 x 64 12.8, 128 x 128 14.9; 512 x 4096 x 4096 20.8
+// against 16.0; 281 x 3520 x 13696 62.4 against 40.2 (weights in the last cache); 2048 x 4096 x
+// 4096 128 x 128 38.6 with two workgroups a CU, 41.3 with one, 256 x 256 45.3; 8192 x 8192 x 1024
+// 91.5 against 85.8.
 struct Estimate {
   const MatmulArgs &a;
   bool aligned;

@@ -5,9 +5,9 @@ namespace bridger {
 
 // q and scale need the row's largest |s w| and its mean square; both come from one walk, since the
 // norm's factor 1 / rms is common to the row: q = rint(s w 127 / max|s w|) and scale = max|s w| /
-// (127 rms).  Squares are added in double (a float square may overflow, and the mean loses nothing).
-// Where extreme inputs take s w out of float's middle range, y is formed in double instead, which
-// takes another walk.
+// (127 rms).  Squares are added in double (a float square may overflow, and the mean loses
+// nothing). Where extreme inputs take s w out of float's middle range, y is formed in double
+// instead, which takes another walk.
 __device__ inline uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
 __device__ inline bool middle(uint32_t most) {
   return most >= __float_as_uint(0x1p-60f) && most <= __float_as_uint(0x1p60f);
@@ -106,9 +106,9 @@ __global__ __launch_bounds__(kRowThreads<G>) void rmsnorm_q8_walk_kernel(Rmsnorm
 }
 
 // G lanes a row, C loads a lane of x, residual and weight; the row stays in registers from the one
-// read to the 8-bit store.  Bound by memory: 8192 x 8192 bfloat16 with a residual, 470 MB, in 78 to 86
-// us (5.5 to 6.0 TB/s; part of what is written stays in the last cache), 100,000 x 784 float 392 MB in
-// 71 to 84.  Rows of a few elements are bound by instructions: 1M x 28 float 144 MB in 38 us.
+// read to the 8-bit store.  Bound by memory: 8192 x 8192 bfloat16 with a residual, 470 MB, in 78 to
+// 86 us (5.5 to 6.0 TB/s; part of what is written stays in the last cache), 100,000 x 784 float 392
+// MB in 71 to 84.  Rows of a few elements are bound by instructions: 1M x 28 float 144 MB in 38 us.
 template <typename T, int G, int C>
 __global__ __launch_bounds__(kRowThreads<G>) void rmsnorm_q8_kernel(RmsnormArgs a) {
   constexpr int V = kPerLoad<T>, W = G > 64 ? G / 64 : 1;
@@ -186,10 +186,10 @@ __global__ __launch_bounds__(kRowThreads<G>) void rmsnorm_q8_kernel(RmsnormArgs 
 }
 
 // Few lanes a row, so that a wave's reductions serve many rows, but no more than four loads of each
-// array in a lane's registers.  With (without) a residual, us, lanes x loads: 1M x 10 float 4 x 1 22, 8
-// x 1 42; 500,000 x 100 16 x 2 118 (45), 32 x 1 112 (69), 64 x 1 166 (139); 100,000 x 784 64 x 4 180
-// (70), 256 x 1 176 (126); 16,384 x 4096 bfloat16 256 x 2 83, 512 x 2 101; 4096 x 11,008 512 x 4 57
-// (36), 1024 x 2 72 (48); 4096 x 16,384 85 (39) against 92 (54).
+// array in a lane's registers.  With (without) a residual, us, lanes x loads: 1M x 10 float 4 x 1
+// 22, 8 x 1 42; 500,000 x 100 16 x 2 118 (45), 32 x 1 112 (69), 64 x 1 166 (139); 100,000 x 784 64
+// x 4 180 (70), 256 x 1 176 (126); 16,384 x 4096 bfloat16 256 x 2 83, 512 x 2 101; 4096 x 11,008
+// 512 x 4 57 (36), 1024 x 2 72 (48); 4096 x 16,384 85 (39) against 92 (54).
 int launch_rmsnorm_q8(const RmsnormArgs &a, int32_t dtype, void *stream) {
   return with_type(dtype, [&](auto t) {
     using T = decltype(t);

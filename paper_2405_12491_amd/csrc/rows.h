@@ -44,9 +44,9 @@ __device__ inline float element(const u32x4 &raw, int i) {
   }
 }
 
-// Rows of at least 16 bytes (shorter ones: tiny).  The 16 bytes of elements from j on: the last, partial ones come from
-// the 16 bytes that end the row, moved down, so that a lane's loads need no branch; `fill` (two
-// elements' bits, or one's of 4 bytes) stands past the end.
+// Rows of at least 16 bytes (shorter ones: tiny).  The 16 bytes of elements from j on: the last,
+// partial ones come from the 16 bytes that end the row, moved down, so that a lane's loads need no
+// branch; `fill` (two elements' bits, or one's of 4 bytes) stands past the end.
 template <typename T>
 struct RowLoad {
   u32x4 raw;

@@ -30,9 +30,10 @@ __device__ inline void store_slot(const TopKArgs &a, int64_t row, int at, T valu
 }
 
 // ============================================================================ FEW CLASSES
-// One lane a row: its K best so far stay sorted in registers.  Classes come in ascending order and a
-// score goes behind its equals, so those stay in the order of their classes.  1M x 10 float, k = 4: 72
-// MB in 16 us (4.6 TB/s); with more slots bound by the insertion, classes x k steps of five instructions.
+// One lane a row: its K best so far stay sorted in registers.  Classes come in ascending order and
+// a score goes behind its equals, so those stay in the order of their classes.  1M x 10 float, k =
+// 4: 72 MB in 16 us (4.6 TB/s); with more slots bound by the insertion, classes x k steps of five
+// instructions.
 template <typename T, int K>
 __global__ __launch_bounds__(256) void top_k_lane_kernel(TopKArgs a) {
   constexpr int V = kPerLoad<T>;
@@ -89,14 +90,14 @@ __global__ __launch_bounds__(256) void top_k_lane_kernel(TopKArgs a) {
 // counting the larger ones.  Rows where too many or too few reach it (many equal scores, masked or
 // broken rows) take the general way below.
 // Long rows are bound by memory: 2048 x 128,000 bfloat16, k = 64, read once, 524 MB in 120 us (4.4
-// TB/s); short ones by a row's fixed steps (bound, collection, ranking): 100,000 x 1000, k = 10, 200
-// MB in 82.
+// TB/s); short ones by a row's fixed steps (bound, collection, ranking): 100,000 x 1000, k = 10,
+// 200 MB in 82.
 template <int G>
 constexpr int kCandidates = G == 64 ? 512 : 1024;  // of one wave: less LDS, so that many fit a CU
 
-// Where the row's scores are.  each(f): f(first class, 16 bytes of scores), the classes kStep apart,
-// in ascending order per lane; NaN past the row's end.  All lanes make the same number of calls.
-// In registers, lane after lane with whole loads: rows of at least 16 bytes.
+// Where the row's scores are.  each(f): f(first class, 16 bytes of scores), the classes kStep
+// apart, in ascending order per lane; NaN past the row's end.  All lanes make the same number of
+// calls. In registers, lane after lane with whole loads: rows of at least 16 bytes.
 template <typename T, int G, int C>
 struct InRegisters {
   static constexpr int kStep = 1;
@@ -234,7 +235,8 @@ __device__ inline void store_ranked(const TopKArgs &a, int64_t row, TopKShared<G
   }
 }
 
-// Stores scores for which `is` holds in ascending class order from slot `at` on; the next free slot.
+// Stores scores for which `is` holds in ascending class order from slot `at` on; the next free
+// slot.
 template <typename T, int G, typename Source, typename Is>
 __device__ inline int store_in_order(const TopKArgs &a, int64_t row, Source &x, TopKShared<G> &s,
                                      int at, int k, Is is) {
@@ -286,10 +288,10 @@ __device__ inline float wave_jth(float v, int j) {
 }
 
 // The general way, from any lower bound of the k-th largest score (-infinity where fewer than k are
-// numbers): scores above it first, then those equal to it and at last NaN, in ascending class order.
-// Where too many lie above it, the k-th largest score is found bit by bit and becomes the bound.
-// Its walks read the row from memory again (from the caches): held in registers they would make up
-// most of the kernel's code.
+// numbers): scores above it first, then those equal to it and at last NaN, in ascending class
+// order. Where too many lie above it, the k-th largest score is found bit by bit and becomes the
+// bound. Its walks read the row from memory again (from the caches): held in registers they would
+// make up most of the kernel's code.
 template <typename T, int G>
 __device__ inline void store_general(const TopKArgs &a, int64_t row, InMemory<T, G> &x,
                                      TopKShared<G> &s, float bound, int k) {
@@ -373,8 +375,8 @@ int launch_top_k(const TopKArgs &a, int32_t dtype, void *stream) {
   return with_type(dtype, [&](auto t) {
     using T = decltype(t);
     const int64_t bytes = (int64_t)a.n_classes * (int)sizeof(T);
-    // a lane's work is classes x k: beyond a few steps it takes many rows to pay (64 classes, k = 16,
-    // us, a lane / a wave a row: 8192 rows 16 / 8, 100,000 27 / 56)
+    // a lane's work is classes x k: beyond a few steps it takes many rows to pay (64 classes, k =
+    // 16, us, a lane / a wave a row: 8192 rows 16 / 8, 100,000 27 / 56)
     if (a.k <= 32 && a.n_classes <= 64 &&
         ((int64_t)a.n_classes * a.k <= 64 || a.n_rows >= 32768)) {
       auto lane = [&](auto k) { return launch_rows(k, 1, a, stream); };
@@ -387,9 +389,10 @@ int launch_top_k(const TopKArgs &a, int32_t dtype, void *stream) {
     }
     auto of = [&](auto k, int threads) { return launch_each_row(k, threads, a, stream); };
     const int k = a.k < a.n_classes ? a.k : a.n_classes;
-    // Few waves a row, each of which pays for its bound and its meetings, but so many that about half
-    // of their lanes hold one of the k (bfloat16, us, one / two / four waves: 100,000 x 1000, k = 10 82
-    // / 133 / 216, k = 64 647 / 209 / 289; 10,000 x 8000, k = 20 37 / 36 / 40, k = 64 309 / 55 / 55).
+    // Few waves a row, each of which pays for its bound and its meetings, but so many that about
+    // half of their lanes hold one of the k (bfloat16, us, one / two / four waves: 100,000 x 1000,
+    // k = 10 82 / 133 / 216, k = 64 647 / 209 / 289; 10,000 x 8000, k = 20 37 / 36 / 40, k = 64 309
+    // / 55 / 55).
     const bool small = a.n_classes <= 128;
     if (bytes <= 1024 && (k <= 32 || (small && k <= 64))) return of(top_k_short_kernel<T, 64>, 64);
     if (bytes <= 2048 && k > 32 && k <= 64) return of(top_k_short_kernel<T, 128>, 128);
