@@ -85,6 +85,12 @@ __device__ inline void store_outputs(const MatmulArgs &a, int64_t row, int64_t o
   }
 }
 
+// The tile of this workgroup: those of one XCD (every eighth workgroup) take neighbouring tiles.
+__device__ inline int64_t tile_of(int64_t tiles) {
+  const int64_t share = tiles / 8, more = tiles % 8, xcd = blockIdx.x % 8;
+  return xcd * share + (xcd < more ? xcd : more) + blockIdx.x / 8;
+}
+
 // ================================================================================ FEW ROWS
 // A workgroup holds 16 R rows by 16 O outputs; its W waves share the features, wave w taking stages
 // w, w + W, .. of 64, and join their sums in LDS.  So few rows still put enough waves on the chip
@@ -132,8 +138,10 @@ __global__ __launch_bounds__(64 * W) void matmul_q8_stream_kernel(MatmulArgs a) 
   const int lane = threadIdx.x & 63, at = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = a.n_features;
-  const int64_t tiles_o = (a.n_outputs + 16 * O - 1) / (16 * O);
-  const int64_t r0 = blockIdx.x / tiles_o * (16 * R), o0 = blockIdx.x % tiles_o * (16 * O);
+  // the tiles of one set of weights run side by side on one XCD, whose L2 they share
+  const int64_t tiles_r = (a.n_rows + 16 * R - 1) / (16 * R);
+  const int64_t tile = tile_of(gridDim.x);
+  const int64_t r0 = tile % tiles_r * (16 * R), o0 = tile / tiles_r * (16 * O);
   // lane l brings chunk (l & 3) ^ (l / 16) of row l / 4 of each part to slot l & 3 of that row;
   // past the end the last row, or output, stands in: its sums are not stored
   auto row_of_part = [&](int p, int i) {
@@ -278,12 +286,10 @@ __global__ __launch_bounds__(128 * WO) void matmul_q8_tile_kernel(MatmulArgs a) 
   const int t = threadIdx.x, lane = t & 63;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int n = a.n_features;
-  // Workgroups of one XCD (every eighth) take neighbouring tiles, in columns of 8 tiles of rows:
-  // those that run together share most of their rows and weights in the XCD's L2.
+  // An XCD's tiles run in columns of 8 tiles of rows: those that run together share most of their
+  // rows and weights in its L2.
   const int64_t tiles_r = (a.n_rows + B - 1) / B, tiles_o = (a.n_outputs + B - 1) / B;
-  const int64_t tiles = tiles_r * tiles_o;
-  const int64_t share = tiles / 8, more = tiles % 8, xcd = blockIdx.x % 8;
-  const int64_t tile = xcd * share + (xcd < more ? xcd : more) + blockIdx.x / 8;
+  const int64_t tile = tile_of(tiles_r * tiles_o);
   const int64_t group = tile / (8 * tiles_o), left = tiles_r - group * 8, height = left < 8 ? left : 8;
   const int64_t within = tile - group * 8 * tiles_o;
   const int64_t r0 = (group * 8 + within % height) * B, o0 = within / height * B;
