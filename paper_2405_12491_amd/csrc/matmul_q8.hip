@@ -624,20 +624,22 @@ static int launch_tile(const MatmulArgs &a, void *stream) {
 }
 
 // Which kernel runs, by an estimate of each one's time in us on 256 CUs.  A streamed tile of 16 R
-// rows by 16 O outputs takes its CU 1 us for 45 KB of rows and weights (35 KB where they pass
-// through registers), no less than 0.55 us for a wave's stage, 0.2 us to begin, and 0.4 us to join
-// 16 tiles of 16 x 16.  A stage of a 256 x 256 tile takes 1.1 us, 1.7 where all CUs compute (the
-// clock falls), of a 128 x 128 tile with four stages in LDS and one workgroup a CU 0.4, and 0.7
-// where all compute, and 0.7 for each of two workgroups a CU with two stages; rows through
-// registers take 1.35 to 1.5 times as long.  No kernel is faster than memory.  Over 168 sizes (1 to
-// 100,000 rows, 8 to 40,000 outputs, 64 to 16,384 features) the choice is within 3% of the fastest
-// of eleven kernels on average; the worst is 1.34 times as long (70 x 6739 x 7644, where tiles of
-// 80 rows would fit).  Sides, us: 1 x 32000 x 4096 16 x 16 tiles 27.3, 32 x 32 31.2; 32 x 4096 x
-// 4096 16 x 32 6.5, 32 x 32 7.7; 64 x 4096 x 4096 32 x 32 7.8, 64 x 32 9.7; 128 x 4096 x 4096 64 x
-// 32 9.5, 64 x 64 12.2; 256 x 4096 x 4096 64 x 64 12.8, 128 x 128 14.9; 512 x 4096 x 4096 20.8
-// against 16.0; 281 x 3520 x 13696 62.4 against 40.2 (weights in the last cache); 2048 x 4096 x
-// 4096 128 x 128 38.6 with two workgroups a CU, 41.3 with one, 256 x 256 45.3; 8192 x 8192 x 1024
-// 91.5 against 85.8.
+// rows by 16 O outputs takes its CU 1 us for 36 KB of rows and weights (28 KB where they pass
+// through registers), no less than 0.36 us for a wave's stage, 0.2 us to begin, and 0.5 us to join
+// 16 tiles of 16 x 16; more than two tiles a CU even out.  A stage of a 256 x 256 tile takes 1.1
+// us, 1.7 where all CUs compute (the clock falls), of a 128 x 128 tile with four stages in LDS and
+// one workgroup a CU 0.5, and 0.8 where all compute, and 0.7 for each of two workgroups a CU with
+// two stages; rows through registers take 1.35 to 1.5 times as long.  No kernel is faster than
+// memory.  Over 107 sizes (1 to 100,000 rows, 8 to 40,000 outputs, 64 to 16,384 features) the
+// choice is within 3% of the fastest of nine kernels on average, and 22% at most.  Sides, us: 1 x
+// 32000 x 4096 16 x 16 tiles 25, 16 x 32 26.3; 16 x 32000 x 4096 16 x 32 30.4, 16 x 16 32.9; 32 x
+// 4096 x 4096 16 x 32 5.5, 32 x 32 6.9; 32 x 32000 x 4096 32 x 64 31.4, 64 x 64 32.8, 32 x 32 36;
+// 64 x 4096 x 4096 32 x 32 6.6, 64 x 32 8; 128 x 4096 x 4096 64 x 32 8.6, 64 x 64 12.2; 256 x 4096
+// x 4096 64 x 64 12.8, 128 x 128 14.9; 512 x 4096 x 4096 20.8 against 16.0; 2048 x 4096 x 4096 128
+// x 128 38.6 with two workgroups a CU, 41.3 with one, 256 x 256 45.3; 8192 x 8192 x 1024 91.5
+// against 85.8.  Rings of more stages, which leave room for fewer workgroups a CU, take longer (16
+// x 4096 x 11,008 16 x 16 tiles with three stages 14.1, four 15.4; 32 x 4096 x 11,008 16 x 32 with
+// two 15.8, four 18.7).
 struct Estimate {
   const MatmulArgs &a;
   bool aligned;
@@ -657,10 +659,11 @@ struct Estimate {
     if (us < least) least = us, best = kernel;
   }
   void stream(int kernel, int R, int O, int W) {
-    const double n = tiles(16 * R, 16 * O), rounds = n > 1024 ? n / 256 : __builtin_ceil(n / 256);
-    const double moved = rounds * 16 * (R + O) * (double)a.n_features / (aligned ? 45e3 : 35e3);
-    const double stages = (a.n_features + 64 * W - 1) / (64 * W) * 0.55;
-    take(kernel, (moved > stages ? moved : stages) + 0.2 * rounds, 0.4 * rounds * R * O / 16);
+    const double n = tiles(16 * R, 16 * O), rounds = n > 512 ? n / 256 : __builtin_ceil(n / 256);
+    const double rows = a.n_rows < 16 * R ? (double)a.n_rows : 16 * R;
+    const double moved = rounds * (rows + 16 * O) * a.n_features / (aligned ? 36e3 : 28e3);
+    const double stages = (a.n_features + 64 * W - 1) / (64 * W) * 0.36;
+    take(kernel, (moved > stages ? moved : stages) + 0.2 * rounds, 0.5 * rounds * R * O / 16);
   }
   void tile(int kernel, int B, bool deep) {
     const double n = tiles(B, B), rounds = __builtin_ceil(n / 256), busy = n < 256 ? n / 256 : 1.0;
@@ -671,7 +674,7 @@ struct Estimate {
     if (B == 256) {
       take(kernel, rounds * (stages * (1.1 + 0.6 * busy) * (aligned ? 1.0 : 1.35) + 3.0));
     } else if (deep) {
-      take(kernel, rounds * (stages * (0.4 + 0.3 * busy) * (aligned ? 1.0 : 1.4) + 0.5));
+      take(kernel, rounds * (stages * (0.5 + 0.3 * busy) * (aligned ? 1.0 : 1.4) + 1.0));
     } else if (n >= 256) {
       take(kernel, n / 256 * stages * 0.7 * (aligned ? 1.0 : 1.5));
     }
@@ -685,19 +688,21 @@ static int launch_part(const MatmulArgs &a, int32_t dtype, void *stream) {
   e.stream(2, 2, 2, 8);
   e.stream(3, 4, 2, 4);
   e.stream(4, 4, 4, 4);
-  e.tile(5, 128, false);
-  e.tile(6, 256, false);
-  e.tile(7, 128, true);
+  e.stream(5, 2, 4, 8);
+  e.tile(6, 128, false);
+  e.tile(7, 256, false);
+  e.tile(8, 128, true);
   return with_type(dtype, [&](auto t) {
     using T = decltype(t);
     switch (e.best) {
-      case 0: return launch_stream<T, 1, 1, 8, 4>(a, stream);
-      case 1: return launch_stream<T, 1, 2, 8, 4>(a, stream);
-      case 2: return launch_stream<T, 2, 2, 8, 4>(a, stream);
+      case 0: return launch_stream<T, 1, 1, 8, 3>(a, stream);
+      case 1: return launch_stream<T, 1, 2, 8, 2>(a, stream);
+      case 2: return launch_stream<T, 2, 2, 8, 2>(a, stream);
       case 3: return launch_stream<T, 4, 2, 4, 3>(a, stream);
       case 4: return launch_stream<T, 4, 4, 4, 2>(a, stream);
-      case 5: return launch_tile<T, 128, 4, false>(a, stream);
-      case 6: return launch_tile<T, 256, 4, false>(a, stream);
+      case 5: return launch_stream<T, 2, 4, 8, 2>(a, stream);
+      case 6: return launch_tile<T, 128, 4, false>(a, stream);
+      case 7: return launch_tile<T, 256, 4, false>(a, stream);
       default: return launch_tile<T, 128, 4, true>(a, stream);
     }
   });
