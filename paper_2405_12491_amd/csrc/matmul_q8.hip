@@ -101,9 +101,9 @@ __device__ inline int64_t tile_of(int64_t tiles) {
 // cycles).  A row's four 16-byte chunks stand at chunk ^ (row / 4 & 3): 16 rows of one chunk hit
 // all banks.
 // ALIGNED: rows go to LDS without passing registers (aligned_rows).
-// One row is bound by memory: 1 x 32,000 x 4096, 131 MB in 25 to 27 us (4.9 to 5.2 TB/s).  Small
+// One row is bound by memory: 1 x 32,000 x 4096, 131 MB in 25 us (5.3 TB/s).  Small
 // products are bound by their chain of launch, first loads, stages and join: 77 x 4099 x 2047, 9
-// MB, in 10.7.
+// MB, in 9.
 typedef __attribute__((address_space(3))) uint8_t lds_byte;
 
 // Rows [first, n) of a matrix, `ld` apart, for loads by 32-bit offsets from row `first`; what lies
