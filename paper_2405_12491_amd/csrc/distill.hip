@@ -179,19 +179,20 @@ template <int G>
 __device__ inline void store_loss(const DistillArgs &a, int64_t row, const Slots &s,
                                   const RowStats &r, int lane) {
   const float inf = __builtin_inff();
-  const float log_mass = __logf(r.mass);
-  float v = s.kl;
+  // T log q, then p (which may pass 1 by its rounding), and T where it makes the product larger last:
+  // for logits of the type's lowest value nothing leaves float before the loss does
+  const float log_mass = a.temperature * __logf(r.mass);
+  const float low = fminf(a.temperature, 1.0f), high = fmaxf(a.temperature, 1.0f);
+  float v = a.temperature * a.temperature * s.kl;
 #pragma unroll
   for (int i = 0; i < kSlots; ++i) {
     if (i * kSlotLanes<G> >= a.k) break;
-    if (s.id[i] >= 0 && s.p[i] != 0.0f) {
-      const float log_q = s.z[i] == -inf ? -inf : (s.z[i] - r.most) / a.temperature - log_mass;
-      v -= s.p[i] * log_q;
-    }
+    if (s.id[i] >= 0 && s.p[i] != 0.0f)
+      v -= high * (s.p[i] * (low * (s.z[i] == -inf ? -inf : s.z[i] - r.most - log_mass)));
   }
   v = lanes_reduce<Sum, kSlotLanes<G>>(v);
   if (lane == 0) {
-    if (a.loss) a.loss[row] = s.any ? a.temperature * a.temperature * v : 0.0f;
+    if (a.loss) a.loss[row] = s.any ? v : 0.0f;
     if (a.stats) {
       a.stats[2 * row] = r.most;
       a.stats[2 * row + 1] = r.mass;

@@ -290,6 +290,29 @@ def test_distill_extreme_temperatures():
         assert torch.isfinite(loss).all() and torch.isfinite(grad).all()
 
 
+@pytest.mark.parametrize("width", [3, 40, 700, 30000, 280000])
+def test_distill_kept_classes_of_the_lowest_value(width):
+    """z / T leaves float for T below 1, the loss does not."""
+    z = _normal(1, 4, width)
+    ids, t = _teacher(2, 4, width, 2, empty=0.0)
+    z[1, ids[1, 0]] = torch.finfo(torch.float32).min
+    z[2] = torch.finfo(torch.float32).min
+    z[2, ids[2, 1]] = 0
+    z[3, ids[3].long()] = torch.finfo(torch.float32).min
+    loss, _ = _check_distill(z, ids, t, 0.5, None, f"{width}")
+    assert bool(torch.isfinite(loss).all())
+    # one class in three slots, whose p add up to a step more than 1
+    same = torch.ones(4, 3, dtype=torch.int32, device="cuda")
+    three = torch.tensor([-0.35896924138069153, 0.1679827868938446, 4.211813926696777], device="cuda").repeat(4, 1)
+    z[1, 1] = torch.finfo(torch.float32).min
+    loss, _ = _check_distill(z, same, three, 0.5, None, f"{width}")
+    assert bool(torch.isfinite(loss).all())
+    ids[:, 0], ids[:, 1], t[:, 0], t[:, 1] = 0, 1, 3.0, -3.0   # p of 0.82 and 0.18 at T = 4
+    z[1:, :], z[1, 1] = 0, torch.finfo(torch.float32).min
+    loss, _ = _check_distill(z, ids, t, 4.0, None, f"{width}")
+    assert bool(torch.isfinite(loss).all()) and float(loss[1]) > 1e38
+
+
 def test_distill_no_rows():
     z = torch.empty(0, 9, device="cuda", requires_grad=True)
     loss = B.distill_loss(z, torch.empty(0, 2, dtype=torch.int32, device="cuda"), torch.empty(0, 2, device="cuda"))
