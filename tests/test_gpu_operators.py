@@ -592,6 +592,32 @@ def test_two_graphs_and_two_streams_side_by_side():
         assert all(_same_bits(x, y) for k in NAMES_ALL for x, y in zip(a[k], o[k]))
 
 
+def test_calls_from_several_threads():
+    """Threads with a stream each; one of them is refused again and again, with its own message."""
+    from concurrent.futures import ThreadPoolExecutor
+    ops = [_every(seed=k, n=300, c=2000)[0] for k in (0, 50, 100)]
+    alone = [{k: [v.clone() for v in o[k][1]()] for k in NAMES_ALL} for o in ops]
+    torch.cuda.synchronize()
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(20):
+                outs = {k: ops[i][k][1]() for k in NAMES_ALL}
+            torch.cuda.current_stream().synchronize()
+        return all(_same_bits(x, y) for k in NAMES_ALL for x, y in zip(alone[i][k], outs[k]))
+
+    def refused(_):
+        z = ops[0]["distill"][0][0]
+        ids, t = _teacher(1, z.shape[0], z.shape[1], 2)
+        for _ in range(200):
+            with pytest.raises(B.BridgerError, match="temperature"):
+                B.distill(z, ids, t, 0.0)
+        return True
+
+    with ThreadPoolExecutor(4) as pool:
+        assert all([*pool.map(work, range(3)), *pool.map(refused, range(1))])
+
+
 def test_backward_in_a_graph_beside_an_eager_one():
     """distill gives the gradient without autograd, so a training step is captured while an eager
     graph of the same logits is alive."""
