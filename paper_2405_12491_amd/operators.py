@@ -228,20 +228,33 @@ def _make_distill_function():
             _call("bridger_distill", logits, *args, temperature, None, loss.data_ptr(),
                   stats.data_ptr(), None, 0)
             ctx.save_for_backward(logits, ids, teacher, stats)
-            ctx.temperature = temperature
+            ctx.temperature, ctx.args, ctx.stride = temperature, args, logits.stride()
             return loss
 
         @staticmethod
-        @torch.autograd.function.once_differentiable
         def backward(ctx, grad_loss):
-            logits, ids, teacher, stats = ctx.saved_tensors
-            weight = grad_loss.contiguous()
-            n, c, args = _check_distill(logits, ids, teacher, weight)
-            grad = ids.new_empty((n, c), dtype=logits.dtype)
-            _call("bridger_distill_backward", logits, *args, ctx.temperature, stats.data_ptr(),
-                  weight.data_ptr(), grad.data_ptr(), c)
-            return grad, None, None, None
+            # with a graph of the backward pass: one that cannot be differentiated again
+            return (once if torch.is_grad_enabled() else backward)(ctx, grad_loss)
 
+    # Runs on autograd's own thread, where every step costs several times its usual time (10 us on
+    # the caller's thread, 35 there): the forward pass's arguments serve again, unless hooks on
+    # saved tensors gave other ones, and autograd has set the device.
+    def backward(ctx, grad_loss):
+        logits, ids, teacher, stats = ctx.saved_tensors
+        args, weight = ctx.args, grad_loss.contiguous()
+        if not (logits.data_ptr() == args[0] and logits.stride() == ctx.stride
+                and ids.data_ptr() == args[3] and ids.is_contiguous()
+                and teacher.data_ptr() == args[4] and teacher.is_contiguous()):
+            args = _check_distill(logits, ids, teacher, weight)[2]
+        grad = ids.new_empty(logits.shape, dtype=logits.dtype)
+        st = _B._lib.bridger_distill_backward(
+            *args, ctx.temperature, stats.data_ptr(), weight.data_ptr(), grad.data_ptr(), args[7],
+            _B._launch_stream(grad.device))
+        if st != _B.BRIDGER_OK:
+            _B._check(st, "bridger_distill_backward")
+        return grad, None, None, None
+
+    once = torch.autograd.function.once_differentiable(backward)
     return Distill
 
 

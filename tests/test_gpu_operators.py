@@ -339,6 +339,33 @@ def test_distill_loss_in_autograd():
         torch.autograd.grad(g.sum(), leaf)
 
 
+@pytest.mark.parametrize("gap", [0, 5])
+def test_distill_loss_with_hooks_on_saved_tensors(gap):
+    """Saved tensors that come back from the host, where they lose the distance between rows."""
+    base = _normal(1, 40, 300 + gap, dtype=torch.bfloat16).requires_grad_()
+    ids, t = _teacher(2, 40, 300, 5)
+    up = torch.rand(40, device="cuda")
+    plain, = torch.autograd.grad(B.distill_loss(base[:, :300], ids, t, 2.0), base, up)
+    with torch.autograd.graph.save_on_cpu():
+        loss = B.distill_loss(base[:, :300], ids, t, 2.0)
+    again, = torch.autograd.grad(loss, base, up)
+    assert _same_bits(plain, again)
+
+
+def test_distill_loss_is_differentiated_once():
+    z = _normal(1, 6, 50).requires_grad_()
+    ids, t = _teacher(2, 6, 50, 5)
+    grad, = torch.autograd.grad(B.distill_loss(z, ids, t).sum(), z, create_graph=True)
+    plain, = torch.autograd.grad(B.distill_loss(z, ids, t).sum(), z)
+    assert _same_bits(grad.detach(), plain)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(grad.square().sum(), z)
+    loss = B.distill_loss(z, ids, t)
+    ids.add_(1)                            # what the backward pass needs has changed
+    with pytest.raises(RuntimeError):
+        loss.sum().backward()
+
+
 # -------------------------------------------------------------------------- rmsnorm_q8
 def _check_norm(x, w, r, eps=1e-6, what="", **out):
     before = [None if v is None else v.clone() for v in (x, r)]
