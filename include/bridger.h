@@ -453,7 +453,8 @@ bridger_status bridger_rmsnorm_q8(const void *x, int64_t ldx, const void *residu
  * Matrix product of 8-bit rows and 8-bit weights, with a scale for each of both (Table 4's
  * matmul):
  *     out[r, o] = a_scale[r] * b_scale[o] * sum_j a[r, j] * b[o, j]  (+ bias[o]).
- * The sum is exact (32-bit integers).
+ * The sum is exact (32-bit integers); it is rounded to float, then multiplied by a_scale and by
+ * b_scale, in this order, before the bias is added.
  *   a  int8 [n_rows, n_features], rows lda apart;  a_scale  float [n_rows]
  *   b  int8 [n_outputs, n_features], rows ldb apart;  b_scale  float [n_outputs]
  *   bias  float [n_outputs], or NULL
