@@ -83,10 +83,10 @@ _codes = {}  # torch dtype -> BRIDGER_*
 def _setup():
     global _torch
     import torch
+    _B.load_library()
     _codes.update({torch.float32: BRIDGER_F32, torch.bfloat16: BRIDGER_BF16,
                    torch.float16: BRIDGER_F16})
-    _torch = torch
-    _B.load_library()
+    _torch = torch  # last: other threads take it for the sign that all of this is done
 
 
 def _code(dtype) -> int:

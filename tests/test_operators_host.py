@@ -135,3 +135,35 @@ def test_raw_call_reports_its_error():
         B.bridger_top_k(A[0], 9, 0, 5, 10, 3, A[1], A[2])
     assert e.value.status == ARG and "distance between rows" in str(e.value)
     assert isinstance(B.load_library().bridger_top_k, ctypes._CFuncPtr)
+
+
+def test_a_library_that_is_missing_is_reported_every_time(monkeypatch, tmp_path):
+    import torch
+    monkeypatch.setattr(B, "LIB_PATH", str(tmp_path / "none.so"))
+    monkeypatch.setattr(B, "_lib", None)
+    monkeypatch.setattr(O, "_torch", None)
+    for _ in range(2):
+        with pytest.raises(OSError, match="build it"):
+            B.top_k(torch.zeros(2, 3), 1)
+
+
+def test_first_calls_of_several_threads(monkeypatch):
+    """A call that finds the operators ready finds the library loaded, however long that took
+    another thread."""
+    import time
+    from concurrent.futures import ThreadPoolExecutor
+
+    import torch
+    real, x = B.load_library, torch.zeros(2, 3)
+    monkeypatch.setattr(B, "_lib", None)
+    monkeypatch.setattr(O, "_torch", None)
+    monkeypatch.setattr(B, "load_library", lambda path=None: (time.sleep(0.3), real(path))[1])
+
+    def first(i):
+        time.sleep(0.05 * i)
+        with pytest.raises(TypeError):         # a tensor of the CPU: past the set-up
+            B.top_k(x, 1)
+        return B._lib is not None
+
+    with ThreadPoolExecutor(4) as pool:
+        assert all(pool.map(first, range(4)))
