@@ -5,7 +5,10 @@
 (include/bridger.h states formulas, types and limits).  ``top_k``, ``distill``, ``distill_loss``,
 ``rmsnorm_q8`` and ``matmul_q8`` take 2-D tensors whose rows are contiguous (any distance between
 rows), on any device, and launch on torch's current stream of that device.  There is no CPU
-fallback.
+fallback.  Only ``distill_loss`` can be differentiated: the others pass no gradient and no tangent
+on, whatever their inputs.  Outputs that the caller gives count as written in place: a backward pass
+that still needs what was there raises, and one that requires grad is refused while gradients are
+recorded.
 """
 from __future__ import annotations
 
@@ -138,6 +141,21 @@ def _dense(t, name, n, width, dtype, device):
         raise ValueError(f"{name} must be contiguous")
 
 
+def _writable(t, name):
+    """Refuses an output of the caller's whose gradient autograd would get wrong."""
+    if t.requires_grad and _torch.is_grad_enabled():
+        raise RuntimeError(f"{name} requires grad, and autograd does not see what is written into "
+                           "it: give a detached tensor, or call under torch.no_grad()")
+
+
+def _written(*outputs):
+    """Tells autograd, which may keep them for a backward pass, that outputs of the caller's (None:
+    none given) have been written."""
+    for t in outputs:
+        if t is not None:
+            _torch.autograd.graph.increment_version(t)
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -165,16 +183,19 @@ def top_k(scores, k: int, values=None, ids=None):
     k, dev = int(k), scores.get_device()
     if not 1 <= k <= BRIDGER_MAX_TOP:
         raise ValueError("k must be between 1 and BRIDGER_MAX_TOP")
+    given = values, ids
     if values is None:
         values = scores.new_empty((n, k))
     else:
         _dense(values, "values", n, k, scores.dtype, dev)
+        _writable(values, "values")
     if ids is None:
         ids = scores.new_empty((n, k), dtype=_torch.int32)
     else:
         _dense(ids, "ids", n, k, _torch.int32, dev)
     _call("bridger_top_k", scores, scores.data_ptr(), ld, _code(scores.dtype), n, c, k,
           values.data_ptr(), ids.data_ptr())
+    _written(*given)
     return values, ids
 
 
@@ -200,16 +221,20 @@ def distill(logits, ids, teacher, temperature: float = 1.0, weight=None, grad=No
     if _torch is None:
         _setup()
     n, c, args = _check_distill(logits, ids, teacher, weight)
+    given = loss, grad
     if loss is None:
         loss = teacher.new_empty((n,), dtype=_torch.float32)
     else:
         _vector(loss, "loss", n, _torch.float32, logits.get_device())
+        _writable(loss, "loss")
     if grad is None:
         grad, ldg = ids.new_empty((n, c), dtype=logits.dtype), c
     else:
         ldg = _rows(grad, "grad", c, n, logits.dtype, logits.get_device())[2]
+        _writable(grad, "grad")
     _call("bridger_distill", logits, *args, float(temperature), _ptr(weight), loss.data_ptr(), None,
           grad.data_ptr(), ldg)
+    _written(*given)
     return loss, grad
 
 
@@ -289,6 +314,7 @@ def rmsnorm_q8(x, weight=None, residual=None, eps: float = 1e-6, q=None, scale=N
     ldr = 0 if residual is None else _rows(residual, "residual", f, n, dtype, dev)[2]
     if weight is not None:
         _vector(weight, "weight", f, dtype, dev)
+    given = q, scale, total
     if q is None:
         q, ldq = x.new_empty((n, f), dtype=_torch.int8), f
     else:
@@ -297,13 +323,16 @@ def rmsnorm_q8(x, weight=None, residual=None, eps: float = 1e-6, q=None, scale=N
         scale = x.new_empty((n,), dtype=_torch.float32)
     else:
         _vector(scale, "scale", n, _torch.float32, dev)
+        _writable(scale, "scale")
     ldt = f
     if total is not None:
         ldt = _rows(total, "total", f, n, dtype, dev)[2]
+        _writable(total, "total")
     elif residual is not None:
         total = x.new_empty((n, f))
     _call("bridger_rmsnorm_q8", x, x.data_ptr(), ldx, _ptr(residual), ldr, _ptr(weight), code, n, f,
           float(eps), _ptr(total), ldt, q.data_ptr(), ldq, scale.data_ptr())
+    _written(*given)
     return q, scale, total
 
 
@@ -320,6 +349,7 @@ def matmul_q8(a, a_scale, b, b_scale, bias=None, dtype=None, out=None):
     _vector(b_scale, "b_scale", m, f32, dev)
     if bias is not None:
         _vector(bias, "bias", m, f32, dev)
+    given = out
     if out is None:
         dtype = dtype or _torch.bfloat16
         code = _code(dtype)
@@ -327,6 +357,8 @@ def matmul_q8(a, a_scale, b, b_scale, bias=None, dtype=None, out=None):
     else:
         ldo = _rows(out, "out", m, n, dtype, dev)[2]
         code = _code(out.dtype)
+        _writable(out, "out")
     _call("bridger_matmul_q8", a, a.data_ptr(), lda, a_scale.data_ptr(), b.data_ptr(), ldb,
           b_scale.data_ptr(), _ptr(bias), n, m, f, code, out.data_ptr(), ldo)
+    _written(given)
     return out

@@ -881,3 +881,76 @@ def test_products_in_a_graph(n, m, f):
         g.replay()
         torch.cuda.synchronize()
         R.check_matmul(a, sa, b, sb, None, out, f"replay {rep}")
+
+
+def test_autograd_sees_what_the_library_writes():
+    """Memory that a backward pass still needs, overwritten by each output that a caller can give."""
+    z0 = _normal(1, 6, 50, scale=2)
+    ids, t = _teacher(2, 6, 50, 5)
+    x, r = _normal(3, 6, 50), _normal(4, 6, 50)
+    a, b = _int8(5, 6, 50), _int8(6, 50, 50)
+    one, many = torch.ones(6, device="cuda"), torch.ones(50, device="cuda")
+
+    def saved(shape, write, dtype=torch.float32):
+        # exp keeps its result for its gradient; whole numbers are kept by index_select
+        if dtype.is_floating_point:
+            out = _normal(7, *shape).requires_grad_().exp()
+            write(out.detach())
+        else:
+            index = torch.zeros(shape[0] * shape[1], dtype=dtype, device="cuda")
+            out = _normal(7, 50).requires_grad_().index_select(0, index)
+            write(index.view(shape))
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            out.sum().backward()
+
+    saved((6, 5), lambda o: B.top_k(z0, 5, values=o))
+    saved((6, 5), lambda o: B.top_k(z0, 5, ids=o), torch.int32)
+    saved((6, 50), lambda o: B.distill(z0, ids, t, grad=o))
+    saved((1, 6), lambda o: B.distill(z0, ids, t, loss=o[0]))
+    saved((6, 50), lambda o: B.distill(o, ids, t, grad=o))
+    saved((6, 50), lambda o: B.rmsnorm_q8(x, None, r, total=o))
+    saved((6, 50), lambda o: B.rmsnorm_q8(o, None, r, total=o))
+    saved((6, 50), lambda o: B.rmsnorm_q8(x, None, o, total=o))
+    saved((1, 6), lambda o: B.rmsnorm_q8(x, scale=o[0]))
+    saved((6, 50), lambda o: B.matmul_q8(a, one, b, many, out=o))
+    q = torch.zeros(6, 50, dtype=torch.int8, device="cuda")
+    before = q._version
+    B.rmsnorm_q8(x, q=q)
+    assert q._version > before
+    # the logits, and the ids, that distill_loss keeps itself
+    for write in (lambda z, i: B.distill(z.detach(), i, t, grad=z.detach()),
+                  lambda z, i: B.top_k(z.detach(), 5, ids=i)):
+        z, i = (z0 * 1.0).requires_grad_(), ids.clone()
+        loss = B.distill_loss(z, i, t)
+        write(z, i)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.sum().backward()
+    # an output of the call's own tells nobody
+    z = (z0 * 1.0).requires_grad_()
+    loss = B.distill_loss(z, ids, t)
+    B.distill(z, ids, t)
+    B.top_k(z, 5)
+    loss.sum().backward()
+
+
+def test_outputs_that_require_grad():
+    z = _normal(1, 6, 50).requires_grad_()
+    ids, t = _teacher(2, 6, 50, 5)
+    a, one = _int8(5, 6, 50), torch.ones(6, device="cuda")
+    small = _normal(3, 6, 5).requires_grad_()
+    row = _normal(4, 6).requires_grad_()
+    before = z.detach().clone()
+    calls = [lambda: B.top_k(z, 5, values=small), lambda: B.distill(z, ids, t, grad=z),
+             lambda: B.distill(z, ids, t, loss=row), lambda: B.rmsnorm_q8(z, total=z),
+             lambda: B.rmsnorm_q8(z, scale=row), lambda: B.rmsnorm_q8(z, None, z * 1.0, total=z),
+             lambda: B.matmul_q8(a, one, a, one, out=(_normal(5, 6, 6).requires_grad_() * 1.0))]
+    for call in calls:
+        with pytest.raises(RuntimeError, match="requires grad"):
+            call()
+    assert torch.equal(z, before)
+    ref = B.distill(before, ids, t)
+    with torch.no_grad():                      # as torch's own in-place operations
+        version = z._version
+        loss, grad = B.distill(z, ids, t, grad=z)
+    assert grad is z and z._version > version
+    assert _same_bits(loss, ref[0]) and _same_bits(z.detach(), ref[1])

@@ -167,3 +167,33 @@ def test_first_calls_of_several_threads(monkeypatch):
 
     with ThreadPoolExecutor(4) as pool:
         assert all(pool.map(first, range(4)))
+
+
+def test_outputs_that_autograd_tracks():
+    """Without gradients a tracked output may be written; with them it is refused, as torch refuses
+    its own `out=`."""
+    import torch
+    leaf = torch.zeros(2, 3, requires_grad=True)
+    for t in (leaf, leaf * 2, (leaf * 2)[:1]):
+        with pytest.raises(RuntimeError, match="values requires grad"):
+            O._writable(t, "values")
+        with torch.no_grad():
+            O._writable(t, "values")
+    for t in (leaf.detach(), torch.zeros(3)):
+        O._writable(t, "values")
+
+
+def test_autograd_hears_of_what_was_written():
+    import torch
+    base = torch.zeros(4, 6)
+    view, other = base[:, 1:3], torch.zeros(2)
+    O._written(view, None, other)
+    assert base._version == view._version == 1 and other._version == 1
+    with torch.inference_mode():
+        inner = torch.zeros(2)
+    O._written(inner, None)                    # has no version, and nothing saves it
+    x = torch.ones(3, requires_grad=True)
+    y = x.exp()
+    O._written(y.detach())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
