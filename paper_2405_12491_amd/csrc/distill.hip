@@ -184,11 +184,13 @@ __device__ inline void store_loss(const DistillArgs &a, int64_t row, const Slots
   const float log_mass = a.temperature * __logf(r.mass);
   const float low = fminf(a.temperature, 1.0f), high = fmaxf(a.temperature, 1.0f);
   float v = a.temperature * a.temperature * s.kl;
+  const bool number = r.mass == r.mass;  // of a broken row no class has a log q, masked ones neither
 #pragma unroll
   for (int i = 0; i < kSlots; ++i) {
     if (i * kSlotLanes<G> >= a.k) break;
     if (s.id[i] >= 0 && s.p[i] != 0.0f)
-      v -= high * (s.p[i] * (low * (s.z[i] == -inf ? -inf : s.z[i] - r.most - log_mass)));
+      v -= high *
+           (s.p[i] * (low * (number && s.z[i] == -inf ? -inf : s.z[i] - r.most - log_mass)));
   }
   v = lanes_reduce<Sum, kSlotLanes<G>>(v);
   if (lane == 0) {

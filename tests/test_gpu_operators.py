@@ -954,3 +954,32 @@ def test_outputs_that_require_grad():
         loss, grad = B.distill(z, ids, t, grad=z)
     assert grad is z and z._version > version
     assert _same_bits(loss, ref[0]) and _same_bits(z.detach(), ref[1])
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids_of)
+@pytest.mark.parametrize("width", [2, 3, 10, 600, 9000, 70000, 140000])
+def test_distill_masked_kept_class_in_a_broken_row(width, dtype):
+    """A row whose only wanted class is masked has loss +infinity, unless its logits hold a NaN or
+    +infinity: then there is no distribution, and the loss is NaN as its gradient is."""
+    z = _normal(3, 6, width, dtype=dtype)
+    at = width // 2
+    ids = torch.full((6, 2), -1, dtype=torch.int32, device="cuda")
+    ids[:, 0] = at
+    t = torch.zeros(6, 2, device="cuda")
+    z[:, at] = -inf
+    z[1, 0] = nan
+    z[2, 0] = inf
+    z[3] = nan                                    # everything else is broken
+    z[3, at] = -inf
+    z[4, 0] = nan
+    ids[4, 1], t[4, 1] = 0, -inf                  # kept, but not wanted
+    z[5] = -inf
+    leaf = z.clone().requires_grad_()
+    alone = B.distill_loss(leaf, ids, t, 2.0)
+    late, = torch.autograd.grad(alone.sum(), leaf)
+    loss, grad = B.distill(z, ids, t, 2.0)
+    for lo, g in ((loss, grad), (alone, late)):
+        assert lo[0] == inf and lo[5] == inf
+        assert torch.isnan(lo[1:5]).all() and torch.isnan(g[1:5]).all()
+        # T (q - p), from what is left
+        assert torch.isfinite(g[[0, 5]]).all() and (g[[0, 5], at] == -2).all()
