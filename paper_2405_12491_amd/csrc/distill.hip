@@ -332,9 +332,15 @@ __global__ __launch_bounds__(1024) void distill_long_kernel(DistillArgs a) {
     s.any = lds_any != 0;
     r = {a.stats[2 * row], a.stats[2 * row + 1], s.any};
   } else {
-    float most = lane < n - whole ? to_float(z[whole + lane]) : -inf;
-    float mass = most == -inf ? 0.0f : 1.0f;
-    if (most != most || most == inf) mass = __builtin_nanf("");
+    // A lane adds n / 1024 exponentials, too many for one float (2^27 equal ones were off by 1e-3):
+    // those of a step are added in float, the steps in double.  They are relative to `base`, which
+    // goes up to the largest logit only once that is 2^kAhead ahead in the exponential: a change of
+    // scale is off by a rounding, logits that rise slowly would make one at every step, and so no
+    // more than a few of them reach what the sum ends with.
+    constexpr float kAhead = 4.0f;
+    float base = lane < n - whole ? to_float(z[whole + lane]) : -inf, most = base;
+    double sum = base == -inf ? 0.0 : 1.0;
+    if (base != base || base == inf) sum = __builtin_nan("");
     for (int64_t j = (int64_t)lane * V; j < whole; j += (int64_t)G * V * U) {
       u32x4 raw[U];
 #pragma unroll
@@ -345,21 +351,27 @@ __global__ __launch_bounds__(1024) void distill_long_kernel(DistillArgs a) {
           const uint32_t f = fill_of((T)-inf);
           raw[u] = u32x4{f, f, f, f};
         }
-      float top = most;
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int i = 0; i < V; ++i) top = fmaxf(top, element<T>(raw[u], i));
-      const float safe = top == -inf ? 0.0f : top;
-      mass *= __builtin_amdgcn_exp2f((most - safe) * factor);
+        for (int i = 0; i < V; ++i) most = fmaxf(most, element<T>(raw[u], i));
+      // (a base that is NaN goes too, the sum being NaN already)
+      if (most != -inf && !((most - base) * factor <= kAhead)) {
+        sum *= (double)__builtin_amdgcn_exp2f((base - most) * factor);
+        base = most;
+      }
+      const float safe = base == -inf ? 0.0f : base;
+      float step = 0.0f;
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int i = 0; i < V; ++i)
-          mass += __builtin_amdgcn_exp2f((element<T>(raw[u], i) - safe) * factor);
-      most = top;
+          step += __builtin_amdgcn_exp2f((element<T>(raw[u], i) - safe) * factor);
+      sum += (double)step;
     }
-    if (most != most) most = -inf;  // NaN is in the mass
+    if (most != most) most = base = -inf;  // NaN is in the sum
+    if (base != most) sum *= (double)__builtin_amdgcn_exp2f((base - most) * factor);
+    const float mass = (float)sum;
     r = join_stats<G>(most, mass, s.any, factor, lds, &lds_any);
     s.any = r.any;
     if (lane < 64) store_loss<G>(a, row, s, r, lane);

@@ -983,3 +983,70 @@ def test_distill_masked_kept_class_in_a_broken_row(width, dtype):
         assert torch.isnan(lo[1:5]).all() and torch.isnan(g[1:5]).all()
         # T (q - p), from what is left
         assert torch.isfinite(g[[0, 5]]).all() and (g[[0, 5], at] == -2).all()
+
+
+def _check_long_row(z, T, most, S, at, what):
+    """One row of float or bfloat16 logits whose sum of exponentials, relative to the largest, is S;
+    the teacher wants class `at` alone, one of the largest: loss = T^2 log S, and the gradient of
+    the other classes is T e^x / S.
+
+    In half steps U of a float, S is off by: the exponents, whose difference, factor and product are
+    rounded (3 |x|, with |x| below 2.8 or weighed by e^x), and 2 for the exponential, 12; 32 terms
+    added in float, 31; changes of scale by e^2.77 and more, each 12 and 1/16 of the one before, 13;
+    the last one, 12; the double sum's rounding, 1; two joins of lanes whose largest are close, of a
+    product and an exponential, 4 each, and 10 additions.  Together below 100.  The logarithm is off
+    by 4 of its own size with its constant, the products with T and T^2 by 3."""
+    n, U = z.shape[1], R.U
+    ids = torch.tensor([[at]], dtype=torch.int32, device="cuda")
+    t = torch.zeros(1, 1, device="cuda")
+    want = T * T * math.log(S)
+    tol = T * T * 100 * U + 7 * U * want
+    loss, grad = B.distill(z, ids, t, T)
+    leaf = z.detach().requires_grad_()
+    alone = B.distill_loss(leaf, ids, t, T)
+    late, = torch.autograd.grad(alone, leaf)
+    for name, lo, g in (("together", loss, grad), ("later", alone, late)):
+        off = abs(lo.item() - want)
+        assert off <= tol, f"{what} {name}: loss off by {off:.2e} of {tol:.2e}"
+        # S, its reciprocal (3), the exponential (2 and three times its exponent) and three products,
+        # then the type's rounding.  An exponential below the smallest normal float, 2^-126, is 0:
+        # that is T 2^-126 / S of the gradient at most (T = 0.25, 2^24 rising logits, S = 1.4e5:
+        # 2.1e-44, 15 of the smallest steps of a float; exponents down to -120, e^-87.3 = 2^-126)
+        worst = 0.0
+        for part in torch.arange(n, device="cuda").split(1 << 23):
+            x = (z[0, part].double() - most) / T
+            ref = T * torch.exp(x) / S
+            err = (g[0, part].double() - ref).abs()
+            most_off = ref * ((108 + 3 * x.abs()) * U * (1 + R.HALF[z.dtype]) + R.HALF[z.dtype])
+            most_off += R.TINY[z.dtype] + T * 2.0 ** -126 / S
+            err[part == at] = 0
+            worst = max(worst, float((err / most_off).max()))
+        assert worst <= 1, f"{what} {name}: gradient {worst} times the bound"
+        ref = T * (1 / S - 1)
+        assert abs(g[0, at].item() - ref) <= abs(ref) * (4 * U + R.HALF[z.dtype])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=ids_of)
+@pytest.mark.parametrize("T,high", [(1.0, 0.357), (1.0, 1.2), (2.0, 0.21)])
+def test_distill_sum_of_a_very_long_row(T, high, dtype):
+    """2^27 classes: equal terms, which a float sum rounds the same way once it is large; every lane
+    has seen the larger ones before them."""
+    n, m = (1 << 27) + 5, 8192
+    z = torch.zeros(1, n, dtype=dtype, device="cuda")
+    z[0, :m] = high
+    most = z[0, 0].item()
+    S = m + (n - m) * math.exp(-most / T)
+    _check_long_row(z, T, most, S, 17, f"{n} x {high}")
+
+
+@pytest.mark.parametrize("T", [0.25, 1.0])
+@pytest.mark.parametrize("order", ["rising", "falling", "steps", "waves"])
+def test_distill_sum_of_a_long_row_in_order(order, T):
+    """Logits whose largest moves at every step, now and then, or never."""
+    n = (1 << 24) + 3
+    j = torch.arange(n, device="cuda", dtype=torch.float64) / n
+    z = {"rising": 30 * j, "falling": 30 - 30 * j, "steps": torch.floor(40 * j) * 0.9,
+         "waves": torch.sin(200 * j) * 20 * j}[order].float().view(1, -1)
+    most, at = z.double().max(1)
+    S = torch.exp((z.double() - most) / T).sum().item()
+    _check_long_row(z, T, most.item(), S, int(at), f"{order} T={T}")
