@@ -377,9 +377,11 @@ enum { BRIDGER_F32 = 0, BRIDGER_BF16 = 1, BRIDGER_F16 = 2 };
 
 /*
  * The k largest of every row's n_classes scores, largest first, with their class ids (Table
- * 4's topk; predict_labels is its k = 1).  Of equal scores (-0 and +0 are equal) the lower
- * class comes first; a NaN comes after every number.  The values are the scores themselves (a
- * zero with its sign; of a NaN, some NaN).  Slots beyond n_classes hold -infinity and the id -1.
+ * 4's topk).  Of equal scores (-0 and +0 are equal) the lower class comes first; a NaN comes
+ * after every number.  The values are the scores themselves (a zero with its sign; of a NaN, some
+ * NaN).  Slots beyond n_classes hold -infinity and the id -1.  With k = 1 on predict's scores the
+ * id is predict_labels' for a model of two classes or more, unless scores are equal or NaN: labels
+ * compare the classes' sums before those are rounded to float (and before the transform).
  *   scores  [n_rows, n_classes], 1 <= n_classes < 2^31
  *   k       1 <= k <= BRIDGER_MAX_TOP
  *   values  [n_rows, k] of the scores' dtype, or NULL;  ids  int32 [n_rows, k], or NULL

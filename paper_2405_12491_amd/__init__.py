@@ -346,7 +346,9 @@ class Forest:
 
     def predict_top(self, X, k: int, values=None, ids=None):
         """The k largest outputs of every row, largest first, and their classes (predict, then
-        top_k): a teacher's scores for distill.  With the identity transform they are logits."""
+        top_k): a teacher's scores for distill.  With the identity transform they are logits.  Of
+        outputs that round alike the lower class comes first, where predict_labels still takes the
+        larger sum."""
         return operators.top_k(self.predict(X), k, values, ids)
 
     def predict_leaves(self, X, out=None):

@@ -1050,3 +1050,22 @@ def test_distill_sum_of_a_long_row_in_order(order, T):
     most, at = z.double().max(1)
     S = torch.exp((z.double() - most) / T).sum().item()
     _check_long_row(z, T, most.item(), S, int(at), f"{order} T={T}")
+
+
+def test_labels_and_first_scores_part_where_sums_round_alike():
+    """Sums of 1 and 1 + 2^-30 are one float: the label is the larger sum's, the first score the
+    lower class's."""
+    from synth import Forest
+    leaf = np.full(3, -1, np.int32)
+    model = Forest(n_features=1, n_classes=2, tree_offsets=np.arange(4, dtype=np.int64),
+                   feature=np.zeros(3, np.int32), threshold=np.zeros(3, np.float32), left=leaf, right=leaf,
+                   value=np.array([1, 1, 2.0 ** -30], np.float32), tree_class=np.array([0, 1, 1], np.int32))
+    X = torch.zeros(5, 1, device="cuda")
+    with B.Forest(model) as f:
+        scores, (values, ids), labels = f.predict(X), f.predict_top(X, 2), f.predict_labels(X)
+    assert (scores == 1).all() and (values == 1).all()
+    assert ids.tolist() == [[0, 1]] * 5 and labels.tolist() == [1] * 5
+    model.value[2] = 2.0 ** -20                    # sums that floats tell apart
+    with B.Forest(model) as f:
+        ids, labels = f.predict_top(X, 1)[1], f.predict_labels(X)
+    assert ids[:, 0].tolist() == labels.tolist() == [1] * 5
