@@ -117,8 +117,11 @@ def _rows(t, name, width, n, dtype, device):
     if w > _MOST or rows > _MOST:  # more than the entry points' 32 bits hold
         raise ValueError(f"{name} has 2^31 or more rows or elements a row")
     step, inner = t.stride()
-    if w > 1 and inner != 1:
-        raise ValueError(f"{name}'s rows must be contiguous")
+    if w > 1:
+        if inner != 1:
+            raise ValueError(f"{name}'s rows must be contiguous")
+    elif t.is_neg():  # (such a view's elements are never neighbours)
+        raise ValueError(f"{name} is a negated view: resolve_neg() it first")
     if rows <= 1:
         return rows, w, w
     if step < w:
@@ -132,7 +135,7 @@ def _vector(t, name, n, dtype, device):
     if t.get_device() != device:
         raise ValueError(f"{name} is on another device")
     shape = t.shape
-    if len(shape) != 1 or shape[0] != n or not (n <= 1 or t.stride(0) == 1):
+    if len(shape) != 1 or shape[0] != n or not (t.stride(0) == 1 if n > 1 else not t.is_neg()):
         raise ValueError(f"{name} must be contiguous [{n}]")
 
 

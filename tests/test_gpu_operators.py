@@ -1069,3 +1069,19 @@ def test_labels_and_first_scores_part_where_sums_round_alike():
     with B.Forest(model) as f:
         ids, labels = f.predict_top(X, 1)[1], f.predict_labels(X)
     assert ids[:, 0].tolist() == labels.tolist() == [1] * 5
+
+
+def test_negated_views_are_refused():
+    """The imaginary part of a conjugate holds the other sign; a row of one element of it looks like
+    any other."""
+    z = torch.complex(_normal(1, 6, 1), _normal(2, 6, 1)).conj().imag
+    assert z.is_neg() and z.shape == (6, 1)
+    ids, t = torch.zeros(6, 1, dtype=torch.int32, device="cuda"), torch.zeros(6, 1, device="cuda")
+    one, q = torch.ones(1, device="cuda"), torch.ones(1, 4, dtype=torch.int8, device="cuda")
+    for call in (lambda: B.top_k(z, 1), lambda: B.distill(z, ids, t), lambda: B.distill(t, ids, z),
+                 lambda: B.rmsnorm_q8(z), lambda: B.rmsnorm_q8(t, z[0]), lambda: B.matmul_q8(q, z[0], q, one),
+                 lambda: B.distill(t[:1], ids[:1], t[:1], weight=z[0])):
+        with pytest.raises(ValueError):
+            call()
+    values, _ = B.top_k(z.resolve_neg(), 1)
+    assert torch.equal(values, z)
