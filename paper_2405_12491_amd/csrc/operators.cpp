@@ -3,7 +3,6 @@
 
 #include <cmath>
 #include <cstdint>
-#include <string>
 
 #include "bridger.h"
 #include "operators.h"

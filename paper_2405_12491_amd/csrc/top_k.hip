@@ -328,14 +328,13 @@ __device__ inline void top_k_row(const TopKArgs &a, int64_t row, Source &x, TopK
 #pragma unroll
     for (int i = 0; i < V; ++i) top = fmaxf(top, element<T>(raw, i));
   });
-  const int share = (k + W - 1) / W;
-  float bound = wave_jth(top, share < 64 ? share : 64);
+  // (a share is at most 64: launch_top_k gives more than 64 slots four waves or more)
+  float bound = wave_jth(top, (k + W - 1) / W);
   if constexpr (G > 64) {
     if ((threadIdx.x & 63) == 0) s.bound[threadIdx.x >> 6] = bound;
     __syncthreads();
     bound = -lanes_reduce<Max, W>(-s.bound[threadIdx.x & (W - 1)]);
   }
-  if (share > 64) bound = -inf;
   int count = collect<T, G>(x, s, [&](float v) { return v >= bound; });
   if (count >= k && count <= kCandidates<G>) {
     store_ranked<T, G>(a, row, s, count, k);
