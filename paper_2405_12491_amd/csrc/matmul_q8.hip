@@ -630,8 +630,9 @@ static int launch_tile(const MatmulArgs &a, void *stream) {
 // us, 1.7 where all CUs compute (the clock falls), of a 128 x 128 tile with four stages in LDS and
 // one workgroup a CU 0.5, and 0.8 where all compute, and 0.7 for each of two workgroups a CU with
 // two stages; rows through registers take 1.35 to 1.5 times as long.  No kernel is faster than
-// memory.  Over 107 sizes (1 to 100,000 rows, 8 to 40,000 outputs, 64 to 16,384 features) the
-// choice is within 3% of the fastest of nine kernels on average, and 22% at most.  Sides, us: 1 x
+// memory.  Over 132 sizes (1 to 100,000 rows, 10 to 36,601 outputs, 64 to 16,256 features; two
+// measurements of each, averaged) the choice takes 4% longer than the fastest of nine kernels on
+// average, and 22% at most; 2% and 22% over the 61 sizes of 8 us or more.  Sides, us: 1 x
 // 32000 x 4096 16 x 16 tiles 25, 16 x 32 26.3; 16 x 32000 x 4096 16 x 32 30.4, 16 x 16 32.9; 32 x
 // 4096 x 4096 16 x 32 5.5, 32 x 32 6.9; 32 x 32000 x 4096 32 x 64 31.4, 64 x 64 32.8, 32 x 32 36;
 // 64 x 4096 x 4096 32 x 32 6.6, 64 x 32 8; 128 x 4096 x 4096 64 x 32 8.6, 64 x 64 12.2; 256 x 4096

@@ -290,7 +290,8 @@ def distill_loss(logits, ids, teacher, temperature: float = 1.0):
     """distill's loss of every row [n], differentiable in ``logits`` (once; the teacher is taken
     as constant).  Where logits need a gradient, a stream that is being captured is refused: autograd
     keeps nodes on the streams they were made on, and a captured backward pass that meets one of an
-    eager graph ends the process.  There take distill and hand its gradient on
+    eager graph ends the process.  (So the backward pass of a loss that was made outside does not
+    belong into a capture either.)  There take distill and hand its gradient on
     (``logits.backward(grad)``)."""
     global _distill_function
     if _torch is None:
