@@ -186,7 +186,7 @@ def top_k(scores, k: int, values=None, ids=None):
     k, dev = int(k), scores.get_device()
     if not 1 <= k <= BRIDGER_MAX_TOP:
         raise ValueError("k must be between 1 and BRIDGER_MAX_TOP")
-    given = values, ids
+    given = None if values is None and ids is None else (values, ids)
     if values is None:
         values = scores.new_empty((n, k))
     else:
@@ -198,7 +198,8 @@ def top_k(scores, k: int, values=None, ids=None):
         _dense(ids, "ids", n, k, _torch.int32, dev)
     _call("bridger_top_k", scores, scores.data_ptr(), ld, _code(scores.dtype), n, c, k,
           values.data_ptr(), ids.data_ptr())
-    _written(*given)
+    if given:
+        _written(*given)
     return values, ids
 
 
@@ -224,7 +225,7 @@ def distill(logits, ids, teacher, temperature: float = 1.0, weight=None, grad=No
     if _torch is None:
         _setup()
     n, c, args = _check_distill(logits, ids, teacher, weight)
-    given = loss, grad
+    given = None if loss is None and grad is None else (loss, grad)
     if loss is None:
         loss = teacher.new_empty((n,), dtype=_torch.float32)
     else:
@@ -237,7 +238,8 @@ def distill(logits, ids, teacher, temperature: float = 1.0, weight=None, grad=No
         _writable(grad, "grad")
     _call("bridger_distill", logits, *args, float(temperature), _ptr(weight), loss.data_ptr(), None,
           grad.data_ptr(), ldg)
-    _written(*given)
+    if given:
+        _written(*given)
     return loss, grad
 
 
@@ -318,7 +320,7 @@ def rmsnorm_q8(x, weight=None, residual=None, eps: float = 1e-6, q=None, scale=N
     ldr = 0 if residual is None else _rows(residual, "residual", f, n, dtype, dev)[2]
     if weight is not None:
         _vector(weight, "weight", f, dtype, dev)
-    given = q, scale, total
+    given = None if q is None and scale is None and total is None else (q, scale, total)
     if q is None:
         q, ldq = x.new_empty((n, f), dtype=_torch.int8), f
     else:
@@ -336,7 +338,8 @@ def rmsnorm_q8(x, weight=None, residual=None, eps: float = 1e-6, q=None, scale=N
         total = x.new_empty((n, f))
     _call("bridger_rmsnorm_q8", x, x.data_ptr(), ldx, _ptr(residual), ldr, _ptr(weight), code, n, f,
           float(eps), _ptr(total), ldt, q.data_ptr(), ldq, scale.data_ptr())
-    _written(*given)
+    if given:
+        _written(*given)
     return q, scale, total
 
 
@@ -364,5 +367,6 @@ def matmul_q8(a, a_scale, b, b_scale, bias=None, dtype=None, out=None):
         _writable(out, "out")
     _call("bridger_matmul_q8", a, a.data_ptr(), lda, a_scale.data_ptr(), b.data_ptr(), ldb,
           b_scale.data_ptr(), _ptr(bias), n, m, f, code, out.data_ptr(), ldo)
-    _written(given)
+    if given is not None:
+        _written(given)
     return out
