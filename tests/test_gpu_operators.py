@@ -1085,3 +1085,26 @@ def test_negated_views_are_refused():
             call()
     values, _ = B.top_k(z.resolve_neg(), 1)
     assert torch.equal(values, z)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids_of)
+@pytest.mark.parametrize("width", [70001, 140003, 140007])
+def test_distill_ends_of_long_rows(width, dtype):
+    """The elements past a long row's whole loads, alone or broken, with little or nothing before them."""
+    z = torch.full((8, width), -inf, dtype=dtype, device="cuda")
+    low = torch.finfo(dtype).min
+    z[0, -1] = 3                                  # the only class
+    z[1, -1], z[1, 5] = 3, 2
+    z[2, -1], z[2, 5] = low, 2
+    z[3], z[3, -1] = low, 1
+    z[4, -1], z[4, -2] = 1, 1
+    z[5, -1], z[5, 5] = nan, 2
+    z[6, -1], z[6, 5] = inf, 2
+    z[7, -1], z[7, 5] = 2, nan
+    ids = torch.full((8, 1), width - 1, dtype=torch.int32, device="cuda")
+    t = torch.zeros(8, 1, device="cuda")
+    for T in (1.0, 0.5):
+        loss, grad = _check_distill(z[:5], ids[:5], t[:5], T, None, f"{width} T={T}")
+        assert loss[0] == 0 and loss[3] == 0 and (grad[0] == 0).all()
+        loss, grad = B.distill(z[5:], ids[5:], t[5:], T)
+        assert torch.isnan(loss).all() and torch.isnan(grad).all()
