@@ -470,6 +470,44 @@ bridger_status bridger_matmul_q8(const int8_t *a, int64_t lda, const float *a_sc
                                  int32_t n_features, int32_t dtype, void *out, int64_t ldo,
                                  void *stream);
 
+/*
+ * The layers that a student is trained with, and its draw.  A lookup of a forest's leaves or of
+ * tokens in a table (Table 4's gather and sum):
+ *     out[r] = scale * sum_s table[first_s + ids[r, s]]
+ * over the slots s of the row.  Slot s reads the entries [offsets[s], offsets[s + 1]) of the table
+ * (a forest's tree offsets: predict_leaves' ids of tree s), or all of them without offsets.  An id
+ * outside its slot's entries, or outside the table, is an empty slot and adds nothing; a row of
+ * empty slots is zero.
+ *   ids      int32 [n_rows, n_slots], rows ldi apart;  1 <= n_slots < 2^31
+ *   offsets  int64 [n_slots + 1], ascending, or NULL
+ *   table    [n_entries, n_features] of dtype, rows ldt apart;  1 <= n_entries, n_features < 2^31
+ *   scale    finite
+ *   out      [n_rows, n_features] of dtype, rows ldo apart
+ */
+bridger_status bridger_embed(const int32_t *ids, int64_t ldi, const int64_t *offsets,
+                             const void *table, int64_t ldt, int32_t dtype, int64_t n_rows,
+                             int32_t n_slots, int32_t n_entries, int32_t n_features, float scale,
+                             void *out, int64_t ldo, void *stream);
+
+/*
+ * The table's gradient from the output's:
+ *     grad_table[e] = scale * sum of grad[r] over the slots (r, s) that read entry e,
+ * zero for an entry that none reads.  The slots are sorted by entry and added in an order that the
+ * ids alone decide; every entry is written, with n_rows == 0 too.
+ *   grad        [n_rows, n_features] of dtype, rows ldg apart
+ *   grad_table  [n_entries, n_features] of dtype, rows ldt apart
+ *   workspace   bridger_embed_backward_workspace bytes, aligned to 16, of this call alone until it
+ *               has run (no more than n_rows * n_slots = 2^31 - 1 slots: BRIDGER_ERR_UNSUPPORTED)
+ */
+bridger_status bridger_embed_backward(const int32_t *ids, int64_t ldi, const int64_t *offsets,
+                                      const void *grad, int64_t ldg, int32_t dtype, int64_t n_rows,
+                                      int32_t n_slots, int32_t n_entries, int32_t n_features,
+                                      float scale, void *grad_table, int64_t ldt, void *workspace,
+                                      int64_t workspace_bytes, void *stream);
+/* 0 for sizes that bridger_embed_backward refuses. */
+int64_t bridger_embed_backward_workspace(int64_t n_rows, int32_t n_slots, int32_t n_entries,
+                                         int32_t n_features);
+
 /* Message for the calling thread's most recent failed call ("" if none).  The
  * paper states no error interface; this is the library's own, so that nothing
  * throws across the C ABI (thread-local storage, valid until the thread's next

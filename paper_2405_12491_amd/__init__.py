@@ -99,6 +99,7 @@ def load_library(path: Optional[str] = None):
                  "bridger_forest_predict_csr_leaves"):
         getattr(lib, name).restype = ctypes.c_int
     operators.declare(lib)
+    layers.declare(lib)
     if path is None:
         _lib = lib
     return lib
@@ -431,7 +432,9 @@ class Forest:
         self.close()
 
 
-from . import operators  # noqa: E402  (uses load_library and _check)
+from . import layers, operators  # noqa: E402  (they use load_library and _check)
+from .layers import (  # noqa: E402,F401
+    bridger_embed, bridger_embed_backward, bridger_embed_backward_workspace, embed, embed_grad)
 from .operators import (  # noqa: E402,F401
     BRIDGER_BF16, BRIDGER_F16, BRIDGER_F32, BRIDGER_MATMUL_Q8_MAX_FEATURES, BRIDGER_MAX_TOP,
     bridger_distill, bridger_distill_backward, bridger_matmul_q8, bridger_rmsnorm_q8,

@@ -105,6 +105,16 @@ const char *distill_fault(const DistillArgs &a, int32_t dtype, int32_t teacher_d
   return nullptr;
 }
 
+// The sizes that both passes of the lookup have; nullptr when they are sound.
+const char *embed_fault(const EmbedArgs &a, int32_t dtype) {
+  if (const char *f = count_fault(a.n_rows, a.n_features)) return f;
+  if (a.n_slots < 1) return "n_slots must be >= 1";
+  if (a.n_entries < 1) return "n_entries must be >= 1";
+  if (!bytes_of(dtype)) return "unknown dtype";
+  if (!std::isfinite(a.scale)) return "scale must be finite";
+  return nullptr;
+}
+
 // What every row operator's arrays have to satisfy: sound inputs and outputs, and no output that
 // shares an element with another array, but for the pairs in `alias` (equal arrays).
 const char *arrays_fault(const Rows *in, int n_in, const Rows *out, int n_out,
@@ -258,6 +268,60 @@ bridger_status bridger_matmul_q8(const int8_t *a, int64_t lda, const float *a_sc
                                     n_features, out, ldo},
                                    dtype, stream);
   });
+}
+
+bridger_status bridger_embed(const int32_t *ids, int64_t ldi, const int64_t *offsets,
+                             const void *table, int64_t ldt, int32_t dtype, int64_t n_rows,
+                             int32_t n_slots, int32_t n_entries, int32_t n_features, float scale,
+                             void *out, int64_t ldo, void *stream) {
+  clear_error();
+  const EmbedArgs a = {ids,        ldi,   offsets, table, ldt,     n_rows, n_slots, n_entries,
+                       n_features, scale, out,     ldo,   nullptr, 1,      1,       0};
+  if (const char *f = embed_fault(a, dtype)) return invalid(f);
+  if (n_rows == 0) return BRIDGER_OK;
+  if (!ids || !table || !out) return invalid("null ids, table or output");
+  const int size = bytes_of(dtype);
+  const Rows in[] = {{ids, n_rows, n_slots, ldi, 4},
+                     {offsets, 1, (int64_t)n_slots + 1, (int64_t)n_slots + 1, 8},
+                     {table, n_entries, n_features, ldt, size}};
+  const Rows o[] = {{out, n_rows, n_features, ldo, size}};
+  if (const char *f = arrays_fault(in, 3, o, 1, nullptr)) return invalid(f);
+  if (bridger_status s = device_ready()) return s;
+  return launched([&] { return launch_embed(a, dtype, stream); });
+}
+
+int64_t bridger_embed_backward_workspace(int64_t n_rows, int32_t n_slots, int32_t n_entries,
+                                         int32_t n_features) {
+  const EmbedArgs a = {nullptr, 0,          nullptr, nullptr, 0, n_rows, n_slots, n_entries,
+                       n_features, 1.0f, nullptr, 0,       nullptr, 1, 1,       0};
+  if (embed_fault(a, BRIDGER_F32) || n_rows > INT32_MAX / (int64_t)n_slots) return 0;
+  return embed_backward_bytes(n_rows, n_slots, n_entries, n_features);
+}
+
+bridger_status bridger_embed_backward(const int32_t *ids, int64_t ldi, const int64_t *offsets,
+                                      const void *grad, int64_t ldg, int32_t dtype, int64_t n_rows,
+                                      int32_t n_slots, int32_t n_entries, int32_t n_features,
+                                      float scale, void *grad_table, int64_t ldt, void *workspace,
+                                      int64_t workspace_bytes, void *stream) {
+  clear_error();
+  const EmbedArgs a = {ids,        ldi,   offsets,    grad, ldg,       n_rows, n_slots, n_entries,
+                       n_features, scale, grad_table, ldt,  workspace, 1,      1,       0};
+  if (const char *f = embed_fault(a, dtype)) return invalid(f);
+  if (n_rows > INT32_MAX / (int64_t)n_slots)
+    return report_error(BRIDGER_ERR_UNSUPPORTED, "more than 2^31 - 1 slots");
+  if ((n_rows && (!ids || !grad)) || !grad_table || !workspace)
+    return invalid("null ids, gradient, table's gradient or workspace");
+  if ((uintptr_t)workspace % 16) return invalid("the workspace is not aligned to 16 bytes");
+  const int64_t bytes = embed_backward_bytes(n_rows, n_slots, n_entries, n_features);
+  if (workspace_bytes < bytes) return invalid("the workspace is too small");
+  const int size = bytes_of(dtype);
+  const Rows in[] = {{n_rows ? ids : nullptr, n_rows, n_slots, ldi, 4},
+                     {n_rows ? offsets : nullptr, 1, (int64_t)n_slots + 1, (int64_t)n_slots + 1, 8},
+                     {n_rows ? grad : nullptr, n_rows, n_features, ldg, size}};
+  const Rows o[] = {{grad_table, n_entries, n_features, ldt, size}, {workspace, 1, bytes, bytes, 1}};
+  if (const char *f = arrays_fault(in, 3, o, 2, nullptr)) return invalid(f);
+  if (bridger_status s = device_ready()) return s;
+  return launched([&] { return launch_embed_backward(a, dtype, stream); });
 }
 
 }  // extern "C"

@@ -74,10 +74,34 @@ struct MatmulArgs {
   int64_t ldo;
 };
 
+struct EmbedArgs {
+  const int32_t *ids;
+  int64_t ldi;
+  const int64_t *offsets;  // null: every slot reads the whole table
+  const void *table;       // backward: the output's gradient
+  int64_t ldt;
+  int64_t n_rows;
+  int32_t n_slots;
+  int32_t n_entries;
+  int32_t n_features;
+  float scale;
+  void *out;  // backward: the table's gradient
+  int64_t ldo;
+  void *workspace;  // backward
+  int32_t tiles;    // parts of a row's features, one a workgroup
+  int32_t parts;    // groups of lanes that share a row's slots
+  int64_t first;    // the launch's first workgroup
+};
+
 // Each returns a hipError_t as int.  Sizes are positive and every argument checked.
 int launch_top_k(const TopKArgs &a, int32_t dtype, void *stream);
 int launch_distill(const DistillArgs &a, int32_t dtype, bool backward, void *stream);
 int launch_rmsnorm_q8(const RmsnormArgs &a, int32_t dtype, void *stream);
 int launch_matmul_q8(const MatmulArgs &a, int32_t dtype, void *stream);
+int launch_embed(const EmbedArgs &a, int32_t dtype, void *stream);
+int launch_embed_backward(const EmbedArgs &a, int32_t dtype, void *stream);
+// Bytes of workspace; n_rows * n_slots fits 31 bits.
+int64_t embed_backward_bytes(int64_t n_rows, int32_t n_slots, int32_t n_entries,
+                             int32_t n_features);
 
 }  // namespace bridger

@@ -281,4 +281,16 @@ int launch_each_row(void (*k)(Args), int threads, const Args &args, void *stream
   return launch_over(k, threads, 1, args, stream);
 }
 
+// Workgroups [0, blocks), as several launches where a dispatch does not hold them.
+template <typename Args>
+int launch_blocks(void (*k)(Args), int64_t blocks, int threads, Args args, void *stream) {
+  constexpr int64_t step = int64_t(1) << 21;
+  for (args.first = 0; args.first < blocks; args.first += step) {
+    const int64_t n = blocks - args.first < step ? blocks - args.first : step;
+    const int err = launch(k, n, threads, 0, args, stream);
+    if (err) return err;
+  }
+  return 0;
+}
+
 }  // namespace bridger
