@@ -508,6 +508,69 @@ bridger_status bridger_embed_backward(const int32_t *ids, int64_t ldi, const int
 int64_t bridger_embed_backward_workspace(int64_t n_rows, int32_t n_slots, int32_t n_entries,
                                          int32_t n_features);
 
+/*
+ * Dropout with numbers from a counter (Table 4's dropout), and a residual added after:
+ *     out = kept ? x / (1 - p) : 0  (+ residual).
+ * Element (r, c) is kept when its random number of 32 bits is at least p 2^32 (rounded to nearest
+ * even).  The numbers are those of Philox4x32-10 with the key {seed[0] mod 2^32, seed[0] / 2^32}
+ * and the counter {c / 8, r, seed[1] mod 2^32, 2 layer + l}: of the four words, taken as eight halves
+ * (the lower half first), half c % 8 is the number's upper half for l = 0 and its lower half for l =
+ * 1.  So the same seed, layer and place give the same choice, and the gradient of x is this operator
+ * of the output's gradient.
+ *   x         [n_rows, n_features] of dtype, rows ldx apart; 1 <= n_features < 2^31
+ *   residual  as x, rows ldr apart, or NULL
+ *   p         between 0 and 1 (1: every element is dropped)
+ *   seed      int64 [2] on the device: a seed, and the number of the training step or the like
+ *   layer     0 <= layer < 2^31: another one for every use of the same seed
+ *   out       as x, rows ldo apart; may be x or residual itself (with the same distance of rows)
+ */
+bridger_status bridger_dropout(const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                               int32_t dtype, int64_t n_rows, int32_t n_features, double p,
+                               const int64_t *seed, int32_t layer, void *out, int64_t ldo,
+                               void *stream);
+
+/*
+ * Layer norm, with a residual added first:
+ *     t = x + residual rounded to dtype,
+ *     out_j = (t_j - mean(t)) / sqrt(mean((t - mean(t))^2) + eps) * weight_j + bias_j.
+ * A NaN or an infinity in a row makes the row NaN, and so does eps = 0 with a row of equal elements.
+ *   x         [n_rows, n_features] of dtype, rows ldx apart; 1 <= n_features < 2^31
+ *   residual  as x, rows ldr apart, or NULL (t = x)
+ *   weight, bias  [n_features] of dtype, or NULL (ones, zeros);  eps  finite, >= 0
+ *   total     receives t, of dtype, rows ldt apart, or NULL; may be x or residual itself (with the
+ *             same distance of rows)
+ *   out       [n_rows, n_features] of dtype, rows ldo apart
+ *   stats     float [n_rows, 3] for bridger_layer_norm_backward (the mean, what its rounding left,
+ *             the factor of t - mean), or NULL
+ */
+bridger_status bridger_layer_norm(const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                                  const void *weight, const void *bias, int32_t dtype,
+                                  int64_t n_rows, int32_t n_features, float eps, void *total,
+                                  int64_t ldt, void *out, int64_t ldo, float *stats, void *stream);
+
+/*
+ * Its gradients from the output's, with h = (t - mean) * factor and s = grad * weight:
+ *     dx = factor * (s - mean(s) - h mean(s h)) + grad_total   (of x and of the residual alike),
+ *     dweight_j = sum of grad_j h_j over the rows,  dbias_j = sum of grad_j.
+ *   grad        [n_rows, n_features] of dtype, rows ldg apart
+ *   t           what the norm was taken of (total, or x where there was no residual), rows ldt
+ *               apart, and the stats that bridger_layer_norm wrote for it
+ *   weight      as above;  grad_total  the gradient of total, rows lds apart, or NULL
+ *   dx          of dtype, rows ldd apart, or NULL
+ *   dweight, dbias  [n_features] of dtype, or NULL; written with n_rows == 0 too
+ *   workspace   bridger_layer_norm_backward_workspace bytes, aligned to 16, of this call alone until
+ *               it has run; NULL with dweight and dbias NULL
+ * At least one output is given.
+ */
+bridger_status bridger_layer_norm_backward(const void *grad, int64_t ldg, const void *t, int64_t ldt,
+                                           const float *stats, const void *weight,
+                                           const void *grad_total, int64_t lds, int32_t dtype,
+                                           int64_t n_rows, int32_t n_features, void *dx, int64_t ldd,
+                                           void *dweight, void *dbias, void *workspace,
+                                           int64_t workspace_bytes, void *stream);
+/* 0 for sizes that bridger_layer_norm_backward refuses, and for n_rows == 0. */
+int64_t bridger_layer_norm_backward_workspace(int64_t n_rows, int32_t n_features, int32_t dtype);
+
 /* Message for the calling thread's most recent failed call ("" if none).  The
  * paper states no error interface; this is the library's own, so that nothing
  * throws across the C ABI (thread-local storage, valid until the thread's next

@@ -434,7 +434,9 @@ class Forest:
 
 from . import layers, operators  # noqa: E402  (they use load_library and _check)
 from .layers import (  # noqa: E402,F401
-    bridger_embed, bridger_embed_backward, bridger_embed_backward_workspace, embed, embed_grad)
+    bridger_dropout, bridger_embed, bridger_embed_backward, bridger_embed_backward_workspace,
+    bridger_layer_norm, bridger_layer_norm_backward, bridger_layer_norm_backward_workspace, dropout,
+    embed, embed_grad, layer_norm, layer_norm_grad)
 from .operators import (  # noqa: E402,F401
     BRIDGER_BF16, BRIDGER_F16, BRIDGER_F32, BRIDGER_MATMUL_Q8_MAX_FEATURES, BRIDGER_MAX_TOP,
     bridger_distill, bridger_distill_backward, bridger_matmul_q8, bridger_rmsnorm_q8,

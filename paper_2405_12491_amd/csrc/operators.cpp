@@ -324,4 +324,103 @@ bridger_status bridger_embed_backward(const int32_t *ids, int64_t ldi, const int
   return launched([&] { return launch_embed_backward(a, dtype, stream); });
 }
 
+bridger_status bridger_dropout(const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                               int32_t dtype, int64_t n_rows, int32_t n_features, double p,
+                               const int64_t *seed, int32_t layer, void *out, int64_t ldo,
+                               void *stream) {
+  clear_error();
+  if (const char *f = count_fault(n_rows, n_features)) return invalid(f);
+  const int size = bytes_of(dtype);
+  if (!size) return invalid("unknown dtype");
+  if (!(p >= 0.0 && p <= 1.0)) return invalid("p must lie between 0 and 1");
+  if (layer < 0) return invalid("layer < 0");
+  if (n_rows == 0) return BRIDGER_OK;
+  if (!x || !seed || !out) return invalid("null x, seed or output");
+  const Rows in[] = {{x, n_rows, n_features, ldx, size},
+                     {residual, n_rows, n_features, ldr, size},
+                     {seed, 1, 2, 2, 8}};
+  const Rows o[] = {{out, n_rows, n_features, ldo, size}};
+  if (const char *f = arrays_fault(in, 3, o, 1, [](int i, int) { return i < 2; })) return invalid(f);
+  if (bridger_status s = device_ready()) return s;
+  const uint64_t limit = (uint64_t)std::nearbyint(p * 4294967296.0);
+  const float scale = p < 1.0 ? (float)(1.0 / (1.0 - p)) : 0.0f;
+  return launched([&] {
+    return launch_dropout({x, ldx, residual, ldr, n_rows, n_features, limit, scale, seed,
+                           (uint32_t)layer, out, ldo, 1, 0},
+                          dtype, stream);
+  });
+}
+
+bridger_status bridger_layer_norm(const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                                  const void *weight, const void *bias, int32_t dtype,
+                                  int64_t n_rows, int32_t n_features, float eps, void *total,
+                                  int64_t ldt, void *out, int64_t ldo, float *stats, void *stream) {
+  clear_error();
+  if (const char *f = count_fault(n_rows, n_features)) return invalid(f);
+  const int size = bytes_of(dtype);
+  if (!size) return invalid("unknown dtype");
+  if (!(eps >= 0.0f) || std::isinf(eps)) return invalid("eps must be finite and >= 0");
+  if (n_rows == 0) return BRIDGER_OK;
+  if (!x || !out) return invalid("null x or output");
+  const Rows in[] = {{x, n_rows, n_features, ldx, size},
+                     {residual, n_rows, n_features, ldr, size},
+                     {weight, 1, n_features, n_features, size},
+                     {bias, 1, n_features, n_features, size}};
+  const Rows o[] = {{total, n_rows, n_features, ldt, size},
+                    {out, n_rows, n_features, ldo, size},
+                    {stats, n_rows, 3, 3, 4}};
+  if (const char *f = arrays_fault(in, 4, o, 3, [](int i, int q) { return i < 2 && q == 0; }))
+    return invalid(f);
+  if (bridger_status s = device_ready()) return s;
+  return launched([&] {
+    return launch_layer_norm({x, ldx, residual, ldr, weight, bias, n_rows, n_features, eps, total,
+                              ldt, out, ldo, stats, 0},
+                             dtype, stream);
+  });
+}
+
+int64_t bridger_layer_norm_backward_workspace(int64_t n_rows, int32_t n_features, int32_t dtype) {
+  const int size = bytes_of(dtype);
+  if (count_fault(n_rows, n_features) || !size) return 0;
+  return layer_norm_backward_bytes(n_rows, n_features, size);
+}
+
+bridger_status bridger_layer_norm_backward(const void *grad, int64_t ldg, const void *t, int64_t ldt,
+                                           const float *stats, const void *weight,
+                                           const void *grad_total, int64_t lds, int32_t dtype,
+                                           int64_t n_rows, int32_t n_features, void *dx, int64_t ldd,
+                                           void *dweight, void *dbias, void *workspace,
+                                           int64_t workspace_bytes, void *stream) {
+  clear_error();
+  if (const char *f = count_fault(n_rows, n_features)) return invalid(f);
+  const int size = bytes_of(dtype);
+  if (!size) return invalid("unknown dtype");
+  if (!dx && !dweight && !dbias) return invalid("no output");
+  const bool weights = dweight || dbias;
+  if (n_rows == 0 && !weights) return BRIDGER_OK;
+  if (n_rows && (!grad || !t || !stats)) return invalid("null gradient, t or stats");
+  const int64_t bytes = weights ? layer_norm_backward_bytes(n_rows, n_features, size) : 0;
+  if (bytes && !workspace) return invalid("null workspace");
+  if (bytes && (uintptr_t)workspace % 16) return invalid("the workspace is not aligned to 16 bytes");
+  if (workspace_bytes < bytes) return invalid("the workspace is too small");
+  const bool rows = n_rows > 0;
+  const Rows in[] = {{rows ? grad : nullptr, n_rows, n_features, ldg, size},
+                     {rows ? t : nullptr, n_rows, n_features, ldt, size},
+                     {rows ? stats : nullptr, n_rows, 3, 3, 4},
+                     {rows ? weight : nullptr, 1, n_features, n_features, size},
+                     {rows ? grad_total : nullptr, n_rows, n_features, lds, size}};
+  const Rows o[] = {{rows ? dx : nullptr, n_rows, n_features, ldd, size},
+                    {dweight, 1, n_features, n_features, size},
+                    {dbias, 1, n_features, n_features, size},
+                    {bytes ? workspace : nullptr, 1, bytes, bytes, 1}};
+  if (const char *f = arrays_fault(in, 5, o, 4, nullptr)) return invalid(f);
+  if (bridger_status s = device_ready()) return s;
+  return launched([&] {
+    return launch_layer_norm_backward(
+        {grad, ldg, t, ldt, stats, weight, grad_total, lds, n_rows, n_features, rows ? dx : nullptr,
+         ldd, dweight, dbias, weights ? (float *)workspace : nullptr, 0, 1, 0},
+        dtype, stream);
+  });
+}
+
 }  // extern "C"

@@ -93,6 +93,62 @@ struct EmbedArgs {
   int64_t first;    // the launch's first workgroup
 };
 
+struct DropoutArgs {
+  const void *x;
+  int64_t ldx;
+  const void *residual;  // null: none
+  int64_t ldr;
+  int64_t n_rows;
+  int32_t n_features;
+  uint64_t limit;  // random numbers of 32 bits from here on keep their element
+  float scale;     // of kept elements
+  const int64_t *seed;
+  uint32_t layer;
+  void *out;
+  int64_t ldo;
+  int32_t tiles;  // parts of a row, one a workgroup
+  int64_t first;  // the launch's first workgroup
+};
+
+struct LayerNormArgs {
+  const void *x;
+  int64_t ldx;
+  const void *residual;  // null: none
+  int64_t ldr;
+  const void *weight;  // null: ones
+  const void *bias;    // null: zeros
+  int64_t n_rows;
+  int32_t n_features;
+  float eps;
+  void *total;  // may be null
+  int64_t ldt;
+  void *out;
+  int64_t ldo;
+  float *stats;   // may be null
+  int64_t first;  // the launch's first row
+};
+
+struct LayerNormGradArgs {
+  const void *grad;
+  int64_t ldg;
+  const void *x;  // what the norm was taken of
+  int64_t ldx;
+  const float *stats;
+  const void *weight;      // null: ones
+  const void *grad_total;  // null: none
+  int64_t lds;
+  int64_t n_rows;
+  int32_t n_features;
+  void *dx;  // may be null
+  int64_t ldd;
+  void *dweight;   // may be null
+  void *dbias;     // may be null
+  float *partial;  // null: neither of both is wanted
+  int32_t parts;   // workgroups whose sums `partial` holds
+  int32_t tiles;   // parts of a long row, one a workgroup
+  int64_t first;   // the launch's first row or workgroup
+};
+
 // Each returns a hipError_t as int.  Sizes are positive and every argument checked.
 int launch_top_k(const TopKArgs &a, int32_t dtype, void *stream);
 int launch_distill(const DistillArgs &a, int32_t dtype, bool backward, void *stream);
@@ -103,5 +159,10 @@ int launch_embed_backward(const EmbedArgs &a, int32_t dtype, void *stream);
 // Bytes of workspace; n_rows * n_slots fits 31 bits.
 int64_t embed_backward_bytes(int64_t n_rows, int32_t n_slots, int32_t n_entries,
                              int32_t n_features);
+
+int launch_dropout(const DropoutArgs &a, int32_t dtype, void *stream);
+int launch_layer_norm(const LayerNormArgs &a, int32_t dtype, void *stream);
+int launch_layer_norm_backward(const LayerNormGradArgs &a, int32_t dtype, void *stream);
+int64_t layer_norm_backward_bytes(int64_t n_rows, int32_t n_features, int element_size);
 
 }  // namespace bridger

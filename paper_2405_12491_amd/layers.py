@@ -1,14 +1,15 @@
 """Layers that a student is trained with, on torch CUDA tensors.
 
-``bridger_embed`` and ``bridger_embed_backward`` marshal device pointers to the C entry points of the
-same names (include/bridger.h states formulas, types and limits).  ``embed`` and ``embed_grad`` follow
-the rules of the row operators (operators.py): rows that are contiguous, at any distance, on any
-device, launched on torch's current stream of that device, no CPU fallback.
+The functions named ``bridger_*`` marshal device pointers to the C entry points of the same names
+(include/bridger.h states formulas, types and limits).  ``embed``, ``dropout``, ``layer_norm`` and the
+gradients ``embed_grad`` and ``layer_norm_grad`` follow the rules of the row operators (operators.py):
+2-D tensors whose rows are contiguous, at any distance, on any device, launched on torch's current
+stream of that device, no CPU fallback.
 
 A call whose inputs need a gradient is differentiated (once).  A stream that is being captured
 refuses such calls: autograd keeps nodes on the streams they were made on, and a captured backward
-pass that meets one of an eager graph ends the process.  There call the forward and the gradient's
-function, ``embed_grad``, one after the other under ``torch.no_grad()``.
+pass that meets one of an eager graph ends the process.  There call the layer and then its gradient's
+function (dropout's is dropout of the gradient) under ``torch.no_grad()``.
 """
 from __future__ import annotations
 
@@ -24,6 +25,16 @@ _ARGTYPES = {
     "bridger_embed": [_P, _I64, _P, _P, _I64, _I32, _I64, _I32, _I32, _I32, _F, _P, _I64, _P],
     "bridger_embed_backward": [_P, _I64, _P, _P, _I64, _I32, _I64, _I32, _I32, _I32, _F, _P, _I64,
                                _P, _I64, _P],
+    "bridger_dropout": [_P, _I64, _P, _I64, _I32, _I64, _I32, ctypes.c_double, _P, _I32, _P, _I64,
+                        _P],
+    "bridger_layer_norm": [_P, _I64, _P, _I64, _P, _P, _I32, _I64, _I32, _F, _P, _I64, _P, _I64, _P,
+                           _P],
+    "bridger_layer_norm_backward": [_P, _I64, _P, _I64, _P, _P, _P, _I64, _I32, _I64, _I32, _P, _I64,
+                                    _P, _P, _P, _I64, _P],
+}
+_SIZES = {
+    "bridger_embed_backward_workspace": [_I64, _I32, _I32, _I32],
+    "bridger_layer_norm_backward_workspace": [_I64, _I32, _I32],
 }
 
 
@@ -32,8 +43,9 @@ def declare(lib):
     for name, types in _ARGTYPES.items():
         fn = getattr(lib, name)
         fn.argtypes, fn.restype = types, ctypes.c_int
-    fn = lib.bridger_embed_backward_workspace
-    fn.argtypes, fn.restype = [_I64, _I32, _I32, _I32], _I64
+    for name, types in _SIZES.items():
+        fn = getattr(lib, name)
+        fn.argtypes, fn.restype = types, _I64
 
 
 # ------------------------------------------------------------- raw entry points
@@ -55,6 +67,33 @@ def bridger_embed_backward(ids_ptr, ldi, offsets_ptr, grad_ptr, ldg, dtype, n_ro
         ids_ptr, ldi, offsets_ptr, grad_ptr, ldg, dtype, n_rows, n_slots, n_entries, n_features,
         scale, grad_table_ptr, ldt, workspace_ptr, workspace_bytes, stream),
         "bridger_embed_backward")
+
+
+def bridger_dropout(x_ptr, ldx, residual_ptr, ldr, dtype, n_rows, n_features, p, seed_ptr, layer,
+                    out_ptr, ldo, stream=0):
+    _B._check(_B.load_library().bridger_dropout(
+        x_ptr, ldx, residual_ptr, ldr, dtype, n_rows, n_features, p, seed_ptr, layer, out_ptr, ldo,
+        stream), "bridger_dropout")
+
+
+def bridger_layer_norm(x_ptr, ldx, residual_ptr, ldr, weight_ptr, bias_ptr, dtype, n_rows,
+                       n_features, eps, total_ptr, ldt, out_ptr, ldo, stats_ptr, stream=0):
+    _B._check(_B.load_library().bridger_layer_norm(
+        x_ptr, ldx, residual_ptr, ldr, weight_ptr, bias_ptr, dtype, n_rows, n_features, eps,
+        total_ptr, ldt, out_ptr, ldo, stats_ptr, stream), "bridger_layer_norm")
+
+
+def bridger_layer_norm_backward_workspace(n_rows, n_features, dtype) -> int:
+    return _B.load_library().bridger_layer_norm_backward_workspace(n_rows, n_features, dtype)
+
+
+def bridger_layer_norm_backward(grad_ptr, ldg, t_ptr, ldt, stats_ptr, weight_ptr, grad_total_ptr,
+                                lds, dtype, n_rows, n_features, dx_ptr, ldd, dweight_ptr, dbias_ptr,
+                                workspace_ptr, workspace_bytes, stream=0):
+    _B._check(_B.load_library().bridger_layer_norm_backward(
+        grad_ptr, ldg, t_ptr, ldt, stats_ptr, weight_ptr, grad_total_ptr, lds, dtype, n_rows,
+        n_features, dx_ptr, ldd, dweight_ptr, dbias_ptr, workspace_ptr, workspace_bytes, stream),
+        "bridger_layer_norm_backward")
 
 
 # ------------------------------------------------------------------------- autograd
@@ -181,3 +220,177 @@ def embed_grad(ids, grad, n_entries: int, scale: float = 1.0, offsets=None, out=
     if _O._torch is None:
         _O._setup()
     return _embed_grad(ids, grad, int(n_entries), float(scale), offsets, out)
+
+
+# -------------------------------------------------------------------------- dropout
+def _dropout(x, p, seed, residual, layer, out):
+    torch = _O._torch
+    n, w, ldx = _rows(x, "x", None, None, None, None)
+    dev, dtype = x.get_device(), x.dtype
+    code = _code(dtype)
+    _vector(seed, "seed", 2, torch.int64, dev)
+    ldr = 0 if residual is None else _rows(residual, "residual", w, n, dtype, dev)[2]
+    if not 0 <= layer <= _MOST:
+        raise ValueError("layer must lie between 0 and 2^31 - 1")
+    given = out
+    if out is None:
+        out, ldo = x.new_empty((n, w)), w
+    else:
+        ldo = _rows(out, "out", w, n, dtype, dev)[2]
+        _writable(out, "out")
+    _call("bridger_dropout", x, x.data_ptr(), ldx, _ptr(residual), ldr, code, n, w, p,
+          seed.data_ptr(), layer, out.data_ptr(), ldo)
+    if given is not None:
+        _written(given)
+    return out
+
+
+def _make_dropout(torch):
+    class Dropout(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, residual, seed, p, layer):
+            ctx.save_for_backward(seed)
+            ctx.p, ctx.layer = p, layer
+            return _dropout(x, p, seed, residual, layer, None)
+
+        def backward(ctx, grad):
+            seed, = ctx.saved_tensors
+            dx = None
+            if ctx.needs_input_grad[0]:
+                dx = _dropout(grad.contiguous(), ctx.p, seed, None, ctx.layer, None)
+            return dx, grad if ctx.needs_input_grad[1] else None, None, None, None
+        backward = _once(torch, backward)
+    return Dropout
+
+
+def dropout(x, p: float, seed, residual=None, layer: int = 0, out=None):
+    """x [n, w] with a share ``p`` of its elements zero and the others times 1 / (1 - p), plus
+    ``residual``.  ``seed`` (int64 [2] on x's device) holds a seed and the number of the step, and
+    ``layer`` tells uses of one seed apart: the same three give the same choice, wherever the call
+    runs, so a captured step draws anew when its program adds 1 to seed[1] (after the backward pass,
+    which needs what the forward pass had).  Differentiable in x and the residual; without autograd
+    the gradient of x is ``dropout(grad, p, seed, layer=layer)``.  ``out`` may be x or residual."""
+    if _O._torch is None:
+        _O._setup()
+    if _tracked("dropout", "dropout of the gradient under no_grad()", x, residual):
+        _untracked_output(out, "dropout")
+        return _function("dropout", _make_dropout).apply(x, residual, seed, float(p), int(layer))
+    return _dropout(x, float(p), seed, residual, int(layer), out)
+
+
+# ----------------------------------------------------------------------- layer_norm
+def _layer_norm(x, weight, bias, residual, eps, out, total, stats):
+    n, w, ldx = _rows(x, "x", None, None, None, None)
+    dev, dtype = x.get_device(), x.dtype
+    code = _code(dtype)
+    ldr = 0 if residual is None else _rows(residual, "residual", w, n, dtype, dev)[2]
+    if weight is not None:
+        _vector(weight, "weight", w, dtype, dev)
+    if bias is not None:
+        _vector(bias, "bias", w, dtype, dev)
+    given = None if out is None and total is None and stats is None else (out, total, stats)
+    if out is None:
+        out, ldo = x.new_empty((n, w)), w
+    else:
+        ldo = _rows(out, "out", w, n, dtype, dev)[2]
+        _writable(out, "out")
+    ldt = w
+    if total is not None:
+        ldt = _rows(total, "total", w, n, dtype, dev)[2]
+        _writable(total, "total")
+    elif residual is not None:
+        total = x.new_empty((n, w))
+    if stats is not None:
+        _O._dense(stats, "stats", n, 3, _O._torch.float32, dev)
+        _writable(stats, "stats")
+    _call("bridger_layer_norm", x, x.data_ptr(), ldx, _ptr(residual), ldr, _ptr(weight), _ptr(bias),
+          code, n, w, eps, _ptr(total), ldt, out.data_ptr(), ldo, _ptr(stats))
+    if given:
+        _written(*given)
+    return out, total
+
+
+def _layer_norm_grad(grad, t, stats, weight, grad_total, out, want_rows, want_weight, want_bias):
+    n, w, ldg = _rows(grad, "grad", None, None, None, None)
+    dev, dtype = grad.get_device(), grad.dtype
+    code = _code(dtype)
+    ldt = _rows(t, "t", w, n, dtype, dev)[2]
+    _O._dense(stats, "stats", n, 3, _O._torch.float32, dev)
+    if weight is not None:
+        _vector(weight, "weight", w, dtype, dev)
+    lds = 0 if grad_total is None else _rows(grad_total, "grad_total", w, n, dtype, dev)[2]
+    given, dx, ldd = out, None, w
+    if out is not None:
+        dx, ldd = out, _rows(out, "out", w, n, dtype, dev)[2]
+        _writable(out, "out")
+    elif want_rows:
+        dx = grad.new_empty((n, w))
+    dweight = grad.new_empty((w,)) if want_weight else None
+    dbias = grad.new_empty((w,)) if want_bias else None
+    bytes_, workspace = 0, None
+    if want_weight or want_bias:
+        bytes_ = _B._lib.bridger_layer_norm_backward_workspace(n, w, code)
+        workspace = grad.new_empty(bytes_, dtype=_O._torch.uint8)
+    _call("bridger_layer_norm_backward", grad, grad.data_ptr(), ldg, t.data_ptr(), ldt,
+          stats.data_ptr(), _ptr(weight), _ptr(grad_total), lds, code, n, w, _ptr(dx), ldd,
+          _ptr(dweight), _ptr(dbias), _ptr(workspace), bytes_)
+    if given is not None:
+        _written(given)
+    return dx, dweight, dbias
+
+
+def _make_layer_norm(torch):
+    class LayerNorm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, weight, bias, residual, eps):
+            _rows(x, "x", None, None, None, None)
+            stats = x.new_empty((x.shape[0], 3), dtype=torch.float32)
+            out, total = _layer_norm(x, weight, bias, residual, eps, None, None, stats)
+            ctx.save_for_backward(x if total is None else total, weight, stats)
+            ctx.set_materialize_grads(False)
+            return out, total
+
+        def backward(ctx, grad, grad_total):
+            t, weight, stats = ctx.saved_tensors
+            rows = ctx.needs_input_grad[0] or ctx.needs_input_grad[3]
+            if grad is None:  # the sum alone was used
+                none = t.new_zeros(t.shape[1])
+                dx = t.new_zeros(t.shape) if grad_total is None else grad_total
+                dweight, dbias = none, none
+            else:
+                dx, dweight, dbias = _layer_norm_grad(
+                    grad.contiguous(), t, stats, weight,
+                    None if grad_total is None else grad_total.contiguous(), None, rows,
+                    ctx.needs_input_grad[1], ctx.needs_input_grad[2])
+            return (dx if ctx.needs_input_grad[0] else None,
+                    dweight if ctx.needs_input_grad[1] else None,
+                    dbias if ctx.needs_input_grad[2] else None,
+                    dx if ctx.needs_input_grad[3] else None, None)
+        backward = _once(torch, backward)
+    return LayerNorm
+
+
+def layer_norm(x, weight=None, bias=None, residual=None, eps: float = 1e-5, out=None, total=None,
+               stats=None):
+    """Layer norm of every row of x (+ residual, the sum rounded to x's type), times ``weight`` [w],
+    plus ``bias`` [w]: (norm [n, w], total), total being x + residual (None without a residual or a
+    ``total`` to write).  Differentiable in all four.  ``total`` may be x or residual itself;
+    ``stats`` (float32 [n, 3]) is written for layer_norm_grad."""
+    if _O._torch is None:
+        _O._setup()
+    if _tracked("layer_norm", "layer_norm and layer_norm_grad under no_grad()", x, weight, bias,
+                residual):
+        for t in (out, total, stats):
+            _untracked_output(t, "layer_norm")
+        return _function("layer_norm", _make_layer_norm).apply(x, weight, bias, residual, float(eps))
+    return _layer_norm(x, weight, bias, residual, float(eps), out, total, stats)
+
+
+def layer_norm_grad(grad, t, stats, weight=None, grad_total=None, out=None, weights: bool = True):
+    """The gradients of layer_norm from that of its output: (of x and the residual alike [n, w], of
+    the weight [w], of the bias [w]; the latter two None without ``weights``).  ``t`` is what the
+    norm was taken of (total, or x where there was no residual), ``stats`` what layer_norm wrote,
+    ``grad_total`` the gradient of total, which is added."""
+    if _O._torch is None:
+        _O._setup()
+    return _layer_norm_grad(grad, t, stats, weight, grad_total, out, True, weights, weights)

@@ -44,3 +44,98 @@ def embed_grad(ids, grad, n_entries, scale=1.0, offsets=None):
             np.add.at(count, at[ok, s], 1)
         tol = (count[:, None] + 1) * U * size * abs(scale)
         return out * scale, np.nan_to_num(tol, posinf=0)
+
+
+def random_words(c0, c1, c2, c3, k0, k1):
+    """Philox4x32-10 on uint64 arrays that hold words of 32 bits."""
+    low = np.uint64(0xFFFFFFFF)
+    c = [np.asarray(v, np.uint64) for v in (c0, c1, c2, c3)]
+    k0, k1 = int(k0), int(k1)
+    for _ in range(10):
+        a, b = c[0] * np.uint64(0xD2511F53), c[2] * np.uint64(0xCD9E8D57)
+        s = np.uint64(32)
+        c = [(b >> s) ^ c[1] ^ np.uint64(k0), b & low, (a >> s) ^ c[3] ^ np.uint64(k1), a & low]
+        k0, k1 = (k0 + 0x9E3779B9) % 2 ** 32, (k1 + 0xBB67AE85) % 2 ** 32
+    return c
+
+
+def kept(n, w, p, seed, layer):
+    """Which elements dropout keeps, bool [n, w]."""
+    s0, step = (int(v) % 2 ** 64 for v in seed)
+    unit, row = np.meshgrid(np.arange((w + 7) // 8, dtype=np.uint64), np.arange(n, dtype=np.uint64))
+    half = []
+    for low in (0, 1):
+        words = random_words(unit, row, np.full_like(unit, step % 2 ** 32),
+                             np.full_like(unit, 2 * layer + low), s0 % 2 ** 32, s0 >> 32)
+        parts = [h for v in words for h in (v & np.uint64(0xFFFF), v >> np.uint64(16))]
+        half.append(np.stack(parts, 2).reshape(n, -1)[:, :w])
+    number = half[0] << np.uint64(16) | half[1]
+    return number.astype(np.float64) >= np.rint(p * 2.0 ** 32)
+
+
+def dropout(x, p, seed, residual=None, layer=0):
+    x = np64(x)
+    up = 1 / (1 - p) if p < 1 else 0.0
+    with np.errstate(all="ignore"):
+        out = np.where(kept(*x.shape, p, seed.tolist(), layer), x * up, 0.0)
+        tol = 2 * U * np.abs(out)                      # the factor, and the product
+        if residual is not None:
+            out = out + np64(residual)
+            tol = tol + U * np.abs(out)
+    return out, np.where(np.isfinite(tol), tol, 0.0)
+
+
+# A lane adds at most 32 values in a row, a row's lanes in at most 10 steps more.
+ADDS = 42
+
+
+def _norm(t, eps):
+    """h, 1 / std, and how far h may be off."""
+    n = t.shape[1]
+    mean = t.mean(1, keepdims=True)
+    c = t - mean
+    r = 1 / np.sqrt((c * c).sum(1, keepdims=True) / n + eps)
+    h = c * r
+    # the mean is off by the sum of t - m (each off by U) and its quotient; 1 / std by half the sum
+    # of squares' error, the root and the quotient; the differences and their product by 4 U
+    er = (ADDS + 4) / 2 * U + 3 * U
+    eh = np.abs(h) * (er + 4 * U) + (ADDS + 3) * U * np.abs(c).mean(1, keepdims=True) * r
+    return h, r, eh, er
+
+
+def layer_norm(t, weight=None, bias=None, eps=1e-5):
+    """The norm of t (the sum, already rounded) and its tolerance."""
+    with np.errstate(all="ignore"):
+        h, _, eh, _ = _norm(np64(t), eps)
+        w = 1.0 if weight is None else np64(weight)
+        y, tol = h * w, eh * np.abs(w) + U * np.abs(h * w)
+        if bias is not None:
+            y = y + np64(bias)
+            tol = tol + U * np.abs(y)
+    return y, np.where(np.isfinite(tol), tol, 0.0)
+
+
+def layer_norm_grad(grad, t, weight=None, grad_total=None, eps=1e-5):
+    """((dx, dweight, dbias), their tolerances)."""
+    with np.errstate(all="ignore"):
+        g = np64(grad)
+        h, r, eh, er = _norm(np64(t), eps)
+        s = g if weight is None else g * np64(weight)
+        mean, along = s.mean(1, keepdims=True), (s * h).mean(1, keepdims=True)
+        size = np.abs(s).mean(1, keepdims=True)
+        dx = r * (s - mean - h * along)
+        e_mean = (ADDS + 3) * U * size
+        e_along = (np.abs(s) * eh).mean(1, keepdims=True) + \
+            (ADDS + 4) * U * np.abs(s * h).mean(1, keepdims=True)
+        terms = np.abs(s) + np.abs(mean) + np.abs(h * along)
+        tol = r * (e_mean + np.abs(h) * e_along + np.abs(along) * eh + 4 * U * terms) \
+            + (er + 2 * U) * np.abs(dx)
+        if grad_total is not None:
+            dx = dx + np64(grad_total)
+            tol = tol + U * np.abs(dx)
+        # a workgroup adds its share of the rows, then up to 256 groups of lanes; the rest in double
+        adds = len(g) / 512 + 300
+        dw, db = (g * h).sum(0), g.sum(0)
+        tw = (np.abs(g) * eh).sum(0) + (adds + 2) * U * np.abs(g * h).sum(0)
+        tb = (adds + 2) * U * np.abs(g).sum(0)
+    return (dx, dw, db), [np.where(np.isfinite(v), v, 0.0) for v in (tol, tw, tb)]

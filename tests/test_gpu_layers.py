@@ -245,3 +245,298 @@ def test_embed_gradient_against_differences():
         diff = ((np64(B.embed(ids, moved, 0.7)) - base) * np64(up)).sum()
         # 80 values of out, each off by 3 roundings of at most 8
         assert abs(diff - grad[e, j]) <= 80 * 3 * R.U * 8 * np.abs(np64(up)).max()
+
+
+# --------------------------------------------------------------------------- dropout
+def _seed(a=1234567890123, b=7):
+    return torch.tensor([a, b], device="cuda")
+
+
+def _check_dropout(x, p, seed, residual=None, layer=0, what=""):
+    ref, tol = L.dropout(x, p, seed, residual, layer)
+    out = B.dropout(x, p, seed, residual, layer)
+    R.assert_near(out, ref, tol, x.dtype, f"{what}: dropout")
+    return out
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids_of)
+@pytest.mark.parametrize("width", [1, 2, 3, 4, 5, 7, 8, 9, 15, 16, 17, 28, 33, 64, 100, 347, 512, 515, 2047, 4099, 9001])
+def test_dropout(width, dtype):
+    for n, p, layer in ((1, 0.5, 0), (13, 0.1, 5), (70, 0.3, 2 ** 31 - 1)):
+        x, res = _normal(width, n, width, dtype=dtype), _normal(7, n, width, dtype=dtype)
+        _check_dropout(x, p, _seed(), None, layer, f"{n}")
+        _check_dropout(x, p, _seed(-3, -1), res, layer, f"{n} residual")
+
+
+def test_dropout_numbers():
+    """Every bit of the 32 counts: the choice of two million elements, whose numbers' upper halves
+    meet the limit's some thirty times."""
+    x = torch.ones(500, 4001, device="cuda")
+    for p in (0.1, 0.9, 0.25, 2.0 ** -32, 1 - 2.0 ** -32, 0.3 + 1e-7):
+        out = B.dropout(x, p, _seed(), layer=1)
+        assert np.array_equal(out.cpu().numpy() != 0, L.kept(500, 4001, p, _seed().tolist(), 1)), p
+    assert torch.equal(B.dropout(x, 0.0, _seed()), x)
+    assert bool((B.dropout(x, 1.0, _seed()) == 0).all())
+    share = float((B.dropout(x, 0.3, _seed()) == 0).float().mean())
+    # 2 million independent choices: a standard deviation of 3.3e-4
+    assert abs(share - 0.3) < 6 * 3.3e-4
+    a = B.dropout(x, 0.5, _seed(1, 2)) != 0
+    for other in (B.dropout(x, 0.5, _seed(1, 3)), B.dropout(x, 0.5, _seed(2, 2)),
+                  B.dropout(x, 0.5, _seed(1, 2), layer=1), B.dropout(x, 0.5, _seed(1 + 2 ** 32, 2))):
+        assert abs(float((a == (other != 0)).float().mean()) - 0.5) < 6 * 3.6e-4
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids_of)
+@pytest.mark.parametrize("width,gap,lead", [(1, 1, 1), (5, 3, 1), (64, 7, 3), (515, 1, 0), (5003, 2, 5)])
+def test_dropout_strided_and_in_place(width, gap, lead, dtype):
+    x, res = _normal(1, 19, width, dtype=dtype), _normal(2, 19, width, dtype=dtype)
+    want = B.dropout(x, 0.4, _seed(), res)
+    _, sx = _strided(x, gap, lead, fill=nan)
+    _, sres = _strided(res, gap + 1, lead, fill=nan)
+    buf, out = _strided(torch.zeros_like(x), gap, lead, fill=5.0)
+    assert B.dropout(sx, 0.4, _seed(), sres, out=out) is out
+    assert _same_bits(out, want) and _untouched(buf, out, 5.0)
+    for which in (0, 1):
+        bufs = [_strided(t, gap, lead, fill=5.0) for t in (x, res)]
+        out = bufs[which][1]
+        B.dropout(bufs[0][1], 0.4, _seed(), bufs[1][1], out=out)
+        assert _same_bits(out, want) and _untouched(bufs[which][0], out, 5.0)
+
+
+def test_dropout_broken_elements():
+    """A dropped element is zero, whatever it was."""
+    x = torch.full((40, 50), nan, device="cuda")
+    x[::2] = inf
+    out = B.dropout(x, 0.5, _seed())
+    keep = torch.from_numpy(L.kept(40, 50, 0.5, _seed().tolist(), 0)).cuda()
+    assert bool((out[~keep] == 0).all()) and not bool(torch.isfinite(out[keep]).any())
+    assert bool((B.dropout(x, 1.0, _seed()) == 0).all())
+    assert B.dropout(torch.empty(0, 5, device="cuda"), 0.5, _seed()).shape == (0, 5)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids_of)
+def test_dropout_in_autograd(dtype):
+    x = _normal(1, 30, 37, dtype=dtype).requires_grad_()
+    res = _normal(2, 30, 37, dtype=dtype).requires_grad_()
+    up = _normal(3, 30, 37, dtype=dtype)
+    seed = _seed()
+    out = B.dropout(x, 0.3, seed, res, layer=4)
+    assert _same_bits(out.detach(), B.dropout(x.detach(), 0.3, seed, res.detach(), 4))
+    dx, dres = torch.autograd.grad(out, (x, res), up)
+    assert _same_bits(dx, B.dropout(up, 0.3, seed, layer=4)) and torch.equal(dres, up)
+    R.assert_near(dx, *L.dropout(up, 0.3, seed, None, 4), dtype)
+    only = B.dropout(x.detach(), 0.3, seed, res)
+    only.sum().backward()
+    assert torch.equal(res.grad, torch.ones_like(up)) and x.grad is None
+    out = B.dropout(x, 0.3, seed)
+    seed[1] += 1                                   # the next step's numbers before the gradient
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.sum().backward()
+
+
+# ------------------------------------------------------------------------ layer_norm
+LN_WIDTHS = [1, 2, 3, 4, 7, 8, 9, 16, 28, 31, 32, 33, 63, 64, 65, 100, 128, 255, 257, 512, 513, 784, 1023, 1025,
+             2047, 2049, 4096, 5001, 8192, 8195, 16384, 16389, 32768, 32771]
+
+
+def _norm_inputs(seed, n, w, dtype, shift=0.5):
+    return ((_normal(seed, n, w) * 2 + shift).to(dtype), _normal(seed + 1, n, w, dtype=dtype),
+            (1 + _normal(seed + 2, w) * 0.3).to(dtype), _normal(seed + 3, w, scale=0.2, dtype=dtype))
+
+
+def _check_norm(x, res, w, b, eps=1e-5, what=""):
+    """Forward, and the gradients through layer_norm_grad."""
+    n, f = x.shape
+    stats = torch.full((n, 3), nan, device="cuda")
+    y, total = B.layer_norm(x, w, b, residual=res, eps=eps, stats=stats)
+    t = x
+    if res is not None:
+        t = (x.float() + res.float()).to(x.dtype)
+        assert _same_bits(t, total), f"{what}: total"
+    else:
+        assert total is None
+    R.assert_near(y, *L.layer_norm(t, w, b, eps), x.dtype, f"{what}: norm")
+    g, gt = _normal(9, n, f, dtype=x.dtype), None if res is None else _normal(8, n, f, dtype=x.dtype)
+    got = B.layer_norm_grad(g, t, stats, w, grad_total=gt)
+    for name, v, ref, tol in zip(("dx", "dweight", "dbias"), got, *L.layer_norm_grad(g, t, w, gt, eps)):
+        R.assert_near(v, ref, tol, x.dtype, f"{what}: {name}")
+    return y, stats
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids_of)
+@pytest.mark.parametrize("width", LN_WIDTHS)
+def test_layer_norm(width, dtype):
+    for n in (1, 5, 70) if width < 1000 else (3,):
+        x, res, w, b = _norm_inputs(width, n, width, dtype)
+        _check_norm(x, None, w, b, what=f"{n}")
+        _check_norm(x, res, w, b, what=f"{n} residual")
+    _check_norm(x, None, None, None, what="plain")
+    _check_norm(x, res, w, None, what="no bias")
+    _check_norm(x, None, None, b, what="no weight")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids_of)
+@pytest.mark.parametrize("width", [40_000, 65_537, 100_003])
+def test_layer_norm_long_rows(width, dtype):
+    x, res, w, b = _norm_inputs(width, 6, width, dtype)
+    _check_norm(x, res, w, b)
+    _check_norm(x, None, None, None)
+
+
+@pytest.mark.parametrize("n", [2, 63, 64, 65, 1023, 1025, 5000, 40_001])
+@pytest.mark.parametrize("width", [3, 28, 130])
+def test_layer_norm_rows(n, width):
+    x, res, w, b = _norm_inputs(n, n, width, torch.float32)
+    _check_norm(x, res, w, b)
+
+
+@pytest.mark.parametrize("width", [28, 700, 5000, 30_000, 70_000])
+def test_layer_norm_far_from_zero(width):
+    """A mean that a float does not hold to the last bit of the row's spread."""
+    x = (_normal(1, 6, width).double() * 2.0 ** -8 + torch.tensor(
+        [1000.3, -1000.1, 1e5, 3.7, 0.0, 77.7], device="cuda")[:, None]).float()
+    _check_norm(x, None, None, None, eps=1e-9)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=ids_of)
+@pytest.mark.parametrize("width", [3, 5, 28, 700, 9000, 70_000])
+def test_layer_norm_extremes(width, dtype):
+    """Rows whose squares or sums leave float, and tiny ones."""
+    base = _normal(1, 7, width)
+    scale = torch.tensor([1e30, 1e-30, 1e19, 1e-19, 3e36, 1e15, 1.0], device="cuda")[:, None]
+    x = (base * scale).to(dtype)
+    for eps in (0.0, 1e-5):
+        y, _ = B.layer_norm(x, eps=eps)
+        R.assert_near(y, *L.layer_norm(x, None, None, eps), dtype, f"{eps}")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids_of)
+@pytest.mark.parametrize("width", [1, 3, 28, 700, 9000, 70_000])
+def test_layer_norm_equal_and_broken_rows(width, dtype):
+    x, res, w, b = _norm_inputs(1, 8, width, dtype)
+    x[0] = 0.0
+    x[1] = 3.0
+    x[2, 0] = nan
+    x[3, -1] = inf
+    x[4, 0] = -inf
+    y, stats = B.layer_norm(x, w, b)[0], None
+    R.assert_near(y, *L.layer_norm(x, w, b), dtype)
+    assert _same_bits(y[0], b) and _same_bits(y[1], b)
+    assert bool(torch.isnan(y[2:5]).all()) and bool(torch.isfinite(y[5:]).all())
+    assert bool(torch.isnan(B.layer_norm(x, w, b, eps=0.0)[0][:2]).all())
+    # a broken row's gradient stays in its row (and in the weight's)
+    stats = torch.empty(8, 3, device="cuda")
+    B.layer_norm(x, w, b, stats=stats)
+    g = _normal(5, 8, width, dtype=dtype)
+    dx, dw, db = B.layer_norm_grad(g, x, stats, w)
+    (rx, _, rb), (tx, _, tb) = L.layer_norm_grad(g, x, w)
+    R.assert_near(dx[5:], rx[5:], tx[5:], dtype)
+    assert bool(torch.isnan(dx[2:5]).all()) and bool(torch.isnan(dw).all())
+    R.assert_near(db, rb, tb, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids_of)
+@pytest.mark.parametrize("width,gap,lead", [(1, 1, 1), (5, 3, 1), (64, 7, 3), (515, 1, 0), (5003, 2, 5), (70_001, 3, 1)])
+def test_layer_norm_strided_and_in_place(width, gap, lead, dtype):
+    n = 11
+    x, res, w, b = _norm_inputs(1, n, width, dtype)
+    stats = torch.empty(n, 3, device="cuda")
+    y, total = B.layer_norm(x, w, b, residual=res, stats=stats)
+    _, sx = _strided(x, gap, lead, fill=nan)
+    _, sres = _strided(res, gap + 1, lead, fill=nan)
+    buf, out = _strided(torch.zeros_like(x), gap, lead, fill=5.0)
+    tbuf, tout = _strided(torch.zeros_like(x), gap, lead, fill=5.0)
+    got = B.layer_norm(sx, w, b, residual=sres, out=out, total=tout)
+    assert got[0] is out and got[1] is tout
+    assert _same_bits(out, y) and _same_bits(tout, total)
+    assert _untouched(buf, out, 5.0) and _untouched(tbuf, tout, 5.0)
+    for which in (0, 1):
+        bufs = [_strided(t, gap, lead, fill=5.0) for t in (x, res)]
+        got, _ = B.layer_norm(bufs[0][1], w, b, residual=bufs[1][1], total=bufs[which][1])
+        assert _same_bits(got, y) and _same_bits(bufs[which][1], total)
+        assert _untouched(bufs[which][0], bufs[which][1], 5.0)
+    alone = torch.zeros_like(x)
+    assert _same_bits(B.layer_norm(x, total=alone)[0], B.layer_norm(x)[0]) and _same_bits(alone, x)
+    g, gt = _normal(4, n, width, dtype=dtype), _normal(5, n, width, dtype=dtype)
+    want = B.layer_norm_grad(g, total, stats, w, grad_total=gt)
+    _, sg = _strided(g, gap, lead, fill=nan)
+    _, sgt = _strided(gt, gap + 2, lead, fill=nan)
+    buf, out = _strided(torch.zeros_like(x), gap, lead, fill=5.0)
+    got = B.layer_norm_grad(sg, tout, stats, w, grad_total=sgt, out=out)
+    assert got[0] is out and _untouched(buf, out, 5.0)
+    assert all(_same_bits(a, v) for a, v in zip(got, want))
+    dx, dw, db = B.layer_norm_grad(g, total, stats, w, grad_total=gt, weights=False)
+    assert _same_bits(dx, want[0]) and dw is None and db is None
+
+
+def test_layer_norm_no_rows():
+    x, w = torch.empty(0, 12, device="cuda"), torch.ones(12, device="cuda")
+    y, total = B.layer_norm(x, w, residual=x)
+    assert y.shape == total.shape == (0, 12)
+    dx, dw, db = B.layer_norm_grad(x, x, torch.empty(0, 3, device="cuda"), w)
+    assert dx.shape == (0, 12) and bool((dw == 0).all()) and bool((db == 0).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids_of)
+def test_layer_norm_in_autograd(dtype):
+    x, res, w, b = (t.requires_grad_() for t in _norm_inputs(1, 30, 37, dtype))
+    g, gt = _normal(3, 30, 37, dtype=dtype), _normal(4, 30, 37, dtype=dtype)
+    stats = torch.empty(30, 3, device="cuda")
+    with torch.no_grad():
+        y, total = B.layer_norm(x, w, b, residual=res, stats=stats)
+        want = B.layer_norm_grad(g, total, stats, w, grad_total=gt)
+    out = B.layer_norm(x, w, b, residual=res)
+    assert _same_bits(out[0].detach(), y) and _same_bits(out[1].detach(), total)
+    got = torch.autograd.grad(out, (x, res, w, b), (g, gt))
+    assert all(_same_bits(a, v) for a, v in zip(got, (want[0], want[0], *want[1:])))
+    # only one of the outputs, and only some of the leaves
+    y, _ = B.layer_norm(x, w, b, residual=res)
+    one = torch.autograd.grad(y, (x, w), g)
+    with torch.no_grad():
+        two = B.layer_norm_grad(g, total, stats, w)
+    assert _same_bits(one[0], two[0]) and _same_bits(one[1], two[1])
+    _, t = B.layer_norm(x, w, b, residual=res)
+    dx, dw, db = torch.autograd.grad(t, (x, w, b), gt)
+    assert torch.equal(dx, gt) and bool((dw == 0).all()) and bool((db == 0).all())
+    y, none = B.layer_norm(x.detach(), w)
+    assert none is None
+    dw, = torch.autograd.grad(y.sum(), w)
+    with torch.no_grad():
+        B.layer_norm(x, w, stats=stats)
+        assert _same_bits(dw, B.layer_norm_grad(torch.ones_like(g), x, stats, w)[1])
+    loss = (B.layer_norm(x, w, b, residual=res)[0].float() ** 2).sum()
+    loss.backward()
+    assert x.grad.data_ptr() != res.grad.data_ptr() and torch.equal(x.grad, res.grad)
+
+
+def test_layer_norm_gradient_against_differences():
+    """Central differences of the sum of norm * up in double, from the definition, at inputs moved by
+    2^-10: off by the third derivative (under 8 per unit here) times 2^-20 / 6."""
+    x, _, w, b = _norm_inputs(5, 4, 9, torch.float32)
+    up = _normal(6, 4, 9)
+    stats = torch.empty(4, 3, device="cuda")
+    y, _ = B.layer_norm(x, w, b, stats=stats)
+    dx, dw, db = (np64(v) for v in B.layer_norm_grad(up, x, stats, w))
+
+    def value(x, w, b):
+        c = x - x.mean(1, keepdims=True)
+        return ((c / np.sqrt((c * c).mean(1, keepdims=True) + 1e-5) * w + b) * np64(up)).sum()
+
+    at, step = [np64(x), np64(w), np64(b)], 2.0 ** -10
+    for k, grad in ((0, dx), (1, dw), (2, db)):
+        for place in np.ndindex(grad.shape):
+            hi, lo = [v.copy() for v in at], [v.copy() for v in at]
+            hi[k][place] += step
+            lo[k][place] -= step
+            diff = (value(*hi) - value(*lo)) / (2 * step)
+            assert abs(diff - grad[place]) <= 8 * 2.0 ** -20 / 6 * 40 + 1e-5, (k, place)
+
+
+@pytest.mark.parametrize("call", ["dropout", "layer_norm", "embed"])
+def test_layers_are_differentiated_once(call):
+    x = _normal(1, 6, 8).requires_grad_()
+    out = {"dropout": lambda: B.dropout(x, 0.5, _seed()), "layer_norm": lambda: B.layer_norm(x)[0],
+           "embed": lambda: B.embed(torch.zeros(3, dtype=torch.int32, device="cuda"), x)}[call]()
+    grad, = torch.autograd.grad(out.sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        grad.sum().backward()
