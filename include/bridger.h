@@ -571,6 +571,33 @@ bridger_status bridger_layer_norm_backward(const void *grad, int64_t ldg, const 
 /* 0 for sizes that bridger_layer_norm_backward refuses, and for n_rows == 0. */
 int64_t bridger_layer_norm_backward_workspace(int64_t n_rows, int32_t n_features, int32_t dtype);
 
+/*
+ * A class of every row, drawn from its scores with a given random number.  The classes are those of
+ * a number above -infinity, in top_k's order (the larger score first, of equal ones the lower class).
+ * With z the scores, M their maximum and T the temperature:
+ *     w_j = e^((z_j - M) / T)  for the first top_k classes, else 0;
+ *     a class stays while the w before it in the order are less than top_p times all of them, and
+ *     while z_j >= M + T log(min_p);
+ *     the class is the lowest j for which the w of the staying classes up to j pass u times the w of
+ *     all staying ones, and logp the logarithm of its share of them.
+ * w, their sums and the comparisons are held in double.  A row without a class gives -1 and -infinity.
+ * Where M = +infinity, w is 1 for the classes that reach it and 0 for others.
+ *   logits       [n_rows, n_classes] of dtype, rows ld apart; 1 <= n_classes < 2^31
+ *   u            float [n_rows], in [0, 1) (others count as the nearest of 0 and 1 - 2^-24, NaN as 0)
+ *   temperature  between 0 and 1e6; below 1e-6 the first class in the order is taken (logp 0)
+ *   top_k        0 (all classes) or more;  top_p  between 0 (the first class alone) and 1 (all);
+ *   min_p        between 0 (all) and 1
+ *   temperatures, top_ks, top_ps, min_ps  [n_rows] (int32 top_ks, else float): each row's own values
+ *                in place of the four above, or NULL.  Those outside their range count as the
+ *                nearest end of it (negative top_ks as 0); a NaN as temperature 0, top_p 1, min_p 0
+ *   ids          int32 [n_rows];  logp  float [n_rows], or NULL
+ */
+bridger_status bridger_sample(const void *logits, int64_t ld, int32_t dtype, int64_t n_rows,
+                              int32_t n_classes, const float *u, double temperature,
+                              const float *temperatures, int32_t top_k, const int32_t *top_ks,
+                              double top_p, const float *top_ps, double min_p, const float *min_ps,
+                              int32_t *ids, float *logp, void *stream);
+
 /* Message for the calling thread's most recent failed call ("" if none).  The
  * paper states no error interface; this is the library's own, so that nothing
  * throws across the C ABI (thread-local storage, valid until the thread's next

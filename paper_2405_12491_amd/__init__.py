@@ -440,4 +440,4 @@ from .layers import (  # noqa: E402,F401
 from .operators import (  # noqa: E402,F401
     BRIDGER_BF16, BRIDGER_F16, BRIDGER_F32, BRIDGER_MATMUL_Q8_MAX_FEATURES, BRIDGER_MAX_TOP,
     bridger_distill, bridger_distill_backward, bridger_matmul_q8, bridger_rmsnorm_q8,
-    bridger_top_k, distill, distill_loss, matmul_q8, rmsnorm_q8, top_k)
+    bridger_sample, bridger_top_k, distill, distill_loss, matmul_q8, rmsnorm_q8, sample, top_k)

@@ -324,6 +324,35 @@ bridger_status bridger_embed_backward(const int32_t *ids, int64_t ldi, const int
   return launched([&] { return launch_embed_backward(a, dtype, stream); });
 }
 
+bridger_status bridger_sample(const void *logits, int64_t ld, int32_t dtype, int64_t n_rows,
+                              int32_t n_classes, const float *u, double temperature,
+                              const float *temperatures, int32_t top_k, const int32_t *top_ks,
+                              double top_p, const float *top_ps, double min_p, const float *min_ps,
+                              int32_t *ids, float *logp, void *stream) {
+  clear_error();
+  if (const char *f = count_fault(n_rows, n_classes)) return invalid(f);
+  const int size = bytes_of(dtype);
+  if (!size) return invalid("unknown dtype");
+  if (!(temperature >= 0.0 && temperature <= 1e6))
+    return invalid("temperature must lie between 0 and 1e6");
+  if (top_k < 0) return invalid("top_k < 0");
+  if (!(top_p >= 0.0 && top_p <= 1.0)) return invalid("top_p must lie between 0 and 1");
+  if (!(min_p >= 0.0 && min_p <= 1.0)) return invalid("min_p must lie between 0 and 1");
+  if (n_rows == 0) return BRIDGER_OK;
+  if (!logits || !u || !ids) return invalid("null logits, u or ids");
+  const Rows in[] = {{logits, n_rows, n_classes, ld, size}, {u, n_rows, 1, 1, 4},
+                     {temperatures, n_rows, 1, 1, 4},       {top_ks, n_rows, 1, 1, 4},
+                     {top_ps, n_rows, 1, 1, 4},             {min_ps, n_rows, 1, 1, 4}};
+  const Rows out[] = {{ids, n_rows, 1, 1, 4}, {logp, n_rows, 1, 1, 4}};
+  if (const char *f = arrays_fault(in, 6, out, 2, nullptr)) return invalid(f);
+  if (bridger_status s = device_ready()) return s;
+  return launched([&] {
+    return launch_sample({logits, ld, n_rows, n_classes, u, temperature, top_p, min_p, top_k,
+                          temperatures, top_ps, min_ps, top_ks, ids, logp, 0},
+                         dtype, stream);
+  });
+}
+
 bridger_status bridger_dropout(const void *x, int64_t ldx, const void *residual, int64_t ldr,
                                int32_t dtype, int64_t n_rows, int32_t n_features, double p,
                                const int64_t *seed, int32_t layer, void *out, int64_t ldo,

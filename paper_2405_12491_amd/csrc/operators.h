@@ -149,6 +149,21 @@ struct LayerNormGradArgs {
   int64_t first;   // the launch's first row or workgroup
 };
 
+struct SampleArgs {
+  const void *logits;
+  int64_t ld;
+  int64_t n_rows;
+  int32_t n_classes;
+  const float *u;
+  double temperature, top_p, min_p;
+  int32_t top_k;
+  const float *temperatures, *top_ps, *min_ps;  // null: the values above for every row
+  const int32_t *top_ks;
+  int32_t *ids;
+  float *logp;    // may be null
+  int64_t first;  // the launch's first row
+};
+
 // Each returns a hipError_t as int.  Sizes are positive and every argument checked.
 int launch_top_k(const TopKArgs &a, int32_t dtype, void *stream);
 int launch_distill(const DistillArgs &a, int32_t dtype, bool backward, void *stream);
@@ -160,6 +175,7 @@ int launch_embed_backward(const EmbedArgs &a, int32_t dtype, void *stream);
 int64_t embed_backward_bytes(int64_t n_rows, int32_t n_slots, int32_t n_entries,
                              int32_t n_features);
 
+int launch_sample(const SampleArgs &a, int32_t dtype, void *stream);
 int launch_dropout(const DropoutArgs &a, int32_t dtype, void *stream);
 int launch_layer_norm(const LayerNormArgs &a, int32_t dtype, void *stream);
 int launch_layer_norm_backward(const LayerNormGradArgs &a, int32_t dtype, void *stream);

@@ -1,9 +1,8 @@
 """Operators over rows of scores, logits and features, on torch CUDA tensors.
 
-``bridger_top_k``, ``bridger_distill``, ``bridger_distill_backward``, ``bridger_rmsnorm_q8`` and
-``bridger_matmul_q8`` marshal device pointers to the C entry points of the same names
-(include/bridger.h states formulas, types and limits).  ``top_k``, ``distill``, ``distill_loss``,
-``rmsnorm_q8`` and ``matmul_q8`` take 2-D tensors whose rows are contiguous (any distance between
+The functions named ``bridger_*`` marshal device pointers to the C entry points of the same names
+(include/bridger.h states formulas, types and limits).  ``top_k``, ``sample``, ``distill``,
+``distill_loss``, ``rmsnorm_q8`` and ``matmul_q8`` take 2-D tensors whose rows are contiguous (any distance between
 rows), on any device, and launch on torch's current stream of that device.  There is no CPU
 fallback.  Only ``distill_loss`` can be differentiated: the others pass no gradient and no tangent
 on, whatever their inputs.  Outputs that the caller gives count as written in place: a backward pass
@@ -22,8 +21,10 @@ BRIDGER_MATMUL_Q8_MAX_FEATURES = 131071
 _MOST = 0x7FFFFFFF
 
 _P, _I32, _I64, _F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+_D = ctypes.c_double
 _ARGTYPES = {
     "bridger_top_k": [_P, _I64, _I32, _I64, _I32, _I32, _P, _P, _P],
+    "bridger_sample": [_P, _I64, _I32, _I64, _I32, _P, _D, _P, _I32, _P, _D, _P, _D, _P, _P, _P, _P],
     "bridger_distill": [_P, _I64, _I32, _P, _P, _I32, _I64, _I32, _I32, _F, _P, _P, _P, _P, _I64,
                         _P],
     "bridger_distill_backward": [_P, _I64, _I32, _P, _P, _I32, _I64, _I32, _I32, _F, _P, _P, _P,
@@ -45,6 +46,15 @@ def declare(lib):
 def bridger_top_k(scores_ptr, ld, dtype, n_rows, n_classes, k, values_ptr, ids_ptr, stream=0):
     _B._check(_B.load_library().bridger_top_k(scores_ptr, ld, dtype, n_rows, n_classes, k,
                                               values_ptr, ids_ptr, stream), "bridger_top_k")
+
+
+def bridger_sample(logits_ptr, ld, dtype, n_rows, n_classes, u_ptr, temperature, temperatures_ptr,
+                   top_k, top_ks_ptr, top_p, top_ps_ptr, min_p, min_ps_ptr, ids_ptr, logp_ptr,
+                   stream=0):
+    _B._check(_B.load_library().bridger_sample(
+        logits_ptr, ld, dtype, n_rows, n_classes, u_ptr, temperature, temperatures_ptr, top_k,
+        top_ks_ptr, top_p, top_ps_ptr, min_p, min_ps_ptr, ids_ptr, logp_ptr, stream),
+        "bridger_sample")
 
 
 def bridger_distill(logits_ptr, ldl, dtype, ids_ptr, teacher_ptr, teacher_dtype, n_rows, n_classes,
@@ -201,6 +211,51 @@ def top_k(scores, k: int, values=None, ids=None):
     if given:
         _written(*given)
     return values, ids
+
+
+def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, ids=None, logp=None):
+    """A class of every row, drawn with the row's random number ``u`` (float32 [n], in [0, 1)) from
+    the softmax of logits / temperature over the ``top_k`` largest (0: all) and, of those, the
+    shortest leading part that holds ``top_p`` of their mass and the classes of at least ``min_p``
+    times the largest probability: (ids int32 [n], logp float32 [n], the drawn class's logarithm of
+    its share of what stays).  The four take a number, or a tensor [n] with a value for each row
+    (float32, top_k int32).  A temperature of 0 takes the largest score.  A row of nothing but
+    -infinity and NaN gives -1."""
+    if _torch is None:
+        _setup()
+    n, c, ld = _rows(logits, "logits", None, None, None, None)
+    dev, f32 = logits.get_device(), _torch.float32
+    _vector(u, "u", n, f32, dev)
+    given = ids is not None or logp is not None
+    scalar, own = [], []
+    for name, v, dtype, none in (("temperature", temperature, f32, 1.0),
+                                 ("top_k", top_k, _torch.int32, 0), ("top_p", top_p, f32, 1.0),
+                                 ("min_p", min_p, f32, 0.0)):
+        if isinstance(v, _torch.Tensor):
+            _vector(v, name, n, dtype, dev)
+            scalar.append(none)
+            own.append(v.data_ptr())
+        else:
+            scalar.append(type(none)(v))
+            own.append(None)
+    k = scalar[1]
+    if not 0 <= k <= _MOST:
+        raise ValueError("top_k must lie between 0 and 2^31 - 1")
+    if ids is None:
+        ids = logits.new_empty((n,), dtype=_torch.int32)
+    else:
+        _vector(ids, "ids", n, _torch.int32, dev)
+    if logp is None:
+        logp = u.new_empty((n,))
+    else:
+        _vector(logp, "logp", n, f32, dev)
+        _writable(logp, "logp")
+    _call("bridger_sample", logits, logits.data_ptr(), ld, _code(logits.dtype), n, c, u.data_ptr(),
+          scalar[0], own[0], k, own[1], scalar[2], own[2], scalar[3], own[3], ids.data_ptr(),
+          logp.data_ptr())
+    if given:
+        _written(ids, logp)
+    return ids, logp
 
 
 def _check_distill(logits, ids, teacher, weight):

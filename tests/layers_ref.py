@@ -139,3 +139,40 @@ def layer_norm_grad(grad, t, weight=None, grad_total=None, eps=1e-5):
         tw = (np.abs(g) * eh).sum(0) + (adds + 2) * U * np.abs(g * h).sum(0)
         tb = (adds + 2) * U * np.abs(g).sum(0)
     return (dx, dw, db), [np.where(np.isfinite(v), v, 0.0) for v in (tol, tw, tb)]
+
+
+def sample_row(z, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """(class, log of its share, the classes that stay, how far the draw and the cut by top_p are from
+    another answer: the smallest distance of a sum from its limit, relative to the sum of all)."""
+    z = np.asarray(z, np.float64)
+    cls = np.flatnonzero(z > -np.inf)
+    cls = cls[np.argsort(-z[cls], kind="stable")]
+    if len(cls) == 0:
+        return -1, -np.inf, cls, 1.0
+    top = z[cls[0]]
+    if not temperature >= 1e-6 or top_p <= 0:
+        return cls[0], 0.0, cls[:1], 1.0
+    temperature = min(temperature, 1e6)
+    if top_k > 0:
+        cls = cls[:top_k]
+    with np.errstate(all="ignore"):
+        w = np.where(z[cls] == top, 1.0, np.exp((z[cls] - top) / temperature))
+    sums = np.cumsum(w)
+    gap, stay = 1.0, len(cls)
+    if top_p < 1:
+        limit = top_p * sums[-1]
+        before = np.concatenate([[0.0], sums[:-1]])
+        stay = int((before < limit).sum())
+        near = np.abs(before[1:] - limit) if len(before) > 1 else np.ones(1)
+        exact = np.all(w == 1.0)                 # whole numbers: no rounding, so no doubt
+        gap = 1.0 if exact else near.min() / sums[-1]
+    if min_p > 0:
+        stay = min(stay, int((z[cls] >= top + temperature * np.log(min(min_p, 1.0))).sum()))
+    order = np.argsort(cls[:stay], kind="stable")
+    cls, w = cls[:stay][order], w[:stay][order]
+    sums = np.cumsum(w)
+    u = min(max(u, 0.0), 1 - 2.0 ** -24) if u == u else 0.0
+    at = min(int((sums <= u * sums[-1]).sum()), len(sums) - 1)
+    if not np.all(w == 1.0):
+        gap = min(gap, np.abs(sums[:-1] - u * sums[-1]).min() / sums[-1] if len(sums) > 1 else 1.0)
+    return cls[at], np.log(w[at] / sums[-1]), cls, gap
