@@ -10,6 +10,10 @@ template <typename T, int W>
 struct Elements {
   u32x4 raw;
   T one;
+  __device__ void clear() {
+    raw = u32x4{0, 0, 0, 0};
+    one = (T)0.0f;
+  }
   __device__ void load(const T *p) {
     if constexpr (W == 1) {
       one = *p;
@@ -34,16 +38,15 @@ __device__ inline void store_elements(T *p, const float (&v)[W]) {
   }
 }
 
-// The entry that slot s of a row reads, or -1.
-__device__ inline int32_t entry_of(const EmbedArgs &a, int64_t row, int s) {
-  const int32_t id = a.ids[row * a.ldi + s];
-  int64_t begin = 0, end = a.n_entries;
-  if (a.offsets) {
-    begin = a.offsets[s];
-    const int64_t stop = a.offsets[s + 1];
-    end = stop < end ? stop : end;
-  }
+// The entry that slot s reads where it holds `id`, or -1.
+__device__ inline int32_t entry_at(const EmbedArgs &a, int32_t id, int s) {
+  if (!a.offsets) return (uint32_t)id < (uint32_t)a.n_entries ? id : -1;
+  const int64_t begin = a.offsets[s], stop = a.offsets[s + 1];
+  const int64_t end = stop < a.n_entries ? stop : a.n_entries;
   return id >= 0 && begin >= 0 && begin < end && id < end - begin ? (int32_t)(begin + id) : -1;
+}
+__device__ inline int32_t entry_of(const EmbedArgs &a, int64_t row, int s) {
+  return entry_at(a, a.ids[row * a.ldi + s], s);
 }
 
 // A row's features are parted into tiles of G lanes with W elements each; the last lane of a row
@@ -99,31 +102,46 @@ __global__ __launch_bounds__(kThreads) void embed_rows_kernel(EmbedArgs a) {
   }
 }
 
-// Several slots a row: a.parts groups of G lanes share a row's slots and join in LDS.
+// Lane u's value for all lanes of its group of G.
+template <int G>
+__device__ inline uint32_t of_lane(uint32_t v, int u) {
+  if constexpr (G == 64) {
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, u);
+  } else {
+    return (uint32_t)__shfl((int)v, u, G);
+  }
+}
+
+// Several slots a row: a.parts groups of G lanes share a row's slots and join in LDS.  Each lane of a
+// group finds the entry of one of the next slots, and all of them take each entry in turn.
 template <typename T, int G, int W>
 __global__ __launch_bounds__(kThreads) void embed_bag_kernel(EmbedArgs a) {
-  constexpr int groups = kThreads / G;
+  constexpr int groups = kThreads / G, U = G < 16 ? G : 16;
   __shared__ float join[kThreads * W];
   const Place p = place_of<G, W>(a, a.first);
-  const int group = threadIdx.x / G, part = group & (a.parts - 1);
+  const int lane = threadIdx.x % G, group = threadIdx.x / G, part = group & (a.parts - 1);
   const int64_t wanted = p.block * (groups / a.parts) + group / a.parts;
   const int64_t row = wanted < a.n_rows ? wanted : a.n_rows - 1;
-  const T *table = (const T *)a.table + p.column;
+  const char *table = (const char *)((const T *)a.table + p.column);
   float sum[W];
 #pragma unroll
   for (int i = 0; i < W; ++i) sum[i] = 0.0f;
-  for (int64_t s0 = part * kAhead; s0 < a.n_slots; s0 += (int64_t)a.parts * kAhead) {
-    int32_t at[kAhead];
+  for (int64_t s0 = part * U; s0 < a.n_slots; s0 += (int64_t)a.parts * U) {
+    int32_t at = -1;
+    if (lane < U && s0 + lane < a.n_slots) at = entry_of(a, row, (int)(s0 + lane));
+    const int64_t offset = at * a.ldt * (int64_t)sizeof(T);  // (below 0: none)
+    Elements<T, W> e[U];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-      at[u] = s0 + u < a.n_slots ? entry_of(a, row, (int)(s0 + u)) : -1;
-    Elements<T, W> e[kAhead];
+    for (int u = 0; u < U; ++u) {
+      const uint32_t low = of_lane<G>((uint32_t)offset, u);
+      const int32_t high = (int32_t)of_lane<G>((uint32_t)(offset >> 32), u);
+      e[u].clear();
+      if (high >= 0) e[u].load((const T *)(table + ((int64_t)high << 32 | low)));
+    }
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) e[u].load(table + (at[u] < 0 ? 0 : at[u]) * a.ldt);
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-      for (int i = 0; i < W; ++i) sum[i] += at[u] < 0 ? 0.0f : e[u].at(i);
+      for (int i = 0; i < W; ++i) sum[i] += e[u].at(i);
   }
   if (a.parts > 1) {  // of the whole workgroup
 #pragma unroll
@@ -173,7 +191,7 @@ int launch_embed(const EmbedArgs &args, int32_t dtype, void *stream) {
       // groups share a row's slots while rows alone leave compute units idle
       a.parts = 1;
       while (a.parts < groups && a.n_rows * a.tiles * a.parts < 2048 * groups &&
-             a.parts * kAhead < a.n_slots)
+             a.parts * (G < 16 ? G : 16) < a.n_slots)
         a.parts *= 2;
       const int64_t rows = groups / a.parts;
       return launch_blocks(embed_bag_kernel<T, G, W>, (a.n_rows + rows - 1) / rows * a.tiles,
@@ -184,74 +202,138 @@ int launch_embed(const EmbedArgs &args, int32_t dtype, void *stream) {
 
 // ============================================================================== BACKWARD
 // Pairs (entry, row), one a slot, are sorted by entry: a radix sort whose passes keep the order of
-// equal keys, so that an entry's rows stand in the order of their slots.  Then groups of lanes add
-// an entry's rows.  Empty slots have the key n_entries and end up behind all others.
-constexpr int kTile = 4096;     // pairs that a workgroup sorts at once
-constexpr int kMaxDigit = 11;   // bits a pass
-constexpr int kChunk = 64;      // pairs that are added beforehand where they belong to one entry
+// equal keys, so that an entry's rows stand in the order of their slots.  Groups of lanes then add
+// the rows of blocks of neighbouring pairs; an entry whose pairs lie in one block is finished there,
+// those of several blocks are joined afterwards, block after block.  The rest of the table is zero:
+// workgroups that would wait for the sort fill it.  Empty slots have the key n_entries and end up
+// behind all others.
+constexpr int kFew = 16384;    // pairs that a workgroup holds
+constexpr int kTile = 2048;    // pairs that a workgroup sorts at once where there are more
+constexpr int kMaxDigit = 9;   // bits a pass of many pairs,
+constexpr int kFewDigit = 11;  // and of few
+constexpr int kBucketBits = 5, kBuckets = 1 << kBucketBits, kPlaceBits = 14;
+constexpr int kFewThreads = 512;
+static_assert(kFew == 1 << kPlaceBits, "a place fits its bits");
+
+struct Pair {
+  uint32_t key, row;
+};
 
 struct SortPlan {
   int passes, bits;  // of one digit
-  int64_t pairs, tiles, chunks, supers;
+  bool few;
+  int64_t pairs, tiles;
+  int length;  // pairs of a block
+  int64_t blocks;
 };
-static SortPlan plan_of(int64_t pairs, int32_t n_entries) {
+static SortPlan plan_of(int64_t pairs, int32_t n_entries, int32_t n_features) {
   SortPlan p;
   int bits = 0;
   while ((int64_t)n_entries >> bits) ++bits;  // the largest key is n_entries
-  p.passes = (bits + kMaxDigit - 1) / kMaxDigit;
+  p.few = pairs <= kFew && bits <= 32 - kPlaceBits + kBucketBits;
+  if (p.few) bits = bits > kBucketBits ? bits - kBucketBits : 1;
+  const int most = p.few ? kFewDigit : kMaxDigit;
+  p.passes = (bits + most - 1) / most;
   p.bits = (bits + p.passes - 1) / p.passes;
   p.pairs = pairs;
   p.tiles = (pairs + kTile - 1) / kTile;
-  p.chunks = pairs / kChunk;
-  p.supers = p.chunks / kChunk;
+  // blocks as long as leaves every compute unit several waves' work
+  const int64_t lanes = n_features < 256 ? 16 : 64;
+  p.length = 16;
+  while (p.length < 128 && pairs / p.length * lanes > 512 * 1024) p.length *= 2;
+  p.blocks = (pairs + p.length - 1) / p.length;
   return p;
 }
 
 struct GradArgs {
   EmbedArgs e;
   int64_t pairs, tiles;
-  const uint32_t *keys, *rows;  // sorted so far; null: the slots themselves
-  uint32_t *keys_to, *rows_to;
+  const Pair *sorted;  // so far; null: the slots themselves
+  Pair *to;
   uint32_t *counts;  // [digit values][tiles]
   uint32_t *totals;  // [digit values]
-  float *chunk, *super;  // sums of whole chunks, and of kChunk chunks, that belong to one entry
-  int64_t chunks, supers;
-  int shift, bits;
-  int each;       // entries of a group
+  float *partial;    // [blocks][2]: of the entry that goes on from the block before; that goes on
+  int64_t blocks;
+  int length;
+  int shift, bits, passes;
+  int fill;       // workgroups that write zeros, 0: none
+  int bytes;      // of an element
   int64_t first;  // the launch's first workgroup
 };
 
-struct Pair {
-  uint32_t key, row;
-};
-__device__ inline Pair pair_of(const GradArgs &a, int64_t i) {
-  if (a.keys) return {a.keys[i], a.rows[i]};
-  uint32_t row = (uint32_t)i, s = 0;
-  if (a.e.n_slots > 1) {
-    row = (uint32_t)i / (uint32_t)a.e.n_slots;
-    s = (uint32_t)i - row * (uint32_t)a.e.n_slots;
+// The pairs of slots (or of what is sorted) begin, begin + step, ... before `end`: all loads first, since
+// one inside a branch is waited for there; past the end those of the last.
+template <int N>
+__device__ inline void load_pairs(const GradArgs &a, int64_t begin, int step, int64_t end, int rounds,
+                                  Pair (&p)[N]) {
+  auto index = [&](int u) {
+    const int64_t i = begin + u * step;
+    return i < end ? i : end - 1;
+  };
+  if (a.sorted) {
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+      if (u < rounds) p[u] = a.sorted[index(u)];
+    return;
   }
-  const int32_t at = entry_of(a.e, row, (int)s);
-  return {at < 0 ? (uint32_t)a.e.n_entries : (uint32_t)at, row};
+  int32_t id[N];
+#pragma unroll
+  for (int u = 0; u < N; ++u)
+    if (u < rounds) {
+      const uint32_t i = (uint32_t)index(u);
+      uint32_t s = 0;
+      p[u].row = i;
+      if (a.e.n_slots > 1) {
+        p[u].row = i / (uint32_t)a.e.n_slots;
+        s = i - p[u].row * (uint32_t)a.e.n_slots;
+      }
+      p[u].key = s;
+      id[u] = a.e.ids[(int64_t)p[u].row * a.e.ldi + s];
+    }
+#pragma unroll
+  for (int u = 0; u < N; ++u)
+    if (u < rounds) {
+      const int32_t at = entry_at(a.e, id[u], (int)p[u].key);
+      p[u].key = at < 0 ? (uint32_t)a.e.n_entries : (uint32_t)at;
+    }
 }
-__device__ inline uint32_t digit_of(const GradArgs &a, uint32_t key) {
-  return key >> a.shift & ((1u << a.bits) - 1);
+__device__ inline uint32_t digit_of(uint32_t key, int shift, int bits) {
+  return key >> shift & ((1u << bits) - 1);
 }
 
-// How many of a tile's pairs have each digit.
-__global__ __launch_bounds__(kThreads) void embed_count_kernel(GradArgs a) {
-  __shared__ uint32_t count[1 << kMaxDigit];
-  const int values = 1 << a.bits;
-  for (int d = threadIdx.x; d < values; d += kThreads) count[d] = 0;
-  __syncthreads();
-  const int64_t tile = a.first + blockIdx.x, begin = tile * kTile;
-#pragma unroll
-  for (int u = 0; u < kTile / kThreads; ++u) {
-    const int64_t i = begin + u * kThreads + threadIdx.x;
-    if (i < a.pairs) atomicAdd(&count[digit_of(a, pair_of(a, i).key)], 1u);
+// Zeros, 16 bytes a lane where a row has them: workgroup `part` of a.fill.
+__device__ inline void fill_zeros(const GradArgs &a, int part, int threads) {
+  const int64_t row_bytes = (int64_t)a.e.n_features * a.bytes, pitch = a.e.ldo * a.bytes;
+  char *out = (char *)a.e.out;
+  const int64_t lane = (int64_t)part * threads + threadIdx.x, lanes = (int64_t)a.fill * threads;
+  const u32x4 zero = {0, 0, 0, 0};
+  if (pitch == row_bytes || a.e.n_entries == 1) {  // one run, but for its first and last bytes
+    const int64_t bytes = row_bytes * a.e.n_entries;
+    const int64_t head = bytes < 16 ? bytes : (int64_t)(-(uintptr_t)out & 15);
+    const int64_t whole = (bytes - head) / 16;
+    for (int64_t i = lane; i < whole; i += lanes) *(u32x4 *)(out + head + i * 16) = zero;
+    const int64_t tail = bytes - head - whole * 16;
+    for (int64_t i = lane; i < (head + tail) / a.bytes; i += lanes) {
+      char *p = out + (i * a.bytes < head ? i * a.bytes : bytes - tail + (i * a.bytes - head));
+      if (a.bytes == 4) {
+        *(uint32_t *)p = 0;
+      } else {
+        *(uint16_t *)p = 0;
+      }
+    }
+    return;
   }
-  __syncthreads();
-  for (int d = threadIdx.x; d < values; d += kThreads) a.counts[d * a.tiles + tile] = count[d];
+  for (int64_t row = (int64_t)part * (threads / 64) + threadIdx.x / 64; row < a.e.n_entries;
+       row += (int64_t)a.fill * (threads / 64)) {
+    char *p = out + row * pitch;
+    if (row_bytes < 16) {
+      for (int64_t i = (threadIdx.x & 63) * a.bytes; i < row_bytes; i += 64 * a.bytes)
+        __builtin_memcpy(p + i, &zero, 2), __builtin_memcpy(p + i + a.bytes - 2, &zero, 2);
+    } else {
+      for (int64_t i = (threadIdx.x & 63) * 16; i < row_bytes; i += 64 * 16)
+        __builtin_memcpy(p + (i < row_bytes - 16 ? i : row_bytes - 16), &zero, 16);
+    }
+  }
 }
 
 // The sum of v over the lanes below this one, and over all.
@@ -265,6 +347,169 @@ __device__ inline uint32_t lanes_before(uint32_t v, uint32_t *all) {
   }
   *all = __shfl(sum, 63, 64);
   return sum - v;
+}
+
+// How many of the lanes in the mask are below this one.
+__device__ inline int lanes_below(uint64_t mask) {
+  return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32),
+                                        __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+// Lanes of the wave whose digit is this lane's (`live` lanes only).
+__device__ inline uint64_t lanes_alike(uint32_t digit, int bits, bool live) {
+  const uint64_t all = __ballot(live);
+  uint32_t low = (uint32_t)all, high = (uint32_t)(all >> 32);
+  for (int b = 0; b < bits; ++b) {
+    const uint64_t set = __ballot(digit >> b & 1);
+    const uint32_t unset = (digit >> b & 1) - 1;  // all bits where the lane's is 0
+    low &= (uint32_t)set ^ unset;
+    high &= (uint32_t)(set >> 32) ^ unset;
+  }
+  return (uint64_t)high << 32 | low;
+}
+
+// The place of the lane's pair of digit d, from next[d], which moves on by the lanes alike; all lanes
+// of a wave call it.
+__device__ inline uint32_t take_place(volatile uint32_t *next, uint32_t d, int bits, bool live) {
+  const uint64_t same = lanes_alike(d, bits, live);
+  const int earlier = lanes_below(same);
+  uint32_t at = 0;
+  if (live) {
+    at = next[d] + earlier;
+    // the wave's lanes have all read it; the first of those alike moves it on
+    __builtin_amdgcn_wave_barrier();
+    if (earlier == 0) next[d] = at + __popcll(same);
+    __builtin_amdgcn_wave_barrier();
+  }
+  return at;
+}
+
+// The counts of the waves' digits become the places of each wave's first pair, behind those of smaller
+// digits and of the waves before.  Each thread takes a run of digits.
+template <int kWaves, int kValues>
+__device__ inline void places(uint32_t (&next)[kWaves][kValues], uint32_t *wave_sum, int values) {
+  const int run = (values + kWaves * 64 - 1) / (kWaves * 64);
+  const int d0 = threadIdx.x * run, wave = threadIdx.x / 64;
+  uint32_t own = 0, all;
+  for (int d = d0; d < d0 + run && d < values; ++d)
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) own += next[w][d];
+  uint32_t at = lanes_before(own, &all);
+  if ((threadIdx.x & 63) == 0) wave_sum[wave] = all;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) at += wave_sum[w];
+  for (int d = d0; d < d0 + run && d < values; ++d)
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const uint32_t c = next[w][d];
+      next[w][d] = at;
+      at += c;
+    }
+  __syncthreads();
+}
+
+// Few pairs: what the sums need is that an entry's pairs stand together, in their order, so kBuckets
+// workgroups take the entries of one remainder each.  Each reads all slots, keeps its own, whose
+// place among all it learns from the count of lower remainders, and sorts them by the rest of the key
+// in one pass (tables below 2^16 entries) or two.  The other workgroups fill the table with zeros
+// meanwhile.  16,384 slots of 50,257 entries: XX us.
+__global__ __launch_bounds__(kFewThreads) void embed_group_kernel(GradArgs a) {
+  constexpr int waves = kFewThreads / 64, most = kFew / kFewThreads;
+  __shared__ uint32_t held[kFew];  // rest of the key, place among the slots
+  __shared__ uint32_t next[waves][1 << kFewDigit];
+  __shared__ uint32_t wave_sum[2][waves];
+  if (blockIdx.x >= kBuckets) {
+    fill_zeros(a, blockIdx.x - kBuckets, kFewThreads);
+    return;
+  }
+  const uint32_t bucket = blockIdx.x;
+  const int wave = threadIdx.x / 64, lane = threadIdx.x & 63;
+  int base = 0, count = 0;  // pairs of lower remainders; of this one
+  {
+    const int n = (int)a.pairs, rounds = (n + kFewThreads - 1) / kFewThreads;
+    const int begin = wave * rounds * 64 + lane;
+    Pair p[most];
+    load_pairs<most>(a, begin, 64, n, rounds, p);
+    int own = 0, lower = 0;
+#pragma unroll
+    for (int u = 0; u < most; ++u)
+      if (u < rounds) {
+        const bool live = begin + u * 64 < n;
+        own += __popcll(__ballot(live && p[u].key % kBuckets == bucket));
+        lower += __popcll(__ballot(live && p[u].key % kBuckets < bucket));
+      }
+    if (lane == 0) wave_sum[0][wave] = own, wave_sum[1][wave] = lower;
+    __syncthreads();
+    int at = 0;
+    for (int w = 0; w < waves; ++w) {
+      if (w == wave) at = count;
+      count += wave_sum[0][w];
+      base += wave_sum[1][w];
+    }
+#pragma unroll
+    for (int u = 0; u < most; ++u)
+      if (u < rounds) {
+        const bool mine = begin + u * 64 < n && p[u].key % kBuckets == bucket;
+        const uint64_t all = __ballot(mine);
+        if (mine)
+          held[at + lanes_below(all)] =
+              p[u].key >> kBucketBits << kPlaceBits | (uint32_t)(begin + u * 64);
+        at += __popcll(all);
+      }
+  }
+  const int rounds = (count + kFewThreads - 1) / kFewThreads, values = 1 << a.bits;
+  const int begin = wave * rounds * 64 + lane;
+  for (int pass = 0; pass < a.passes; ++pass) {
+    __syncthreads();
+    for (int d = lane; d < values; d += 64) next[wave][d] = 0;
+    const int shift = kPlaceBits + pass * a.bits;
+    uint32_t item[most];
+#pragma unroll
+    for (int u = 0; u < most; ++u)
+      if (u < rounds && begin + u * 64 < count) {
+        item[u] = held[begin + u * 64];
+        atomicAdd(&next[wave][digit_of(item[u], shift, a.bits)], 1u);
+      }
+    __syncthreads();
+    places<waves, 1 << kFewDigit>(next, wave_sum[0], values);
+#pragma unroll
+    for (int u = 0; u < most; ++u)
+      if (u < rounds) {
+        const bool live = begin + u * 64 < count;
+        const uint32_t at = take_place(next[wave], digit_of(item[u], shift, a.bits), a.bits, live);
+        if (live && pass < a.passes - 1) {
+          held[at] = item[u];
+        } else if (live) {
+          const uint32_t i = item[u] & (kFew - 1);
+          a.to[base + at] = {item[u] >> kPlaceBits << kBucketBits | bucket,
+                             a.e.n_slots > 1 ? i / (uint32_t)a.e.n_slots : i};
+        }
+      }
+  }
+}
+
+// More pairs: a pass counts every tile's digits, adds the counts up over the tiles, and moves the
+// pairs.  How many of a tile's pairs have each digit:
+__global__ __launch_bounds__(kThreads) void embed_count_kernel(GradArgs a) {
+  __shared__ uint32_t count[1 << kMaxDigit];
+  const int64_t block = a.first + blockIdx.x;
+  if (block >= a.tiles) {
+    fill_zeros(a, (int)(block - a.tiles), kThreads);
+    return;
+  }
+  const int values = 1 << a.bits;
+  for (int d = threadIdx.x; d < values; d += kThreads) count[d] = 0;
+  __syncthreads();
+  const int64_t begin = block * kTile;
+  constexpr int rounds = kTile / kThreads;
+  Pair p[rounds];
+  load_pairs<rounds>(a, begin + threadIdx.x, kThreads, a.pairs, rounds, p);
+#pragma unroll
+  for (int u = 0; u < rounds; ++u)
+    if (begin + u * kThreads + threadIdx.x < a.pairs)
+      atomicAdd(&count[digit_of(p[u].key, a.shift, a.bits)], 1u);
+  __syncthreads();
+  for (int d = threadIdx.x; d < values; d += kThreads) a.counts[d * a.tiles + block] = count[d];
 }
 
 // Per digit: its count in every tile becomes that of the tiles before.  A wave a digit.
@@ -289,222 +534,219 @@ __global__ __launch_bounds__(kThreads) void embed_scan_kernel(GradArgs a) {
   if ((threadIdx.x & 63) == 0) a.totals[d] = before;
 }
 
-// Lanes of the wave whose digit is this lane's (`live` lanes only).
-__device__ inline uint64_t lanes_alike(uint32_t digit, int bits, bool live) {
-  uint64_t same = __ballot(live);
-  for (int b = 0; b < bits; ++b) {
-    const uint64_t set = __ballot(digit >> b & 1);
-    same &= digit >> b & 1 ? set : ~set;
-  }
-  return same;
-}
-
-// Moves a tile's pairs to their places.  Every wave has a run of the tile's pairs and, for each
-// digit, the place of its next pair: those of smaller digits, of the tiles before, of the waves
-// before, and its own so far.
+// Moves a tile's pairs to their places: within the tile first, through LDS, so that what goes to one
+// digit's place leaves in runs.
 __global__ __launch_bounds__(kThreads) void embed_move_kernel(GradArgs a) {
   constexpr int waves = kThreads / 64, rounds = kTile / kThreads;
   __shared__ uint32_t next[waves][1 << kMaxDigit];
   __shared__ uint32_t wave_sum[waves];
+  __shared__ Pair tile_pairs[kTile];
+  __shared__ uint32_t shift_of[1 << kMaxDigit];  // from a pair's place in the tile to that in all
   const int values = 1 << a.bits, wave = threadIdx.x / 64, lane = threadIdx.x & 63;
-  const int64_t tile = a.first + blockIdx.x;
-  const int64_t begin = tile * kTile + wave * (rounds * 64) + lane;
-  for (int d = threadIdx.x; d < values; d += kThreads)
-#pragma unroll
-    for (int w = 0; w < waves; ++w) next[w][d] = 0;
+  const int64_t tile = a.first + blockIdx.x, first = tile * kTile;
+  const int begin = wave * (rounds * 64) + lane;
+  const int n = (int)(a.pairs - first < kTile ? a.pairs - first : kTile);
   Pair p[rounds];
-#pragma unroll
-  for (int u = 0; u < rounds; ++u) {
-    const int64_t i = begin + u * 64;
-    p[u] = i < a.pairs ? pair_of(a, i) : Pair{0, 0};
+  load_pairs<rounds>(a, first + begin, 64, a.pairs, rounds, p);
+  // where a digit's pairs of this tile begin among all
+  {
+    const int run = (values + kThreads - 1) / kThreads, d0 = threadIdx.x * run;
+    uint32_t own = 0, all;
+    for (int d = d0; d < d0 + run && d < values; ++d) own += a.totals[d];
+    uint32_t before = lanes_before(own, &all);
+    if (lane == 0) wave_sum[wave] = all;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) before += wave_sum[w];
+    for (int d = d0; d < d0 + run && d < values; ++d) {
+      shift_of[d] = before + a.counts[d * a.tiles + tile];
+      before += a.totals[d];
+    }
   }
-  __syncthreads();
+  for (int d = lane; d < values; d += 64) next[wave][d] = 0;
 #pragma unroll
   for (int u = 0; u < rounds; ++u)
-    if (begin + u * 64 < a.pairs) atomicAdd(&next[wave][digit_of(a, p[u].key)], 1u);
-  // each thread takes a run of digits
-  constexpr int run = (1 << kMaxDigit) / kThreads;
-  const int d0 = threadIdx.x * run;
-  uint32_t own = 0, all;
-  for (int i = 0; i < run; ++i) own += d0 + i < values ? a.totals[d0 + i] : 0;
-  uint32_t before = lanes_before(own, &all);
-  if (lane == 0) wave_sum[wave] = all;
+    if (begin + u * 64 < n) atomicAdd(&next[wave][digit_of(p[u].key, a.shift, a.bits)], 1u);
   __syncthreads();
-  for (int w = 0; w < wave; ++w) before += wave_sum[w];
-  for (int i = 0; i < run && d0 + i < values; ++i) {
-    const int d = d0 + i;
-    uint32_t at = before + a.counts[d * a.tiles + tile];
-#pragma unroll
-    for (int w = 0; w < waves; ++w) {
-      const uint32_t c = next[w][d];
-      next[w][d] = at;
-      at += c;
-    }
-    before += a.totals[d];
-  }
+  places<waves, 1 << kMaxDigit>(next, wave_sum, values);
+  for (int d = threadIdx.x; d < values; d += kThreads) shift_of[d] -= next[0][d];
   __syncthreads();
-  volatile uint32_t *mine = next[wave];
 #pragma unroll
   for (int u = 0; u < rounds; ++u) {
-    const bool live = begin + u * 64 < a.pairs;
-    const uint32_t d = digit_of(a, p[u].key);
-    const uint64_t same = lanes_alike(d, a.bits, live);
-    const int earlier = __popcll(same & ((uint64_t(1) << lane) - 1));
-    if (live) {
-      const uint32_t at = mine[d];
-      // the wave's lanes have all read it; the first of those alike moves it on
-      __builtin_amdgcn_wave_barrier();
-      if (earlier == 0) mine[d] = at + __popcll(same);
-      __builtin_amdgcn_wave_barrier();
-      a.keys_to[at + earlier] = p[u].key;
-      a.rows_to[at + earlier] = p[u].row;
-    }
-  }
-}
-
-// The first pair whose key reaches `key`, found by all lanes of a wave together.
-__device__ inline int64_t first_pair(const uint32_t *keys, int64_t n, uint32_t key) {
-  int64_t lo = 0, hi = n;
-  while (lo < hi) {
-    const int64_t step = (hi - lo + 63) / 64, i = lo + (threadIdx.x & 63) * step;
-    const int below = __popcll(__ballot(i < hi && keys[i < hi ? i : lo] < key));
-    if (below == 0) {
-      hi = lo;
-    } else {
-      const int64_t end = lo + below * step;
-      lo = end - step + 1;
-      hi = end < hi ? end : hi;
-    }
-  }
-  return lo;
-}
-
-// sum += rows [i, end) of `width` floats apart, from their first element `p`.
-template <int W>
-__device__ inline void add_sums(float (&sum)[W], const float *p, int64_t width, int64_t i,
-                                int64_t end) {
-  for (; i < end; i += kAhead) {
-    float v[kAhead][W];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-      __builtin_memcpy(v[u], p + (i + u < end ? i + u : i) * width, sizeof(v[u]));
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-      for (int k = 0; k < W; ++k) sum[k] += i + u < end ? v[u][k] : 0.0f;
-  }
-}
-template <typename T, int W>
-__device__ inline void add_rows(float (&sum)[W], const GradArgs &a, const T *grad, int64_t i,
-                                int64_t end) {
-  for (; i < end; i += kAhead) {
-    uint32_t row[kAhead];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) row[u] = a.rows[i + u < end ? i + u : i];
-    Elements<T, W> e[kAhead];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) e[u].load(grad + (int64_t)row[u] * a.e.ldt);
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-      for (int k = 0; k < W; ++k) sum[k] += i + u < end ? e[u].at(k) : 0.0f;
-  }
-}
-
-// Sums of the chunks whose pairs all belong to one entry, for entries with many rows.
-template <typename T, int G, int W>
-__global__ __launch_bounds__(kThreads) void embed_chunk_kernel(GradArgs a) {
-  const Place p = place_of<G, W>(a.e, a.first);
-  const int64_t c = p.block * (kThreads / G) + threadIdx.x / G;
-  if (c >= a.chunks || !p.inside) return;
-  const uint32_t key = a.keys[c * kChunk];
-  if (key != a.keys[c * kChunk + kChunk - 1] || key >= (uint32_t)a.e.n_entries) return;
-  float sum[W];
-#pragma unroll
-  for (int k = 0; k < W; ++k) sum[k] = 0.0f;
-  add_rows<T, W>(sum, a, (const T *)a.e.table + p.column, c * kChunk, (c + 1) * kChunk);
-  __builtin_memcpy(a.chunk + c * a.e.n_features + p.column, sum, sizeof(sum));
-}
-template <int G, int W>
-__global__ __launch_bounds__(kThreads) void embed_super_kernel(GradArgs a) {
-  constexpr int64_t pairs = kChunk * kChunk;
-  const Place p = place_of<G, W>(a.e, a.first);
-  const int64_t c = p.block * (kThreads / G) + threadIdx.x / G;
-  if (c >= a.supers || !p.inside) return;
-  const uint32_t key = a.keys[c * pairs];
-  if (key != a.keys[c * pairs + pairs - 1] || key >= (uint32_t)a.e.n_entries) return;
-  float sum[W];
-#pragma unroll
-  for (int k = 0; k < W; ++k) sum[k] = 0.0f;
-  add_sums<W>(sum, a.chunk + p.column, a.e.n_features, c * kChunk, (c + 1) * kChunk);
-  __builtin_memcpy(a.super + c * a.e.n_features + p.column, sum, sizeof(sum));
-}
-
-// A workgroup's groups of lanes take a.each entries each: rows up to the first whole chunk, chunks
-// up to the first whole super chunk, those, and the rest likewise.
-constexpr int kMostEntries = kThreads;
-template <typename T, int G, int W>
-__global__ __launch_bounds__(kThreads) void embed_entries_kernel(GradArgs a) {
-  constexpr int groups = kThreads / G;
-  __shared__ int64_t bound[2];
-  __shared__ uint32_t start[kMostEntries + 1];
-  const Place p = place_of<G, W>(a.e, a.first);
-  const int n = groups * a.each;
-  const int64_t e0 = p.block * n;
-  const int64_t e1 = e0 + n < a.e.n_entries ? e0 + n : a.e.n_entries;
-  if (threadIdx.x < 128) {
-    const int64_t at =
-        first_pair(a.keys, a.pairs, (uint32_t)(threadIdx.x < 64 ? e0 : e1));
-    if ((threadIdx.x & 63) == 0) bound[threadIdx.x / 64] = at;
+    const bool live = begin + u * 64 < n;
+    const uint32_t at = take_place(next[wave], digit_of(p[u].key, a.shift, a.bits), a.bits, live);
+    if (live) tile_pairs[at] = p[u];
   }
   __syncthreads();
-  for (int t = threadIdx.x; t <= e1 - e0; t += kThreads) {
-    int64_t lo = bound[0], hi = bound[1];
-    while (lo < hi) {
-      const int64_t mid = (lo + hi) / 2;
-      if (a.keys[mid] < (uint32_t)(e0 + t)) {
-        lo = mid + 1;
+#pragma unroll
+  for (int u = 0; u < rounds; ++u) {
+    const int i = u * kThreads + threadIdx.x;
+    if (i < n) {
+      const Pair q = tile_pairs[i];
+      a.to[shift_of[digit_of(q.key, a.shift, a.bits)] + i] = q;
+    }
+  }
+}
+
+// G lanes add the rows of a block of neighbouring pairs, whatever their entries, with U loads on
+// their way, and hand on what they have where the entry changes.
+template <typename T, int G, int W>
+__global__ __launch_bounds__(64) void embed_blocks_kernel(GradArgs a) {
+  constexpr int U = G < 16 ? G : 16;
+  const Place p = place_of<G, W>(a.e, a.first);
+  const int lane = threadIdx.x % G;
+  const int64_t block = p.block * (64 / G) + threadIdx.x / G;
+  if (block >= a.blocks) return;
+  const int64_t begin = block * a.length;
+  const int64_t end = begin + a.length < a.pairs ? begin + a.length : a.pairs;
+  const uint32_t none = 0xFFFFFFFFu;
+  const uint32_t key_before = begin > 0 ? a.sorted[begin - 1].key : none;
+  const uint32_t key_after = end < a.pairs ? a.sorted[end].key : none;
+  const T *grad = (const T *)a.e.table + p.column;
+  float sum[W];
+  uint32_t key = key_before;
+  bool goes_on = true;  // from the block before
+  auto hand_on = [&](bool further) __attribute__((always_inline)) {
+    if (key < (uint32_t)a.e.n_entries && p.inside) {
+      if (goes_on || further) {
+        __builtin_memcpy(
+            a.partial + (2 * block + !goes_on) * (int64_t)a.e.n_features + p.column, sum,
+            sizeof(sum));
       } else {
-        hi = mid;
+        float v[W];
+#pragma unroll
+        for (int k = 0; k < W; ++k) v[k] = sum[k] * a.e.scale;
+        store_elements<T, W>((T *)a.e.out + (int64_t)key * a.e.ldo + p.column, v);
       }
     }
-    start[t] = (uint32_t)lo;
+  };
+  for (int64_t i0 = begin; i0 < end; i0 += U) {
+    Pair mine = {none, 0};
+    if (lane < U && i0 + lane < end) mine = a.sorted[i0 + lane];
+    uint32_t keys[U];
+    Elements<T, W> e[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      keys[u] = of_lane<G>(mine.key, u);
+      const uint32_t row = of_lane<G>(mine.row, u);
+      e[u].clear();
+      if (keys[u] < (uint32_t)a.e.n_entries) e[u].load(grad + (int64_t)row * a.e.ldt);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (i0 + u >= end) break;
+      if (keys[u] != key || (i0 == begin && u == 0)) {
+        if (i0 > begin || u > 0) hand_on(false);
+        goes_on = keys[u] == key_before && i0 == begin && u == 0;
+        key = keys[u];
+#pragma unroll
+        for (int k = 0; k < W; ++k) sum[k] = 0.0f;
+      }
+#pragma unroll
+      for (int k = 0; k < W; ++k) sum[k] += e[u].at(k);
+    }
+  }
+  hand_on(key == key_after);
+}
+
+// Entries of several blocks: the block where one begins has its first sum, the blocks after it one
+// each.  A workgroup looks at kHeads blocks; a group of lanes adds the sums of a short entry, all
+// groups together those of a long one.
+constexpr int kHeads = 16, kShort = 32;
+template <typename T, int G, int W>
+__global__ __launch_bounds__(kThreads) void embed_join_kernel(GradArgs a) {
+  constexpr int groups = kThreads / G;
+  __shared__ int32_t last[kHeads];  // blocks after the one where an entry begins; 0: none begins
+  __shared__ uint32_t entry[kHeads];
+  __shared__ float join[kThreads * W];
+  const Place p = place_of<G, W>(a.e, a.first);
+  const int group = threadIdx.x / G, width = a.e.n_features;
+  const int64_t block0 = p.block * kHeads;
+  if (threadIdx.x < kHeads) {
+    const int64_t block = block0 + threadIdx.x, end = (block + 1) * a.length;
+    int32_t count = 0;
+    uint32_t key = 0;
+    if (end < a.pairs) {
+      key = a.sorted[end - 1].key;
+      const int64_t begin = block * a.length;
+      if (key < (uint32_t)a.e.n_entries && a.sorted[end].key == key &&
+          (begin == 0 || a.sorted[begin - 1].key != key)) {
+        // the last block that begins with the entry: in growing steps, then by halves
+        int64_t lo = block + 1, step = 1;
+        while (lo + step < a.blocks && a.sorted[(lo + step) * a.length].key == key) {
+          lo += step;
+          step *= 2;
+        }
+        int64_t hi = lo + step < a.blocks ? lo + step : a.blocks;  // the first that does not, or later
+        while (hi - lo > 1) {
+          const int64_t mid = (lo + hi) / 2;
+          if (a.sorted[mid * a.length].key == key) {
+            lo = mid;
+          } else {
+            hi = mid;
+          }
+        }
+        count = (int32_t)(lo - block);
+      }
+    }
+    last[threadIdx.x] = count;
+    entry[threadIdx.x] = key;
   }
   __syncthreads();
-  if (!p.inside) return;
-  const T *grad = (const T *)a.e.table + p.column;
-  T *out = (T *)a.e.out + p.column;
-  const int width = a.e.n_features;
-  for (int t = threadIdx.x / G; t < e1 - e0; t += groups) {
+  // sum += those of blocks [c, end)
+  auto add = [&](float(&sum)[W], int64_t c, int64_t end) {
+    for (; c < end; c += kAhead) {
+      float v[kAhead][W];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        __builtin_memcpy(v[u],
+                         a.partial + 2 * (c + u < end ? c + u : c) * (int64_t)width + p.column,
+                         sizeof(v[u]));
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+        for (int k = 0; k < W; ++k) sum[k] += c + u < end ? v[u][k] : 0.0f;
+    }
+  };
+  auto finish = [&](float(&sum)[W], int h) {
+    if (!p.inside) return;
+#pragma unroll
+    for (int k = 0; k < W; ++k) sum[k] *= a.e.scale;
+    store_elements<T, W>((T *)a.e.out + (int64_t)entry[h] * a.e.ldo + p.column, sum);
+  };
+  for (int h = group; h < kHeads; h += groups) {
+    if (last[h] == 0 || last[h] > kShort) continue;
+    const int64_t block = block0 + h;
+    float sum[W];
+    __builtin_memcpy(sum, a.partial + (2 * block + 1) * (int64_t)width + p.column, sizeof(sum));
+    add(sum, block + 1, block + 1 + last[h]);
+    finish(sum, h);
+  }
+  for (int h = 0; h < kHeads; ++h) {
+    if (last[h] <= kShort) continue;  // of the whole workgroup
+    const int64_t block = block0 + h, share = (last[h] + groups - 1) / groups;
+    const int64_t c = block + 1 + group * share, end = block + 1 + last[h];
     float sum[W];
 #pragma unroll
     for (int k = 0; k < W; ++k) sum[k] = 0.0f;
-    const int64_t i0 = start[t], i1 = start[t + 1];
-    const int64_t c0 = (i0 + kChunk - 1) / kChunk, c1 = i1 / kChunk;  // whole chunks
-    if (c0 >= c1) {
-      add_rows<T, W>(sum, a, grad, i0, i1);
-    } else {
-      add_rows<T, W>(sum, a, grad, i0, c0 * kChunk);
-      const int64_t s0 = (c0 + kChunk - 1) / kChunk, s1 = c1 / kChunk;
-      const float *chunk = a.chunk + p.column;
-      if (s0 >= s1) {
-        add_sums<W>(sum, chunk, width, c0, c1);
-      } else {
-        add_sums<W>(sum, chunk, width, c0, s0 * kChunk);
-        add_sums<W>(sum, a.super + p.column, width, s0, s1);
-        add_sums<W>(sum, chunk, width, s1 * kChunk, c1);
-      }
-      add_rows<T, W>(sum, a, grad, c1 * kChunk, i1);
-    }
+    if (group == 0)
+      __builtin_memcpy(sum, a.partial + (2 * block + 1) * (int64_t)width + p.column, sizeof(sum));
+    add(sum, c, c + share < end ? c + share : end);
 #pragma unroll
-    for (int k = 0; k < W; ++k) sum[k] *= a.e.scale;
-    store_elements<T, W>(out + (e0 + t) * a.e.ldo, sum);
+    for (int k = 0; k < W; ++k) join[k * kThreads + threadIdx.x] = sum[k];
+    __syncthreads();
+    if (group == 0) {
+      for (int q = 1; q < groups; ++q)
+#pragma unroll
+        for (int k = 0; k < W; ++k) sum[k] += join[k * kThreads + threadIdx.x + q * G];
+      finish(sum, h);
+    }
+    __syncthreads();
   }
 }
 
 // The workspace's parts, each from a multiple of 16 bytes.
 struct Parts {
-  int64_t keys[2], rows[2], counts, totals, chunk, super, bytes;
+  int64_t pairs[2], counts, totals, partial, bytes;
 };
 static Parts parts_of(const SortPlan &p, int64_t width) {
   Parts w;
@@ -514,74 +756,75 @@ static Parts parts_of(const SortPlan &p, int64_t width) {
     at += (words * 4 + 15) / 16 * 16;
     return begin;
   };
-  for (int i = 0; i < 2; ++i) w.keys[i] = take(p.pairs), w.rows[i] = take(p.pairs);
-  w.counts = take(p.tiles << p.bits);
-  w.totals = take(int64_t(1) << p.bits);
-  w.chunk = take(p.chunks * width);
-  w.super = take(p.supers * width);
+  w.pairs[0] = take(2 * p.pairs);
+  w.pairs[1] = p.few ? w.pairs[0] : take(2 * p.pairs);
+  w.counts = take(p.few ? 0 : p.tiles << p.bits);
+  w.totals = take(p.few ? 0 : int64_t(1) << p.bits);
+  w.partial = take(p.blocks * 2 * width);
   w.bytes = at;
   return w;
 }
 
 int64_t embed_backward_bytes(int64_t n_rows, int32_t n_slots, int32_t n_entries,
                              int32_t n_features) {
-  return parts_of(plan_of(n_rows * n_slots, n_entries), n_features).bytes;
+  const SortPlan p = plan_of(n_rows * n_slots, n_entries, n_features);
+  return parts_of(p, n_features).bytes;
 }
 
 int launch_embed_backward(const EmbedArgs &args, int32_t dtype, void *stream) {
-  const SortPlan plan = plan_of(args.n_rows * args.n_slots, args.n_entries);
+  const SortPlan plan = plan_of(args.n_rows * args.n_slots, args.n_entries, args.n_features);
   const Parts parts = parts_of(plan, args.n_features);
   char *ws = (char *)args.workspace;
-  uint32_t *keys[2], *rows[2];
-  for (int i = 0; i < 2; ++i) {
-    keys[i] = (uint32_t *)(ws + parts.keys[i]);
-    rows[i] = (uint32_t *)(ws + parts.rows[i]);
-  }
   GradArgs a = {};
   a.e = args;
   a.pairs = plan.pairs;
   a.tiles = plan.tiles;
   a.counts = (uint32_t *)(ws + parts.counts);
   a.totals = (uint32_t *)(ws + parts.totals);
-  a.chunk = (float *)(ws + parts.chunk);
-  a.super = (float *)(ws + parts.super);
-  a.chunks = plan.chunks;
-  a.supers = plan.supers;
+  a.partial = (float *)(ws + parts.partial);
+  a.blocks = plan.blocks;
+  a.length = plan.length;
   a.bits = plan.bits;
+  a.passes = plan.passes;
+  a.bytes = dtype == BRIDGER_F32 ? 4 : 2;
+  const int64_t out_bytes = (int64_t)args.n_entries * args.n_features * a.bytes;
+  auto fill_of = [&](int threads) {  // 64 bytes or more a lane
+    const int64_t n = (out_bytes + threads * 64 - 1) / (threads * 64);
+    const int64_t most = 2048 * 256 / threads;
+    return (int)(n < most ? n : most);
+  };
   int err = 0;
-  for (int pass = 0; pass < plan.passes && plan.pairs; ++pass) {
+  if (plan.few) {
+    a.fill = fill_of(kFewThreads);
+    a.to = (Pair *)(ws + parts.pairs[0]);
+    err = launch(embed_group_kernel, kBuckets + (int64_t)a.fill, kFewThreads, 0, a, stream);
+    a.sorted = a.to;
+  }
+  for (int pass = 0; pass < plan.passes && !plan.few; ++pass) {
     a.shift = pass * plan.bits;
-    a.keys_to = keys[pass & 1];
-    a.rows_to = rows[pass & 1];
-    err = launch_blocks(embed_count_kernel, a.tiles, kThreads, a, stream);
+    a.to = (Pair *)(ws + parts.pairs[pass & 1]);
+    a.fill = pass == 0 ? fill_of(kThreads) : 0;
+    err = launch_blocks(embed_count_kernel, a.tiles + a.fill, kThreads, a, stream);
     if (!err) {
       const int waves = kThreads / 64;
       err = launch(embed_scan_kernel, ((1 << a.bits) + waves - 1) / waves, kThreads, 0, a, stream);
     }
     if (!err) err = launch_blocks(embed_move_kernel, a.tiles, kThreads, a, stream);
     if (err) return err;
-    a.keys = a.keys_to;
-    a.rows = a.rows_to;
+    a.sorted = a.to;
   }
+  if (err || !plan.pairs) return err;
   return with_type(dtype, [&](auto t) {
     using T = decltype(t);
     return with_lanes<T>(args.n_features, [&](auto lanes, auto elements) {
       constexpr int G = decltype(lanes)::value, W = decltype(elements)::value;
-      constexpr int groups = kThreads / G;
       GradArgs g = a;
       g.e.tiles = tiles_of(g.e.n_features, G, W);
-      int e = 0;
-      auto blocks = [&](int64_t n) { return (n + groups - 1) / groups * g.e.tiles; };
-      if (g.chunks) e = launch_blocks(embed_chunk_kernel<T, G, W>, blocks(g.chunks), kThreads, g, stream);
-      if (!e && g.supers)
-        e = launch_blocks(embed_super_kernel<G, W>, blocks(g.supers), kThreads, g, stream);
-      if (e) return e;
-      // several entries a group where the chip is full without
-      g.each = 1;
-      while (g.each * groups < 64 && (int64_t)g.e.n_entries * g.e.tiles > (int64_t)g.each * groups * 4096)
-        g.each *= 2;
-      const int64_t n = groups * g.each;
-      return launch_blocks(embed_entries_kernel<T, G, W>, (g.e.n_entries + n - 1) / n * g.e.tiles,
+      const int64_t at_once = 64 / G;
+      const int e = launch_blocks(embed_blocks_kernel<T, G, W>,
+                                  (g.blocks + at_once - 1) / at_once * g.e.tiles, 64, g, stream);
+      if (e || g.blocks == 1) return e;
+      return launch_blocks(embed_join_kernel<T, G, W>, (g.blocks + kHeads - 1) / kHeads * g.e.tiles,
                            kThreads, g, stream);
     });
   });

@@ -145,8 +145,8 @@ def test_embed_grad_many_rows_of_one_entry(n):
 
 
 def test_embed_grad_order():
-    """Sums in the order of the rows: equal bits whatever else runs, and those of a sum in order
-    where an entry has few rows."""
+    """Sums in an order that the ids decide: equal bits every time, and the sums of two rows rounded
+    once."""
     ids = _ids(3, 5000, 1, [900], empty=0.0)[:, 0]
     grad = _normal(4, 5000, 24)
     first = B.embed_grad(ids, grad, 900)
@@ -156,7 +156,7 @@ def test_embed_grad_order():
     g, at, count = grad.cpu().numpy(), ids.cpu().numpy(), np.bincount(ids.cpu().numpy(), minlength=900)
     for r in range(5000):
         want[at[r]] += g[r]
-    few = count <= 32
+    few = count <= 2
     assert np.array_equal(first.cpu().numpy()[few], want[few])
 
 
