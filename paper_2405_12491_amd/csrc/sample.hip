@@ -3,33 +3,87 @@
 
 namespace bridger {
 
-// 2^x, x <= 0: 2^n times the series of e^(f ln 2), |f| <= 1/2, whose rest is below 7e-15 of it.  A
-// draw compares sums of these with a random number, so they are held in double.
-__device__ inline double exp2_of(double x) {
-  if (!(x > -1100.0)) return 0.0;
-  const double n = __builtin_rint(x), f = x - n;
-  double s = 7.0549116208011233e-09;  // (ln 2)^k / k!, k = 11 to 0
-  s = __builtin_fma(s, f, 1.0178086009239699e-07);
-  s = __builtin_fma(s, f, 1.3215486790144309e-06);
-  s = __builtin_fma(s, f, 1.5252733804059840e-05);
-  s = __builtin_fma(s, f, 1.5403530393381610e-04);
-  s = __builtin_fma(s, f, 1.3333558146428443e-03);
-  s = __builtin_fma(s, f, 9.6181291076284772e-03);
-  s = __builtin_fma(s, f, 5.5504108664821580e-02);
-  s = __builtin_fma(s, f, 2.4022650695910071e-01);
-  s = __builtin_fma(s, f, 6.9314718055994531e-01);
-  s = __builtin_fma(s, f, 1.0);
-  return __builtin_ldexp(s, (int)n);
+// A value that all lanes agree on, in scalar registers.
+__device__ inline uint32_t uniform(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
 }
+__device__ inline double uniform(double v) {
+  const uint2 w = __builtin_bit_cast(uint2, v);
+  return __builtin_bit_cast(double, make_uint2(uniform(w.x), uniform(w.y)));
+}
+__device__ inline float uniform(float v) { return __uint_as_float(uniform(__float_as_uint(v))); }
+
+// A row's weights, e^((v - top) / T): 2^n times a polynomial in f, n + f = (v - top) log2(e) / T, |f| <=
+// 1/2, that meets 2^f at eleven Chebyshev points and is off by at most 3.2e-16 of it; 1 for the largest,
+// 0 below 2^-1075.  A draw compares sums of these with a random number, so they are held in double.
+struct Weights {
+  double top, factor;  // log2(e) / T
+  double last;         // v - top of weight 0
+  __device__ Weights(float top, double factor)
+      : top(uniform((double)top)), factor(uniform(factor)), last(uniform(-1100.0 / factor)) {}
+  // (a score of +infinity is its row's largest)
+  __device__ double operator()(float v) const {
+    return (double)v == top ? 1.0 : of((double)v - top);
+  }
+  __device__ double of(double d) const {
+    double w[1];
+    of<1>({d}, w);
+    return w[0];
+  }
+  // N at a time, step by step: one alone waits for its own results (1 x 128,000 unfiltered: XX us).
+  template <int N>
+  __device__ void of(const double (&d)[N], double (&w)[N]) const {
+    constexpr double round = 0x1.8p52;  // leaves whole numbers, in the lower word
+    constexpr double c[] = {1.0208690299958306e-07, 1.321544258792169e-06, 1.5252657260200837e-05,
+                            0.0001540353044173605,  0.0013333558230164974, 0.009618129107606888,
+                            0.05550410866444772,    0.24022650695910097,   0.69314718055995, 1.0};
+    double t[N], f[N], s[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const double x = fmax(d[i], last);  // (NaN: last)
+      t[i] = __builtin_fma(x, factor, round);
+      f[i] = __builtin_fma(x, factor, round - t[i]);
+      s[i] = 7.072585949269223e-09;
+    }
+#pragma unroll
+    for (int k = 0; k < 10; ++k) {
+      double ck = c[k];
+      asm("" : "+s"(ck));  // (in vector registers it would take a copy, too)
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i] = __builtin_fma(s[i], f[i], ck);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      w[i] = __builtin_ldexp(s[i], (int)(uint32_t)__builtin_bit_cast(uint64_t, t[i]));
+  }
+  // The sum of the weights of four scores, those that are `in`.
+  __device__ double sum(const float (&v)[4], const bool (&in)[4]) const {
+    double d[4], w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      d[i] = in[i] ? (double)v[i] - top : last;
+      d[i] = (double)v[i] == top && in[i] ? 0.0 : d[i];
+    }
+    of<4>(d, w);
+    return (w[0] + w[1]) + (w[2] + w[3]);
+  }
+};
 
 template <int G>
 constexpr int kSorted = G >= 1024 ? 2048 : G > 64 ? 1024 : 512;  // candidates that LDS holds
 
 constexpr int kSegments = 16;  // of a row, whose sums the draw keeps
+constexpr int kBins = 8;       // of a range that a cut is looked for in
 
 template <int G>
 struct SampleShared {
-  uint64_t key[kSorted<G>];
+  union {
+    uint64_t key[kSorted<G> + 8];
+    struct {  // a lane's weights and numbers of scores
+      double weight[kBins][G];
+      int count[kBins][G];
+    } bin;
+  };
   double segment[kSegments][G / 64];
   double part[kSegments];
   double wave[2][G / 64];
@@ -109,14 +163,15 @@ __device__ inline void each_score(u32x4 raw, F f) {
   }
 }
 
-// A row's weights: e^((v - top) / T), 1 for the largest.
-struct Weights {
-  float top;
-  double factor;  // log2(e) / T
-  __device__ double operator()(float v) const {
-    return v == top ? 1.0 : exp2_of(((double)v - (double)top) * factor);
+// The same, four at a time: f(scores, the first one's place).
+template <typename T, typename F>
+__device__ inline void each_four(u32x4 raw, F f) {
+#pragma unroll 1
+  for (int i = 0; i < kPerLoad<T>; i += 4) {
+    f({element<T>(raw, 0), element<T>(raw, 1), element<T>(raw, 2), element<T>(raw, 3)}, i);
+    raw = u32x4{raw[2], raw[3], 0, 0};
   }
-};
+}
 
 // ---------------------------------------------------------------------------- candidates
 // Scores of [lo, up) in the order that `kept` keeps go to the candidates; their number (it may pass
@@ -133,25 +188,61 @@ __device__ inline int collect(Source &x, SampleShared<G> &s, Keep kept, uint32_t
 #pragma unroll
     for (int i = 1; i < V; ++i) top = fmaxf(top, element<T>(raw, i));
     if (top >= low) {
-      each_score<T>(raw, [&](float v, int i) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float v = element<T>(raw, i);
         if (v >= low && order_of(v) < up && kept(v, j + i)) {
           const int at = atomicAdd(&s.count, 1);
           if (at < kSorted<G>) s.key[at] = key_of(v, j + i);
         }
-      });
+      }
     }
   });
   __syncthreads();
   return s.count;
 }
 
-// Sorts the first `count` candidates, the largest first (zeros behind): compare and exchange over a
-// network of the next power of two.
+// Sorts the first `count` candidates, the largest first (some zeros behind).  Few: each goes where as
+// many larger ones say.  More: compare and exchange over a network of the next power of two.
 template <int G>
 __device__ inline void sort_candidates(SampleShared<G> &s, int count) {
+  constexpr int E = G < 256 ? 256 / G : 1, most = G < 256 ? 256 : G < 512 ? G : 512;
+  __syncthreads();
+  if (count <= most) {
+    if (threadIdx.x < 8) s.key[count + threadIdx.x] = 0;
+    __syncthreads();
+    uint64_t mine[E];
+    int larger[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int t = e * G + threadIdx.x;
+      if (e * G < count) {
+        mine[e] = s.key[t < count ? t : count];
+        larger[e] = 0;
+      }
+    }
+    if ((threadIdx.x & ~63) < count)
+#pragma unroll 1
+      for (int q = 0; q < count; q += 8) {  // four loads on their way at once
+        ulonglong2 other[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) other[i] = *(const ulonglong2 *)&s.key[q + 2 * i];
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (e * G < count)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              larger[e] += (other[i].x > mine[e]) + (other[i].y > mine[e]);
+      }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (e * G + (int)threadIdx.x < count) s.key[larger[e]] = mine[e];
+    __syncthreads();
+    return;
+  }
   int size = 64;
   while (size < count) size *= 2;
-  __syncthreads();
   for (int t = count + threadIdx.x; t < size; t += G) s.key[t] = 0;
 #pragma unroll 1
   for (int run = 2; run <= size; run *= 2)
@@ -197,74 +288,120 @@ struct Listed {
 };
 
 // ------------------------------------------------------------------- cuts of whole rows
-// The general way to a row's target-th score in the order (by weight: to the last one before which
-// less than `target` of the weight stands): halves the range [lo, up) that holds it, `base` being
-// what reaches up, until LDS holds it or one score is left, that of many classes.  Its walks read the
-// row from memory again: held in registers they would make up most of the code.
+// A row in memory, as InMemory, with the next load on its way while one is looked at.
 template <typename T, int G>
-__device__ inline void cut(InMemory<T, G> &x, SampleShared<G> &s, Kept &kept, const Weights &weight,
-                           bool by_weight, double target) {
-  const uint32_t lowest = order_of(-__builtin_inff()) + 1;
-  uint32_t lo = lowest, up = order_of(weight.top) + 1;
-  double base = 0.0;
-  while (lo < up) {
-    const uint32_t middle = lo + (up - lo) / 2;
-    const int count = collect<T, G>(x, s, kept, middle, up);
-    const float v = value_of(middle);
-    double reach = base + count;
-    if (count <= kSorted<G>) {
-      sort_candidates<G>(s, count);
-      int stay = target - base < count ? (int)(target - base) : count;
-      if (by_weight) {
-        const Listed<G> l(s, count, weight, 32);
-        stay = l.leading(s, count, target - base);
-        reach = base + l.all;
-      }
-      if (count && (reach >= target || middle == lo)) {
+struct Streamed {
+  static constexpr int kStep = 1;
+  const T *row;
+  int n;
+  __device__ Streamed(const T *row, int n) : row(row), n(n) {}
+  template <typename F>
+  __device__ void each(F f) {
+    constexpr int V = kPerLoad<T>;
+    const T nan = (T)__builtin_nanf("");
+    auto at = [&](int64_t j0) {
+      const int64_t j = j0 + (int64_t)threadIdx.x * V;
+      return (int)(j < n ? j : n);
+    };
+    RowLoad<T> next;
+    if (n < V) {
+      next.tiny(row, at(0), n, nan);
+      f(at(0), next.raw);
+      return;
+    }
+    next.issue(row, at(0), n);
+#pragma unroll 1
+    for (int64_t j0 = 0; j0 < n; j0 += G * V) {
+      RowLoad<T> l = next;
+      if (j0 + G * V < n) next.issue(row, at(j0 + G * V), n);
+      l.take(at(j0), n, fill_of(nan));
+      f(at(j0), l.raw);
+    }
+  }
+};
+
+// The general way to a row's target-th score in the order (by weight: to the last one before which
+// less than `target` of the weight stands), of those of order `lo` or more: parts the range [lo, up)
+// that holds it into kBins, until LDS holds the range or one score is left, that of many classes.  Its
+// walks read the row from memory again: held in registers they would make up most of the code.
+struct Range {
+  uint32_t lo, up;
+  double base;  // the measure of what reaches up
+  int within;   // classes in the range (INT32_MAX: not known)
+};
+template <typename T, int G>
+__device__ inline void cut(Streamed<T, G> &x, SampleShared<G> &s, Kept &kept, const Weights &weight,
+                           const Range &range, bool by_weight, double target) {
+  uint32_t lo = range.lo, up = range.up;
+  double base = range.base;
+  int within = range.within;
+  for (;;) {
+    const bool one = up - lo == 1;
+    if (one || within <= kSorted<G>) {
+      const int count = collect<T, G>(x, s, kept, lo, up);
+      if (count == 0) return;  // all of it stays: rounding leaves the target past the last
+      if (count <= kSorted<G>) {
+        sort_candidates<G>(s, count);
+        int stay = target - base < count ? (int)(target - base) : count;
+        if (by_weight) stay = Listed<G>(s, count, weight, 32).leading(s, count, target - base);
         const uint64_t key = s.key[stay > 0 ? stay - 1 : 0];
         kept.score = value_of((uint32_t)(key >> 32));
         kept.cls = class_of(key);
         return;
       }
-    } else if (up - middle == 1) {
-      const double one = by_weight ? weight(v) : 1.0;
-      reach = base + count * one;
-      if (reach >= target || middle == lo) {
-        double want = __builtin_ceil((target - base) / one);  // of its classes
-        if (!(want >= 1.0)) want = 1.0;
-        int32_t cls = 0;
-        for (int bit = 30; bit >= 0; --bit) {  // the largest class with fewer than those before it
-          const int32_t next = cls | 1 << bit;
-          int below = 0;
-          x.each([&](int j, const u32x4 &raw) __attribute__((always_inline)) {
-            each_score<T>(raw, [&](float e, int i) {
-              below += e == v && j + i < next && kept(e, j + i);
-            });
+    }
+    if (one) {
+      const float v = value_of(lo);
+      double want = __builtin_ceil((target - base) / (by_weight ? weight(v) : 1.0));
+      if (!(want >= 1.0)) want = 1.0;  // of its classes
+      int32_t cls = 0;
+      for (int bit = 30; bit >= 0; --bit) {  // the largest class with fewer than those before it
+        const int32_t next = cls | 1 << bit;
+        int below = 0;
+        x.each([&](int j, const u32x4 &raw) __attribute__((always_inline)) {
+          each_score<T>(raw, [&](float e, int i) {
+            below += e == v && j + i < next && kept(e, j + i);
           });
-          if ((double)sum_all<G>(below, s.found) < want) cls = next;
-        }
-        kept.score = v;
-        kept.cls = cls;
-        return;
-      }
-    } else if (by_weight) {
-      double w = 0.0;
-      x.each([&](int j, const u32x4 &raw) __attribute__((always_inline)) {
-        each_score<T>(raw, [&](float e, int i) {
-          if (e >= v && order_of(e) < up && kept(e, j + i)) w += weight(e);
         });
+        if ((double)sum_all<G>(below, s.found) < want) cls = next;
+      }
+      kept.score = v;
+      kept.cls = cls;
+      return;
+    }
+    int shift = 0;
+    while ((up - 1 - lo) >> shift >= kBins) ++shift;
+    const int bins = (int)((up - 1 - lo) >> shift) + 1;
+    __syncthreads();
+    for (int b = 0; b < bins; ++b) {
+      s.bin.weight[b][threadIdx.x] = 0.0;
+      s.bin.count[b][threadIdx.x] = 0;
+    }
+    x.each([&](int j, const u32x4 &raw) __attribute__((always_inline)) {
+      each_score<T>(raw, [&](float e, int i) {
+        const uint32_t o = order_of(e);
+        if (o >= lo && o < up && kept(e, j + i)) {
+          const uint32_t b = (o - lo) >> shift;
+          s.bin.count[b][threadIdx.x] += 1;
+          if (by_weight) s.bin.weight[b][threadIdx.x] += weight(e);
+        }
       });
-      reach = base + sum_all<G>(w, s.wave[0]);
-    }
-    if (reach >= target) {
-      if (middle == lo) return;  // (not reached: a range of one score is settled above)
-      lo = middle;
-    } else {
+    });
+    // from the largest scores down: the bin that reaches the target, or the last
+    int b = bins;
+    double reach = base;
+    do {
+      --b;
       base = reach;
-      up = middle;
-    }
+      within = sum_all<G>(s.bin.count[b][threadIdx.x], s.found);
+      reach += by_weight ? sum_all<G>(s.bin.weight[b][threadIdx.x], s.wave[0]) : (double)within;
+    } while (reach < target && b > 0);
+    const uint32_t begin = lo + ((uint32_t)b << shift);
+    const uint64_t end = (uint64_t)begin + (uint64_t(1) << shift);
+    up = end < up ? (uint32_t)end : up;
+    lo = begin;
+    __syncthreads();  // the bins are read
   }
-  // all of it stays: rounding leaves the target past the last
 }
 
 // ------------------------------------------------------------------------------- draws
@@ -280,8 +417,9 @@ __device__ inline double weigh_row(Source &x, SampleShared<G> &s, Keep kept, con
   int step = 0, segment = 0, within = 0;
   double sum = 0.0;
   x.each([&](int j, const u32x4 &raw) __attribute__((always_inline)) {
-    each_score<T>(raw, [&](float v, int i) {
-      if (kept(v, j + i)) sum += weight(v);
+    each_four<T>(raw, [&](const float(&v)[4], int i) {
+      sum += weight.sum(v, {kept(v[0], j + i), kept(v[1], j + i + 1), kept(v[2], j + i + 2),
+                            kept(v[3], j + i + 3)});
     });
     ++step;
     if (++within == each || step == steps) {
@@ -340,8 +478,9 @@ __device__ inline void draw_row(const SampleArgs &a, int64_t row, SampleShared<G
       l.take(j, n, fill_of((T)__builtin_nanf("")));
     }
     double mine = 0.0, total;
-    each_score<T>(l.raw, [&](float v, int i) {
-      if (kept(v, j + i)) mine += weight(v);
+    each_four<T>(l.raw, [&](const float(&v)[4], int i) {
+      mine += weight.sum(v, {kept(v[0], j + i), kept(v[1], j + i + 1), kept(v[2], j + i + 2),
+                             kept(v[3], j + i + 3)});
     });
     double at = start + lanes_before<G>(mine, s.sum, &total);
     start += total;
@@ -399,23 +538,25 @@ __device__ inline void draw_listed(const SampleArgs &a, int64_t row, SampleShare
 }
 
 // The lowest class of the largest score.
-template <typename T, int G>
-__device__ inline void first_of(const SampleArgs &a, int64_t row, SampleShared<G> &s, float top) {
-  InMemory<T, G> x((const T *)a.logits + row * a.ld, a.n_classes);
+template <typename T, int G, typename Source>
+__device__ inline void first_of(Source &x, SampleShared<G> &s, float top) {
   if (threadIdx.x == 0) s.chosen = INT32_MAX;
   __syncthreads();
+  int first = INT32_MAX;
   x.each([&](int j, const u32x4 &raw) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = kPerLoad<T> - 1; i >= 0; --i)
-      if (element<T>(raw, i) == top) atomicMin(&s.chosen, j + i);
+      if (element<T>(raw, i) == top && j + i < first) first = j + i;
   });
+  if (first < INT32_MAX) atomicMin(&s.chosen, first);
   __syncthreads();
   if (threadIdx.x == 0) s.cls = s.chosen, s.share = 1.0;
 }
 
 // What stays is found as a list of candidates in LDS wherever that holds it, and drawn from there; a
 // row without cuts is drawn from the sums of its segments, the rest (more kept classes than LDS
-// holds) from memory.
+// holds, cuts too near to call from quick sums) from memory.  Each walk over the registers stands here
+// once: they are written out, load after load.
 template <typename T, int G, typename Source>
 __device__ inline void sample_row(const SampleArgs &a, int64_t row, Source &x,
                                   SampleShared<G> &s) {
@@ -426,11 +567,39 @@ __device__ inline void sample_row(const SampleArgs &a, int64_t row, Source &x,
   const int k = a.top_ks ? a.top_ks[row] : a.top_k;
   const double p = a.top_ps ? (double)a.top_ps[row] : a.top_p;
   const double m = a.min_ps ? (double)a.min_ps[row] : a.min_p;
+  const bool by_k = k > 0 && k < a.n_classes, by_p = p < 1.0;
+  if (temperature > 1e6) temperature = 1e6;
+  const double factor = uniform(1.4426950408889634 / temperature);
   float most = -inf;  // of the lane
-  x.each([&](int, const u32x4 &raw) __attribute__((always_inline)) {
+  // The sum of its weights relative to its first load's largest, and of each times its exponent's size,
+  // in quick floats: exact enough for most cuts by top_p, and done while the row's loads arrive.
+  float from_score = 0.0f, lane_size = 0.0f;
+  double lane_all = 0.0;
+  if (by_p && !by_k) {
+    const float high = (float)factor, low = (float)(factor - (double)high);
+    bool first = true;
+    x.each([&](int, const u32x4 &raw) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) most = fmaxf(most, element<T>(raw, i));
-  });
+      for (int i = 0; i < V; ++i) most = fmaxf(most, element<T>(raw, i));
+      if (first && most > -inf) from_score = most;
+      first = false;
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float d = element<T>(raw, i) - from_score;
+        const float e = fmaxf(__builtin_fmaf(d, low, d * high), -200.0f);  // (NaN: no weight)
+        const float w = __builtin_amdgcn_exp2f(e);
+        sum += w;
+        lane_size = __builtin_fmaf(w, fabsf(e), lane_size);
+      }
+      lane_all += (double)sum;
+    });
+  } else {
+    x.each([&](int, const u32x4 &raw) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) most = fmaxf(most, element<T>(raw, i));
+    });
+  }
   float top = lanes_reduce<Max, 64>(most);
   if constexpr (G > 64) {
     if (lane == 0) s.bound[wave] = top;
@@ -438,108 +607,120 @@ __device__ inline void sample_row(const SampleArgs &a, int64_t row, Source &x,
     top = lanes_reduce<Max, W>(s.bound[threadIdx.x & (W - 1)]);
     __syncthreads();
   }
+  top = uniform(top);
   if (top == -inf) {  // nothing to draw from
     if (threadIdx.x == 0) s.cls = -1, s.share = 0.0;
     return;
   }
   if (!(temperature >= 1e-6) || k == 1 || p <= 0.0) {
-    first_of<T, G>(a, row, s, top);
+    first_of<T, G>(x, s, top);
     return;
   }
-  if (temperature > 1e6) temperature = 1e6;
-  const Weights weight = {top, 1.4426950408889634 / temperature};
+  const Weights weight(top, factor);
   const uint32_t lowest = order_of(-inf) + 1, all_up = order_of(top) + 1;
-  float least = value_of(lowest);  // what min_p leaves
-  if (m > 0.0) {
-    const double v = (double)top + temperature * log(m < 1.0 ? m : 1.0);
-    float f = (float)v;
-    if ((double)f < v) f = value_of(order_of(f) + 1);
-    least = f > least ? f : least;
-  }
+  // the order of the smallest score that is at least v
+  auto order_from = [&](double v) {
+    const float f = (float)v;
+    const uint32_t o = uniform(order_of(f) + ((double)f < v));
+    return o > lowest ? o : lowest;
+  };
+  // what min_p leaves
+  const uint32_t reach_m =
+      m > 0.0 ? order_from((double)top + temperature * log(m < 1.0 ? m : 1.0)) : lowest;
   const int steps = (int)(((int64_t)a.n_classes + G * V - 1) / (G * V));
   const int each = (steps + kSegments - 1) / kSegments;
-  auto valid = [&](float v, int) { return v >= value_of(lowest); };
-  auto stays = [&](float v, int) { return v >= least; };
-  // at least j lanes a wave, so W j classes, reach the j-th largest of their maxima
-  auto bound_of = [&](int j) {
-    float b = wave_jth(most, j);
+  Kept kept = {-inf, -inf, -1};
+  kept.floor = value_of(reach_m);
+  if (!by_k && !by_p && reach_m == lowest) {
+    const double all = weigh_row<T, G>(x, s, kept, weight, steps, each);
+    draw_row<T, G>(a, row, s, kept, weight, all, steps, each);
+    return;
+  }
+
+  // Where the candidates begin.  By top_p: the quick sum is off by 2^-23 times 1.1 of each weight's
+  // exponent (the difference, its product and the second one round by 2^-24 of it each, times ln 2), 2
+  // for the exponential and 4 for the sum of a load's weights, taken as 8.  Classes of a weight below
+  // (1 - p) all / n hold less than 1 - p of it together: no cut below.
+  uint32_t lo = by_k ? lowest : reach_m;
+  double all = 0.0, off = 0.0;
+  const bool quick = by_p && !by_k && lane_all <= 0x1p100;
+  if (by_p && !by_k) {
+    // (rows whose first scores say nothing of the others: infinite sums are not quick)
+    const double shift = ((double)from_score - (double)top) * factor;
+    const double down = Weights(0.0f, factor).of((double)from_score - (double)top);
+    const double lane_off = (double)lane_size + lane_all * fabs(shift);
+    const bool held = __all(quick && shift <= 60.0);  // (false for NaN)
+    all = held ? lane_all * down : (double)inf;
+    off = held ? lane_off * down : (double)inf;
+    all = uniform(sum_all<G>(all, s.wave[0]));
+    off = uniform(0x1p-23 * (1.2 * sum_all<G>(off, s.wave[1]) + 8.0 * all));
+    if (all < (double)inf && off < all) {
+      const uint32_t o =
+          order_from((double)top + temperature * (log((1.0 - p) * all / a.n_classes) - 1.0));
+      lo = o > lo ? o : lo;
+    } else {
+      all = off = (double)inf;
+    }
+  }
+  uint32_t from = lo;
+  const int share = by_k ? (k + W - 1) / W : 32;
+  if (by_k ? share <= 64 : by_p && a.n_classes > kSorted<G>) {
+    // at least that many lanes a wave, so W times as many classes, reach the wave's bound
+    float b = wave_jth(most, share);
     if constexpr (G > 64) {
       __syncthreads();
       if (lane == 0) s.bound[wave] = b;
       __syncthreads();
       b = -lanes_reduce<Max, W>(-s.bound[threadIdx.x & (W - 1)]);
     }
-    const uint32_t o = order_of(b);
-    return o > lowest ? o : lowest;
-  };
-  const bool by_k = k > 0 && k < a.n_classes, by_p = p < 1.0;
-  if (!by_k && !by_p) {
-    const double all = weigh_row<T, G>(x, s, stays, weight, steps, each);
-    draw_row<T, G>(a, row, s, stays, weight, all, steps, each);
-    return;
+    const uint32_t o = order_of(uniform(b));
+    from = o > from ? o : from;
   }
-  double all = 0.0;
-  if (!by_k) all = weigh_row<T, G>(x, s, valid, weight, steps, each);
-  const int share = by_k ? (k + W - 1) / W : 32;
-  const uint32_t bound =
-      (by_k ? share > 64 : a.n_classes <= kSorted<G>) ? lowest : bound_of(share);
-  int count = collect<T, G>(x, s, valid, bound, all_up);
-  InMemory<T, G> row_again((const T *)a.logits + row * a.ld, a.n_classes);
-  Kept kept = {-inf, least, -1};
+  int count = collect<T, G>(
+      x, s, [&](float v, int) { return true; }, from, all_up);
   bool listed = count <= kSorted<G>;
-  if (by_k) {
-    if (!listed) {
-      // (count of them reach the bound at least, more than LDS holds)
-      Kept all_of = {-inf, -inf, -1};
-      cut<T, G>(row_again, s, all_of, weight, false, (double)k);
-      kept.score = all_of.score;
-      kept.cls = all_of.cls;
-      all_of.floor = -inf;
-      if (k <= kSorted<G>) {
-        count = collect<T, G>(row_again, s, all_of, lowest, all_up);
-        listed = true;
-      }
-    }
-    if (listed) {
-      sort_candidates<G>(s, count);
-      if (count > k) count = k;
-      if (by_p) {
-        const Listed<G> l(s, count, weight, 32);
-        count = l.leading(s, count, p * l.all);
-      }
-    } else if (by_p) {
-      Kept of_k = {kept.score, -inf, kept.cls};
-      all = weigh_row<T, G>(row_again, s, of_k, weight, steps, each);
-      cut<T, G>(row_again, s, of_k, weight, true, p * all);
-      kept.score = of_k.score;
-      kept.cls = of_k.cls;
-    }
-  } else {
-    if (listed) {
-      sort_candidates<G>(s, count);
+  Range range = {lo, all_up, 0.0, INT32_MAX};  // where a general cut by top_p is looked for
+  if (listed) {
+    sort_candidates<G>(s, count);
+    if (by_k && count > k) count = k;
+    if (by_p) {
       const Listed<G> l(s, count, weight, 32);
-      const double target = p * all;
-      listed = l.all >= target || bound == lowest;
-      if (listed) count = l.leading(s, count, target);
-    }
-    if (!listed) {
-      Kept all_of = {-inf, -inf, -1};
-      cut<T, G>(row_again, s, all_of, weight, true, p * all);
-      kept.score = all_of.score;
-      kept.cls = all_of.cls;
+      if (by_k) all = l.all;
+      const double least = p * (all - off), greatest = p * (all + off);
+      if (off >= all) {
+        listed = false;
+      } else if (l.all >= greatest || from == lo) {
+        const int stay = l.leading(s, count, least);
+        if (off > 0.0 && stay != l.leading(s, count, greatest)) {
+          listed = false;
+          range = {from, all_up, 0.0, count};
+        }
+        count = stay;
+      } else {
+        listed = false;
+        if (l.all < least) range.up = from, range.base = l.all;
+      }
     }
   }
   if (listed) {
-    if (m > 0.0) {
-      int reach = 0;
-      for (int t = threadIdx.x; t < count; t += G)
-        reach += value_of((uint32_t)(s.key[t] >> 32)) >= least;
-      count = sum_all<G>(reach, s.found);
+    int reach = 0;  // min_p
+    for (int t = threadIdx.x; t < count; t += G) reach += (uint32_t)(s.key[t] >> 32) >= reach_m;
+    draw_listed<G>(a, row, s, sum_all<G>(reach, s.found), weight);
+    return;
+  }
+  // top_k, then top_p of what that keeps, then the draw
+  Streamed<T, G> again((const T *)a.logits + row * a.ld, a.n_classes);
+  for (int turn = by_k ? 0 : 1; turn < 3; ++turn) {
+    if (turn == 1 && !by_p) continue;
+    kept.floor = turn == 2 ? value_of(reach_m) : -inf;
+    double weights = 0.0;
+    if (turn > 0) weights = weigh_row<T, G>(again, s, kept, weight, steps, each);
+    if (turn == 2) {
+      draw_row<T, G>(a, row, s, kept, weight, weights, steps, each);
+    } else {
+      if (by_k) range = {turn == 0 ? lowest : reach_m, all_up, 0.0, INT32_MAX};
+      cut<T, G>(again, s, kept, weight, range, turn == 1, turn == 1 ? p * weights : (double)k);
     }
-    draw_listed<G>(a, row, s, count, weight);
-  } else {
-    all = weigh_row<T, G>(row_again, s, kept, weight, steps, each);
-    draw_row<T, G>(a, row, s, kept, weight, all, steps, each);
   }
 }
 
@@ -555,7 +736,7 @@ template <typename T, int G, int C>
 __global__ __launch_bounds__(G) void sample_kernel(SampleArgs a) {
   __shared__ __attribute__((aligned(16))) SampleShared<G> s;
   const int64_t row = a.first + blockIdx.x;
-  InRegisters<T, G, C> x((const T *)a.logits + row * a.ld, a.n_classes);
+  InRegisters<T, G, C, true> x((const T *)a.logits + row * a.ld, a.n_classes);
   sample_row<T, G>(a, row, x, s);
   store_draw<G>(a, row, s);
 }
@@ -565,7 +746,7 @@ template <typename T, int G>
 __global__ __launch_bounds__(G) void sample_memory_kernel(SampleArgs a) {
   __shared__ __attribute__((aligned(16))) SampleShared<G> s;
   const int64_t row = a.first + blockIdx.x;
-  InMemory<T, G> x((const T *)a.logits + row * a.ld, a.n_classes);
+  Streamed<T, G> x((const T *)a.logits + row * a.ld, a.n_classes);
   sample_row<T, G>(a, row, x, s);
   store_draw<G>(a, row, s);
 }
@@ -576,6 +757,9 @@ int launch_sample(const SampleArgs &a, int32_t dtype, void *stream) {
     const int64_t bytes = (int64_t)a.n_classes * (int)sizeof(T);
     auto of = [&](auto k, int threads) { return launch_each_row(k, threads, a, stream); };
     if (bytes < 16) return of(sample_memory_kernel<T, 64>, 64);
+    // top_k of a wave's 64 maxima or more: more waves, or the bound finds nothing
+    const int k = a.top_ks || a.top_k >= a.n_classes ? 0 : a.top_k;
+    if (k > 64 && bytes > 1024 && bytes <= 16384) return of(sample_kernel<T, 256, 4>, 256);
     if (bytes <= 1024) return of(sample_kernel<T, 64, 1>, 64);
     if (bytes <= 2048) return of(sample_kernel<T, 64, 2>, 64);
     if (bytes <= 4096) return of(sample_kernel<T, 64, 4>, 64);
@@ -583,7 +767,7 @@ int launch_sample(const SampleArgs &a, int32_t dtype, void *stream) {
     if (bytes <= 16384) return of(sample_kernel<T, 256, 4>, 256);
     if (bytes <= 32768) return of(sample_kernel<T, 256, 8>, 256);
     if (bytes <= 65536) return of(sample_kernel<T, 512, 8>, 512);
-    if (bytes <= 131072) return of(sample_kernel<T, 512, 16>, 512);
+    if (bytes <= 131072) return of(sample_kernel<T, 1024, 8>, 1024);
     if (bytes <= 262144) return of(sample_kernel<T, 1024, 16>, 1024);
     return of(sample_memory_kernel<T, 1024>, 1024);
   });
