@@ -73,15 +73,16 @@ template <int G>
 constexpr int kSorted = G >= 1024 ? 2048 : G > 64 ? 1024 : 512;  // candidates that LDS holds
 
 constexpr int kSegments = 16;  // of a row, whose sums the draw keeps
-constexpr int kBins = 8;       // of a range that a cut is looked for in
+template <int G>
+constexpr int kBins = G >= 512 ? 4 : 8;  // of a range that a cut is looked for in
 
 template <int G>
 struct SampleShared {
   union {
     uint64_t key[kSorted<G> + 8];
     struct {  // a lane's weights and numbers of scores
-      double weight[kBins][G];
-      int count[kBins][G];
+      double weight[kBins<G>][G];
+      int count[kBins<G>][G];
     } bin;
   };
   double segment[kSegments][G / 64];
@@ -173,11 +174,72 @@ __device__ inline void each_four(u32x4 raw, F f) {
   }
 }
 
+// A row's scores.  each(f): f(first class, 16 bytes of scores), in ascending order per lane, NaN past the
+// row's end; all lanes make the same number of calls.  Every walk reads the row again, from the caches,
+// with the next loads on their way while one is looked at: held in registers a long row leaves too few
+// of them for the rest (2048 x 128,000 bfloat16, top_k 50: 230 us, 285 from registers).  kRing loads
+// take turns, written out; each_again() is for walks that few rows take.
+template <typename T, int G, int kRing>
+struct Scores {
+  const T *row;
+  int n;
+  static constexpr int V = kPerLoad<T>;
+  __device__ int at(int64_t j0) const {
+    const int64_t j = j0 + (int64_t)threadIdx.x * V;
+    return (int)(j < n ? j : n);
+  }
+  template <typename F>
+  __device__ void look(RowLoad<T> l, int64_t j0, F &f) const {
+    const int j = at(j0);
+    if (j0 + G * V > n) l.take(j, n, fill_of((T)__builtin_nanf("")));
+    f(j, l.raw);
+  }
+  template <typename F>
+  __device__ bool tiny(F &f) const {
+    if (n >= V) return false;
+    RowLoad<T> l;
+    l.tiny(row, (int)threadIdx.x * V, n, (T)__builtin_nanf(""));
+    f(at(0), l.raw);
+    return true;
+  }
+  template <typename F>
+  __device__ void each(F f) const {
+    if (tiny(f)) return;
+    constexpr int64_t step = G * V;
+    RowLoad<T> ring[kRing];
+#pragma unroll
+    for (int u = 0; u < kRing; ++u)
+      if (u * step < n) ring[u].issue(row, at(u * step), n);
+#pragma unroll 1
+    for (int64_t j0 = 0; j0 < n; j0 += kRing * step) {
+#pragma unroll
+      for (int u = 0; u < kRing; ++u)
+        if (j0 + u * step < n) {
+          look(ring[u], j0 + u * step, f);
+          if (j0 + (u + kRing) * step < n) ring[u].issue(row, at(j0 + (u + kRing) * step), n);
+        }
+    }
+  }
+  template <typename F>
+  __device__ void each_again(F f) const {
+    if (tiny(f)) return;
+    constexpr int64_t step = G * V;
+    RowLoad<T> next;
+    next.issue(row, at(0), n);
+#pragma unroll 1
+    for (int64_t j0 = 0; j0 < n; j0 += step) {
+      const RowLoad<T> l = next;
+      if (j0 + step < n) next.issue(row, at(j0 + step), n);
+      look(l, j0, f);
+    }
+  }
+};
+
 // ---------------------------------------------------------------------------- candidates
 // Scores of [lo, up) in the order that `kept` keeps go to the candidates; their number (it may pass
 // kSorted, whose entries alone are there).
-template <typename T, int G, typename Source, typename Keep>
-__device__ inline int collect(Source &x, SampleShared<G> &s, Keep kept, uint32_t lo, uint32_t up) {
+template <typename T, int G, int A, typename Keep>
+__device__ inline int collect(const Scores<T, G, A> &x, SampleShared<G> &s, Keep kept, uint32_t lo, uint32_t up) {
   constexpr int V = kPerLoad<T>;
   const float low = value_of(lo);
   __syncthreads();
@@ -288,49 +350,16 @@ struct Listed {
 };
 
 // ------------------------------------------------------------------- cuts of whole rows
-// A row in memory, as InMemory, with the next load on its way while one is looked at.
-template <typename T, int G>
-struct Streamed {
-  static constexpr int kStep = 1;
-  const T *row;
-  int n;
-  __device__ Streamed(const T *row, int n) : row(row), n(n) {}
-  template <typename F>
-  __device__ void each(F f) {
-    constexpr int V = kPerLoad<T>;
-    const T nan = (T)__builtin_nanf("");
-    auto at = [&](int64_t j0) {
-      const int64_t j = j0 + (int64_t)threadIdx.x * V;
-      return (int)(j < n ? j : n);
-    };
-    RowLoad<T> next;
-    if (n < V) {
-      next.tiny(row, at(0), n, nan);
-      f(at(0), next.raw);
-      return;
-    }
-    next.issue(row, at(0), n);
-#pragma unroll 1
-    for (int64_t j0 = 0; j0 < n; j0 += G * V) {
-      RowLoad<T> l = next;
-      if (j0 + G * V < n) next.issue(row, at(j0 + G * V), n);
-      l.take(at(j0), n, fill_of(nan));
-      f(at(j0), l.raw);
-    }
-  }
-};
-
 // The general way to a row's target-th score in the order (by weight: to the last one before which
 // less than `target` of the weight stands), of those of order `lo` or more: parts the range [lo, up)
-// that holds it into kBins, until LDS holds the range or one score is left, that of many classes.  Its
-// walks read the row from memory again: held in registers they would make up most of the code.
+// that holds it into kBins, until LDS holds the range or one score is left, that of many classes.
 struct Range {
   uint32_t lo, up;
   double base;  // the measure of what reaches up
   int within;   // classes in the range (INT32_MAX: not known)
 };
-template <typename T, int G>
-__device__ inline void cut(Streamed<T, G> &x, SampleShared<G> &s, Kept &kept, const Weights &weight,
+template <typename T, int G, int A>
+__device__ inline void cut(const Scores<T, G, A> &x, SampleShared<G> &s, Kept &kept, const Weights &weight,
                            const Range &range, bool by_weight, double target) {
   uint32_t lo = range.lo, up = range.up;
   double base = range.base;
@@ -338,7 +367,7 @@ __device__ inline void cut(Streamed<T, G> &x, SampleShared<G> &s, Kept &kept, co
   for (;;) {
     const bool one = up - lo == 1;
     if (one || within <= kSorted<G>) {
-      const int count = collect<T, G>(x, s, kept, lo, up);
+      const int count = collect<T, G, A>(x, s, kept, lo, up);
       if (count == 0) return;  // all of it stays: rounding leaves the target past the last
       if (count <= kSorted<G>) {
         sort_candidates<G>(s, count);
@@ -358,7 +387,7 @@ __device__ inline void cut(Streamed<T, G> &x, SampleShared<G> &s, Kept &kept, co
       for (int bit = 30; bit >= 0; --bit) {  // the largest class with fewer than those before it
         const int32_t next = cls | 1 << bit;
         int below = 0;
-        x.each([&](int j, const u32x4 &raw) __attribute__((always_inline)) {
+        x.each_again([&](int j, const u32x4 &raw) __attribute__((always_inline)) {
           each_score<T>(raw, [&](float e, int i) {
             below += e == v && j + i < next && kept(e, j + i);
           });
@@ -370,14 +399,14 @@ __device__ inline void cut(Streamed<T, G> &x, SampleShared<G> &s, Kept &kept, co
       return;
     }
     int shift = 0;
-    while ((up - 1 - lo) >> shift >= kBins) ++shift;
+    while ((up - 1 - lo) >> shift >= kBins<G>) ++shift;
     const int bins = (int)((up - 1 - lo) >> shift) + 1;
     __syncthreads();
     for (int b = 0; b < bins; ++b) {
       s.bin.weight[b][threadIdx.x] = 0.0;
       s.bin.count[b][threadIdx.x] = 0;
     }
-    x.each([&](int j, const u32x4 &raw) __attribute__((always_inline)) {
+    x.each_again([&](int j, const u32x4 &raw) __attribute__((always_inline)) {
       each_score<T>(raw, [&](float e, int i) {
         const uint32_t o = order_of(e);
         if (o >= lo && o < up && kept(e, j + i)) {
@@ -406,8 +435,8 @@ __device__ inline void cut(Streamed<T, G> &x, SampleShared<G> &s, Kept &kept, co
 
 // ------------------------------------------------------------------------------- draws
 // The weights of a row's kept classes, by waves and segments (steps of a walk, whose classes ascend).
-template <typename T, int G, typename Source, typename Keep>
-__device__ inline double weigh_row(Source &x, SampleShared<G> &s, Keep kept, const Weights &weight,
+template <typename T, int G, int A>
+__device__ inline double weigh_row(const Scores<T, G, A> &x, SampleShared<G> &s, const Kept &kept, const Weights &weight,
                                    int steps, int each) {
   constexpr int W = G / 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -538,8 +567,8 @@ __device__ inline void draw_listed(const SampleArgs &a, int64_t row, SampleShare
 }
 
 // The lowest class of the largest score.
-template <typename T, int G, typename Source>
-__device__ inline void first_of(Source &x, SampleShared<G> &s, float top) {
+template <typename T, int G, int A>
+__device__ inline void first_of(const Scores<T, G, A> &x, SampleShared<G> &s, float top) {
   if (threadIdx.x == 0) s.chosen = INT32_MAX;
   __syncthreads();
   int first = INT32_MAX;
@@ -555,13 +584,12 @@ __device__ inline void first_of(Source &x, SampleShared<G> &s, float top) {
 
 // What stays is found as a list of candidates in LDS wherever that holds it, and drawn from there; a
 // row without cuts is drawn from the sums of its segments, the rest (more kept classes than LDS
-// holds, cuts too near to call from quick sums) from memory.  Each walk over the registers stands here
-// once: they are written out, load after load.
-template <typename T, int G, typename Source>
-__device__ inline void sample_row(const SampleArgs &a, int64_t row, Source &x,
-                                  SampleShared<G> &s) {
+// holds, cuts too near to call from quick sums) from memory.
+template <typename T, int G, int A>
+__device__ inline void sample_row(const SampleArgs &a, int64_t row, SampleShared<G> &s) {
   constexpr int V = kPerLoad<T>, W = G / 64;
   const float inf = __builtin_inff();
+  const Scores<T, G, A> x = {(const T *)a.logits + row * a.ld, a.n_classes};
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   double temperature = a.temperatures ? (double)a.temperatures[row] : a.temperature;
   const int k = a.top_ks ? a.top_ks[row] : a.top_k;
@@ -575,14 +603,14 @@ __device__ inline void sample_row(const SampleArgs &a, int64_t row, Source &x,
   // in quick floats: exact enough for most cuts by top_p, and done while the row's loads arrive.
   float from_score = 0.0f, lane_size = 0.0f;
   double lane_all = 0.0;
-  if (by_p && !by_k) {
-    const float high = (float)factor, low = (float)(factor - (double)high);
-    bool first = true;
-    x.each([&](int, const u32x4 &raw) __attribute__((always_inline)) {
+  const float high = (float)factor, low = (float)(factor - (double)high);
+  bool first = true;
+  x.each([&](int, const u32x4 &raw) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) most = fmaxf(most, element<T>(raw, i));
-      if (first && most > -inf) from_score = most;
-      first = false;
+    for (int i = 0; i < V; ++i) most = fmaxf(most, element<T>(raw, i));
+    if (first && most > -inf) from_score = most;
+    first = false;
+    if (by_p && !by_k) {
       float sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
@@ -593,13 +621,8 @@ __device__ inline void sample_row(const SampleArgs &a, int64_t row, Source &x,
         lane_size = __builtin_fmaf(w, fabsf(e), lane_size);
       }
       lane_all += (double)sum;
-    });
-  } else {
-    x.each([&](int, const u32x4 &raw) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) most = fmaxf(most, element<T>(raw, i));
-    });
-  }
+    }
+  });
   float top = lanes_reduce<Max, 64>(most);
   if constexpr (G > 64) {
     if (lane == 0) s.bound[wave] = top;
@@ -613,7 +636,7 @@ __device__ inline void sample_row(const SampleArgs &a, int64_t row, Source &x,
     return;
   }
   if (!(temperature >= 1e-6) || k == 1 || p <= 0.0) {
-    first_of<T, G>(x, s, top);
+    first_of<T, G, A>(x, s, top);
     return;
   }
   const Weights weight(top, factor);
@@ -632,7 +655,7 @@ __device__ inline void sample_row(const SampleArgs &a, int64_t row, Source &x,
   Kept kept = {-inf, -inf, -1};
   kept.floor = value_of(reach_m);
   if (!by_k && !by_p && reach_m == lowest) {
-    const double all = weigh_row<T, G>(x, s, kept, weight, steps, each);
+    const double all = weigh_row<T, G, A>(x, s, kept, weight, steps, each);
     draw_row<T, G>(a, row, s, kept, weight, all, steps, each);
     return;
   }
@@ -676,7 +699,7 @@ __device__ inline void sample_row(const SampleArgs &a, int64_t row, Source &x,
     const uint32_t o = order_of(uniform(b));
     from = o > from ? o : from;
   }
-  int count = collect<T, G>(
+  int count = collect<T, G, A>(
       x, s, [&](float v, int) { return true; }, from, all_up);
   bool listed = count <= kSorted<G>;
   Range range = {lo, all_up, 0.0, INT32_MAX};  // where a general cut by top_p is looked for
@@ -709,17 +732,16 @@ __device__ inline void sample_row(const SampleArgs &a, int64_t row, Source &x,
     return;
   }
   // top_k, then top_p of what that keeps, then the draw
-  Streamed<T, G> again((const T *)a.logits + row * a.ld, a.n_classes);
   for (int turn = by_k ? 0 : 1; turn < 3; ++turn) {
     if (turn == 1 && !by_p) continue;
     kept.floor = turn == 2 ? value_of(reach_m) : -inf;
     double weights = 0.0;
-    if (turn > 0) weights = weigh_row<T, G>(again, s, kept, weight, steps, each);
+    if (turn > 0) weights = weigh_row<T, G, A>(x, s, kept, weight, steps, each);
     if (turn == 2) {
       draw_row<T, G>(a, row, s, kept, weight, weights, steps, each);
     } else {
       if (by_k) range = {turn == 0 ? lowest : reach_m, all_up, 0.0, INT32_MAX};
-      cut<T, G>(again, s, kept, weight, range, turn == 1, turn == 1 ? p * weights : (double)k);
+      cut<T, G, A>(x, s, kept, weight, range, turn == 1, turn == 1 ? p * weights : (double)k);
     }
   }
 }
@@ -731,23 +753,14 @@ __device__ inline void store_draw(const SampleArgs &a, int64_t row, const Sample
   if (a.logp) a.logp[row] = (float)log(s.share);
 }
 
-// A workgroup of G lanes a row, which stays in their registers.
-template <typename T, int G, int C>
-__global__ __launch_bounds__(G) void sample_kernel(SampleArgs a) {
+// A workgroup of G lanes a row, with kRing loads on their way.  Many rows: few of them, in so few
+// registers that two workgroups of 1024 lanes share a compute unit (2048 x 128,000 bfloat16, top_k 50:
+// 230 us, one at a time 266).  A row or two for each compute unit: more (1 x 128,000: 22 us, 28).
+template <typename T, int G, int kRing>
+__global__ __launch_bounds__(G, G >= 512 && kRing < 8 ? 8 : 4) void sample_kernel(SampleArgs a) {
   __shared__ __attribute__((aligned(16))) SampleShared<G> s;
   const int64_t row = a.first + blockIdx.x;
-  InRegisters<T, G, C, true> x((const T *)a.logits + row * a.ld, a.n_classes);
-  sample_row<T, G>(a, row, x, s);
-  store_draw<G>(a, row, s);
-}
-
-// Rows below 16 bytes, and rows that do not fit a workgroup's registers: every walk reads the row.
-template <typename T, int G>
-__global__ __launch_bounds__(G) void sample_memory_kernel(SampleArgs a) {
-  __shared__ __attribute__((aligned(16))) SampleShared<G> s;
-  const int64_t row = a.first + blockIdx.x;
-  Streamed<T, G> x((const T *)a.logits + row * a.ld, a.n_classes);
-  sample_row<T, G>(a, row, x, s);
+  sample_row<T, G, kRing>(a, row, s);
   store_draw<G>(a, row, s);
 }
 
@@ -756,20 +769,15 @@ int launch_sample(const SampleArgs &a, int32_t dtype, void *stream) {
     using T = decltype(t);
     const int64_t bytes = (int64_t)a.n_classes * (int)sizeof(T);
     auto of = [&](auto k, int threads) { return launch_each_row(k, threads, a, stream); };
-    if (bytes < 16) return of(sample_memory_kernel<T, 64>, 64);
     // top_k of a wave's 64 maxima or more: more waves, or the bound finds nothing
     const int k = a.top_ks || a.top_k >= a.n_classes ? 0 : a.top_k;
-    if (k > 64 && bytes > 1024 && bytes <= 16384) return of(sample_kernel<T, 256, 4>, 256);
-    if (bytes <= 1024) return of(sample_kernel<T, 64, 1>, 64);
-    if (bytes <= 2048) return of(sample_kernel<T, 64, 2>, 64);
-    if (bytes <= 4096) return of(sample_kernel<T, 64, 4>, 64);
-    if (bytes <= 8192) return of(sample_kernel<T, 128, 4>, 128);
-    if (bytes <= 16384) return of(sample_kernel<T, 256, 4>, 256);
-    if (bytes <= 32768) return of(sample_kernel<T, 256, 8>, 256);
-    if (bytes <= 65536) return of(sample_kernel<T, 512, 8>, 512);
-    if (bytes <= 131072) return of(sample_kernel<T, 1024, 8>, 1024);
-    if (bytes <= 262144) return of(sample_kernel<T, 1024, 16>, 1024);
-    return of(sample_memory_kernel<T, 1024>, 1024);
+    const int64_t most = k > 64 && bytes > 1024 && bytes <= 16384 ? 16384 : bytes;
+    if (most <= 4096) return of(sample_kernel<T, 64, 4>, 64);
+    if (most <= 8192) return of(sample_kernel<T, 128, 4>, 128);
+    if (a.n_rows <= 256) return of(sample_kernel<T, 1024, 8>, 1024);
+    if (most <= 32768) return of(sample_kernel<T, 256, 4>, 256);
+    if (most <= 65536) return of(sample_kernel<T, 512, 4>, 512);
+    return of(sample_kernel<T, 1024, 4>, 1024);
   });
 }
 

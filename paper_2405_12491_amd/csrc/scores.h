@@ -27,9 +27,8 @@ __device__ inline int32_t class_of(uint64_t key) {
 
 // Where the row's scores are.  each(f): f(first class, 16 bytes of scores), the classes kStep
 // apart, in ascending order per lane; NaN past the row's end.  All lanes make the same number of
-// calls. In registers, lane after lane with whole loads: rows of at least 16 bytes.  kAnew: each walk
-// works its classes out anew rather than holds them, where registers are short.
-template <typename T, int G, int C, bool kAnew = false>
+// calls. In registers, lane after lane with whole loads: rows of at least 16 bytes.
+template <typename T, int G, int C>
 struct InRegisters {
   static constexpr int kStep = 1;
   RowLoad<T> x[C];
@@ -38,8 +37,7 @@ struct InRegisters {
 #pragma unroll
     for (int c = 0; c < C; ++c) x[c].issue(row, (c * G + (int)threadIdx.x) * kPerLoad<T>, n);
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-      if (!kAnew || (c + 1) * G * kPerLoad<T> > n) x[c].take((c * G + lane()) * kPerLoad<T>, n, nan);
+    for (int c = 0; c < C; ++c) x[c].take((c * G + (int)threadIdx.x) * kPerLoad<T>, n, nan);
   }
   template <typename F>
   __device__ void each(F f) {
@@ -48,12 +46,7 @@ struct InRegisters {
   // written out: a loop that stayed one would index registers
   template <typename F, int... c>
   __device__ void each_of(F f, std::integer_sequence<int, c...>) {
-    ((forget(x[c].raw), f((c * G + lane()) * kPerLoad<T>, x[c].raw)), ...);
-  }
-  __device__ static int lane() {
-    int t = threadIdx.x;
-    if constexpr (kAnew) asm volatile("" : "+v"(t));
-    return t;
+    ((forget(x[c].raw), f((c * G + (int)threadIdx.x) * kPerLoad<T>, x[c].raw)), ...);
   }
 };
 // In memory: every walk reads the row again.
