@@ -238,7 +238,7 @@ static SortPlan plan_of(int64_t pairs, int32_t n_entries, int32_t n_features) {
   p.pairs = pairs;
   p.tiles = (pairs + kTile - 1) / kTile;
   // blocks as long as leaves every compute unit several waves' work
-  const int64_t lanes = n_features < 256 ? 16 : 64;
+  const int64_t lanes = n_features > 128 ? n_features / 8 : 16;
   p.length = 16;
   while (p.length < 128 && pairs / p.length * lanes > 512 * 1024) p.length *= 2;
   p.blocks = (pairs + p.length - 1) / p.length;

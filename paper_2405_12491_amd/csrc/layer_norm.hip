@@ -429,19 +429,30 @@ __global__ __launch_bounds__(256) void layer_norm_columns_kernel(LayerNormGradAr
   for (int i = 0; i < V; ++i) to[j + i] = dw[i], to[(int64_t)n + j + i] = db[i];
 }
 
-// The sums of the workgroups' sums: 16 lanes a column, each with every 16th of them, in double.
+// The sums of the workgroups' sums: 16 lanes a column, each with every 16th of them and 8 loads on
+// their way, in double.
 template <typename T>
 __global__ __launch_bounds__(1024) void layer_norm_join_kernel(LayerNormGradArgs a) {
-  constexpr int columns = 64, lanes = 16;
+  constexpr int columns = 64, lanes = 16, ahead = 8;
   __shared__ double join[lanes][columns];
   const int64_t j = (a.first + blockIdx.x) * columns + (threadIdx.x & 63);
   const int part = threadIdx.x >> 6, n = a.n_features;
   double sum = 0.0;
   if (j < 2 * (int64_t)n)
-    for (int p = part; p < a.parts; p += lanes) sum += (double)a.partial[(int64_t)p * 2 * n + j];
+    for (int p0 = part; p0 < a.parts; p0 += ahead * lanes) {
+      float v[ahead];
+#pragma unroll
+      for (int u = 0; u < ahead; ++u) {
+        const int p = p0 + u * lanes;
+        v[u] = a.partial[(int64_t)(p < a.parts ? p : p0) * 2 * n + j];
+      }
+#pragma unroll
+      for (int u = 0; u < ahead; ++u) sum += p0 + u * lanes < a.parts ? (double)v[u] : 0.0;
+    }
   join[part][threadIdx.x & 63] = sum;
   __syncthreads();
   if (part || j >= 2 * (int64_t)n) return;
+#pragma unroll
   for (int p = 1; p < lanes; ++p) sum += join[p][threadIdx.x];
   T *to = (T *)(j < n ? a.dweight : a.dbias);
   if (to) to[j < n ? j : j - n] = from_float<T>((float)sum);
@@ -451,7 +462,7 @@ __global__ __launch_bounds__(1024) void layer_norm_join_kernel(LayerNormGradArgs
 static int parts_of(int64_t n_rows, int32_t n_features, int size) {
   const int64_t bytes = (int64_t)n_features * size;
   if (bytes > 65536) {
-    const int64_t tiles = (n_features + 256 * (16 / size) - 1) / (256 * (16 / size));
+    const int64_t tile = 256 * (16 / size), tiles = (n_features + tile - 1) / tile;
     const int64_t parts = (2048 + tiles - 1) / tiles;
     return (int)(n_rows < 4 * parts ? (n_rows + 3) / 4 : parts);
   }

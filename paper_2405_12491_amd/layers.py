@@ -104,7 +104,7 @@ def _tracked(name, instead, *inputs):
         return False
     for t in inputs:
         if t is not None and getattr(t, "requires_grad", False):
-            if torch.cuda.is_current_stream_capturing():
+            if t.is_cuda and torch.cuda.is_current_stream_capturing():
                 raise RuntimeError(f"{name} with a gradient on a stream that is being captured: "
                                    f"take {instead}")
             return True

@@ -540,3 +540,431 @@ def test_layers_are_differentiated_once(call):
     grad, = torch.autograd.grad(out.sum(), x, create_graph=True)
     with pytest.raises(RuntimeError):
         grad.sum().backward()
+
+
+# ------------------------------------------------------------- together, streams, graphs
+def _every(seed=0, n=65, c=1030):
+    """name -> (inputs that a replay may scale, call): each operator without autograd."""
+    ids = _ids(seed, n, 6, [70] * 6)
+    off = torch.arange(0, 421, 70, device="cuda")
+    one = _ids(seed + 1, 40 * n, 1, [300])[:, 0]
+    table, grad = _normal(seed + 1, 420, c, dtype=torch.bfloat16), _normal(seed + 2, n, c, dtype=torch.float16)
+    tall = _normal(seed + 3, 40 * n, 24)
+    x, res, w, b = _norm_inputs(seed + 4, n, c, torch.bfloat16)
+    stats = torch.empty(n, 3, device="cuda")
+    B.layer_norm(x, w, b, stats=stats)
+    seeds = _seed(seed, 5)
+    z, u = _normal(seed + 9, n, c, scale=3), torch.rand(n, device="cuda", generator=_gen(seed))
+    return {
+        "embed": ([table], lambda: (B.embed(ids, table, 0.5, off),)),
+        "embed_grad": ([grad], lambda: (B.embed_grad(ids, grad, 420, 0.5, off),)),
+        "embed_grad_many": ([tall], lambda: (B.embed_grad(one, tall, 300),)),
+        "dropout": ([x, res], lambda: (B.dropout(x, 0.3, seeds, res),)),
+        "layer_norm": ([x, res], lambda: B.layer_norm(x, w, b, residual=res)),
+        "layer_norm_grad": ([grad, w], lambda: B.layer_norm_grad(grad.bfloat16(), x, stats, w)),
+        "sample": ([z], lambda: B.sample(z, u, temperature=0.8, top_k=40, top_p=0.9)),
+        "sample_all": ([z], lambda: B.sample(z, u, top_p=0.99, temperature=3.0)),
+    }
+
+
+NAMES_ALL = ["embed", "embed_grad", "embed_grad_many", "dropout", "layer_norm", "layer_norm_grad", "sample", "sample_all"]
+
+
+@pytest.mark.parametrize("name", NAMES_ALL)
+@pytest.mark.parametrize("n", [1, 65, 700])
+def test_equal_bits_again(name, n):
+    call = _every(n=n)[name][1]
+    first = [v.clone() for v in call()]
+    for _ in range(5):
+        assert all(_same_bits(x, y) for x, y in zip(first, call()))
+
+
+@pytest.mark.parametrize("name", NAMES_ALL)
+def test_in_a_graph(name):
+    """Captured once, replayed with other inputs in place and eager work between the replays."""
+    inputs, call = _every(n=130)[name]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        call()
+    s.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        out = call()
+    for rep in range(4):
+        for v in inputs:
+            v.mul_(0.5 + 0.3 * rep)
+        torch.cuda.synchronize()
+        for v in out:
+            v.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        eager = call()
+        torch.cuda.synchronize()
+        assert all(_same_bits(x, y) for x, y in zip(out, eager)), rep
+
+
+@pytest.mark.parametrize("n", [600, 30_000])
+def test_ids_that_change_between_replays(n):
+    """The gradient's plan depends on sizes alone: a graph serves any ids."""
+    ids = torch.zeros(n, dtype=torch.int32, device="cuda")
+    grad = _normal(1, n, 40)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        B.embed_grad(ids, grad, 90)
+    s.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        out = B.embed_grad(ids, grad, 90)
+    for seed in range(4):
+        ids.copy_(_ids(seed, n, 1, [[90], [3], [1], [2000]][seed])[:, 0])
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        R.assert_near(out, *L.embed_grad(ids, grad, 90), torch.float32)
+        assert _same_bits(out, B.embed_grad(ids, grad, 90))
+
+
+def test_a_captured_step_draws_anew():
+    """seed[1] advances inside the graph: every replay drops other elements."""
+    x, seed = torch.ones(50, 70, device="cuda"), _seed(3, 0)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        B.dropout(x, 0.5, seed)
+        seed.add_(torch.tensor([0, 0], device="cuda"))
+    s.synchronize()
+    step = torch.tensor([0, 1], device="cuda")
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        out = B.dropout(x, 0.5, seed)
+        back = B.dropout(out, 0.5, seed)
+        seed.add_(step)
+    for rep in range(4):
+        g.replay()
+        torch.cuda.synchronize()
+        keep = torch.from_numpy(L.kept(50, 70, 0.5, (3, rep), 0)).cuda()
+        assert torch.equal(out != 0, keep) and torch.equal(back != 0, keep)
+
+
+def test_two_graphs_and_two_streams_side_by_side():
+    """Workspaces are a call's own: graphs and streams that run at once give what each gives alone."""
+    ops = [_every(seed=k, n=400) for k in (0, 50)]
+    alone = [{k: [v.clone() for v in o[k][1]()] for k in NAMES_ALL} for o in ops]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ops]
+    graphs, outs = [], []
+    for s, o in zip(streams, ops):
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            for k in NAMES_ALL:
+                o[k][1]()
+        s.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            outs.append({k: o[k][1]() for k in NAMES_ALL})
+        graphs.append(g)
+    for _ in range(10):
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    for a, o in zip(alone, outs):
+        assert all(_same_bits(x, y) for k in NAMES_ALL for x, y in zip(a[k], o[k]))
+    for _ in range(10):
+        eager = []
+        for s, o in zip(streams, ops):
+            with torch.cuda.stream(s):
+                eager.append({k: o[k][1]() for k in NAMES_ALL})
+    torch.cuda.synchronize()
+    for a, o in zip(alone, eager):
+        assert all(_same_bits(x, y) for k in NAMES_ALL for x, y in zip(a[k], o[k]))
+
+
+def test_calls_from_several_threads():
+    from concurrent.futures import ThreadPoolExecutor
+    ops = [_every(seed=k, n=300) for k in (0, 50, 100)]
+    alone = [{k: [v.clone() for v in o[k][1]()] for k in NAMES_ALL} for o in ops]
+    torch.cuda.synchronize()
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(10):
+                outs = {k: ops[i][k][1]() for k in NAMES_ALL}
+            torch.cuda.current_stream().synchronize()
+        return all(_same_bits(x, y) for k in NAMES_ALL for x, y in zip(alone[i][k], outs[k]))
+
+    with ThreadPoolExecutor(3) as pool:
+        assert all(pool.map(work, range(3)))
+
+
+def test_with_a_gradient_they_are_refused_in_a_graph():
+    x = _normal(1, 6, 8).requires_grad_()
+    ids = torch.zeros(3, dtype=torch.int32, device="cuda")
+    calls = [lambda: B.embed(ids, x), lambda: B.dropout(x, 0.5, seed), lambda: B.layer_norm(x)[0],
+             lambda: B.layer_norm(x.detach(), x[0])[0], lambda: B.dropout(x.detach(), 0.5, seed, x)]
+    seed = _seed()
+    w = x[0].detach()
+    eager = [c() for c in calls]
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        for c in calls[:3] + calls[4:]:
+            with pytest.raises(RuntimeError, match="being captured"):
+                c()
+        with torch.no_grad():
+            out = [c() for c in calls]
+    for _ in range(3):
+        for v in out:
+            v.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, e.detach()) for a, e in zip(out, eager))
+    sum(e.sum() for e in eager).backward()
+    assert bool(torch.isfinite(x.grad).all()) and w.shape == (8,)
+
+
+def test_a_step_in_a_graph_beside_an_eager_one():
+    """embed -> dropout -> layer_norm and back without autograd is captured while an eager graph of the
+    same leaves is alive."""
+    table = _normal(1, 50, 64).requires_grad_()
+    w, b = _normal(2, 64).requires_grad_(), _normal(3, 64).requires_grad_()
+    ids, seed, up = _ids(4, 90, 1, [50])[:, 0], _seed(), _normal(5, 90, 64)
+
+    def step():
+        with torch.no_grad():
+            stats = torch.empty(90, 3, device="cuda")
+            h = B.dropout(B.embed(ids, table, 8.0), 0.2, seed)
+            y, _ = B.layer_norm(h, w, b, stats=stats)
+            dx, dw, db = B.layer_norm_grad(up, h, stats, w)
+            return y, B.embed_grad(ids, B.dropout(dx, 0.2, seed), 50, 8.0), dw, db
+
+    eager, _ = B.layer_norm(B.dropout(B.embed(ids, table, 8.0), 0.2, seed), w, b)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+    s.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        out = step()
+    for _ in range(3):
+        for v in out:
+            v.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert _same_bits(out[0], eager.detach())
+    grads = torch.autograd.grad(eager, (table, w, b), up)
+    assert all(_same_bits(a, v) for a, v in zip(out[1:], grads))
+
+
+def test_on_another_stream_and_with_torch_between():
+    """Outputs are ready for torch on the stream of the call."""
+    s = torch.cuda.Stream()
+    ops = _every(n=200)
+    alone = {k: [v.clone() for v in ops[k][1]()] for k in NAMES_ALL}
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        busy = torch.randn(4096, 4096, device="cuda")
+        for _ in range(10):
+            busy = busy @ busy * 1e-3
+        outs = {k: [v + 0 for v in ops[k][1]()] for k in NAMES_ALL}
+    s.synchronize()
+    assert all(torch.equal(x, y) for k in NAMES_ALL for x, y in zip(alone[k], outs[k]))
+
+
+def test_together_with_a_forest():
+    """A student of a forest's leaves: predict_leaves -> embed -> dropout -> layer_norm -> class scores, the
+    forest's largest scores to learn from, an answer drawn at last."""
+    from synth import make_workload
+    w = make_workload("rf_d8", 500)
+    X = torch.from_numpy(w.X()).cuda()
+    off = torch.from_numpy(np.ascontiguousarray(w.forest.tree_offsets)).cuda()
+    nodes, k, width, classes = int(off[-1]), len(off) - 1, 48, 10
+    with B.Forest(w.forest) as f:
+        leaves = f.predict_leaves(X)
+    table = _normal(1, nodes, width, scale=0.3).requires_grad_()
+    gain, shift = torch.ones(width, device="cuda").requires_grad_(), torch.zeros(width, device="cuda").requires_grad_()
+    head = _normal(2, width, classes, scale=0.2).requires_grad_()
+    teacher_ids = torch.stack([torch.arange(2, dtype=torch.int32)] * 500).cuda()
+    teacher = _normal(3, 500, 2)
+    seed = _seed()
+
+    def forward():
+        h = B.dropout(B.embed(leaves, table, 1.0 / k, off), 0.1, seed, layer=2)
+        y, total = B.layer_norm(h, gain, shift, residual=h)
+        return y, total, y @ head
+
+    y, total, logits = forward()
+    loss = B.distill_loss(logits, teacher_ids, teacher).sum()
+    grads = torch.autograd.grad(loss, (table, gain, shift, head))
+    # the same in torch, 64 bits
+    ref = [t.detach().double().requires_grad_() for t in (table, gain, shift, head)]
+    at = (leaves.long() + off[:-1]).reshape(-1)
+    e = ref[0][at].view(500, k, width).sum(1) / k
+    keep = torch.from_numpy(L.kept(500, width, 0.1, seed.tolist(), 2)).cuda()
+    h = torch.where(keep, e / 0.9, 0.0)
+    t = h + h
+    c = t - t.mean(1, keepdim=True)
+    z = (c / (c.pow(2).mean(1, keepdim=True) + 1e-5).sqrt() * ref[1] + ref[2]) @ ref[3]
+    p = torch.softmax(teacher.double(), 1)
+    want = -(p * torch.log_softmax(z, 1)[:, :2]).sum() + (p * p.log()).sum()
+    # Sums of 100 leaves, 48 features, 10 classes and 500 rows, one after the other: under 1000 roundings
+    # of terms that are at most 10 times their sum.
+    assert abs(float(loss.detach()) - float(want.detach())) <= 1e4 * R.U * float(want.detach())
+    for got, r in zip(grads, torch.autograd.grad(want, ref)):
+        assert float((got.double() - r).abs().max()) <= 1e4 * R.U * float(r.abs().max())
+    ids, logp = B.sample(logits.detach(), torch.rand(500, device="cuda", generator=_gen(9)), top_k=5)
+    _, top = B.top_k(logits.detach(), 5)
+    assert bool((top == ids[:, None]).any(1).all()) and bool((logp <= 0).all())
+
+
+# -------------------------------------------------------------------- sizes and refusals
+def test_far_offsets():
+    """Rows whose offsets pass 2^31 elements (and 2^32 bytes)."""
+    far, c = (1 << 31) + 24, 1000
+    buf = torch.empty(2 * far + c, dtype=torch.bfloat16, device="cuda")
+    rows = torch.as_strided(buf, (3, c), (far, 1))
+    x = _normal(1, 3, c, dtype=torch.bfloat16)
+    rows.copy_(x)
+    ids = torch.tensor([2, 0, 1, 2, -1], dtype=torch.int32, device="cuda")
+    bag = torch.tensor([[2, 0], [1, 2]], dtype=torch.int32, device="cuda")
+    assert _same_bits(B.embed(ids, rows), B.embed(ids, x)) and _same_bits(B.embed(bag, rows), B.embed(bag, x))
+    assert _same_bits(B.embed_grad(ids[:3], rows, 9), B.embed_grad(ids[:3], x, 9))
+    assert _same_bits(B.dropout(rows, 0.5, _seed(), rows), B.dropout(x, 0.5, _seed(), x))
+    stats = torch.empty(3, 3, device="cuda")
+    assert _same_bits(B.layer_norm(rows, stats=stats)[0], B.layer_norm(x)[0])
+    for a, v in zip(B.layer_norm_grad(rows, rows, stats), B.layer_norm_grad(x, x, stats)):
+        assert _same_bits(a, v)
+    u = torch.rand(3, device="cuda")
+    for how in (dict(), dict(top_k=9), dict(top_p=0.9)):
+        assert all(_same_bits(a, v) for a, v in zip(B.sample(rows, u, **how), B.sample(x, u, **how)))
+    # outputs there
+    want = B.embed(torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda"), x, 3.0)
+    assert _same_bits(B.embed(torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda"), x, 3.0, out=rows), want)
+    want = B.embed_grad(ids, _normal(3, 5, c, dtype=torch.bfloat16), 3)
+    assert _same_bits(B.embed_grad(ids, _normal(3, 5, c, dtype=torch.bfloat16), 3, out=rows), want)
+    want = B.dropout(x, 0.5, _seed())
+    assert _same_bits(B.dropout(x, 0.5, _seed(), out=rows), want)
+    assert _same_bits(B.layer_norm(x, out=rows)[0], B.layer_norm(x)[0])
+
+
+def test_more_workgroups_than_a_launch_takes():
+    """Very long rows: parts of several launches, columns near 2^31."""
+    w = 1_500_000_007
+    x = torch.ones(3, w, dtype=torch.bfloat16, device="cuda")
+    B.dropout(x, 0.5, _seed(), out=x)
+    units = (w + 7) // 8
+    for r in range(3):
+        for first in (0, (2 ** 21 * 256 - r * units) % units, units - 40):
+            first = min(first, units - 40)
+            unit, row = np.arange(first, first + 40, dtype=np.uint64), np.full(40, r, np.uint64)
+            words = L.random_words(unit, row, np.full(40, 7, np.uint64), np.zeros(40, np.uint64),
+                                   1234567890123 % 2 ** 32, 1234567890123 >> 32)
+            half = np.stack([h for v in words for h in (v & np.uint64(0xFFFF), v >> np.uint64(16))], 1).reshape(-1)
+            got = np64(x[r, first * 8:first * 8 + 320])
+            assert np.array_equal(got != 0, (half >= 32768)[:len(got)]), (r, first)
+    table = x[:2]
+    ids = torch.tensor([1, 0, 1], dtype=torch.int32, device="cuda")
+    out = B.embed(ids, table, 2.0)
+    for r, e in enumerate((1, 0, 1)):
+        for part in (slice(0, 5000), slice(w // 2, w // 2 + 5000), slice(w - 5000, w)):
+            assert torch.equal(out[r, part], table[e, part] * 2)
+    del out
+    y, _ = B.layer_norm(table)
+    # zeros and twos in equal shares: -1 and 1 to about 2^-15, half a step of the output
+    assert torch.equal(y[1, -5000:], (table[1, -5000:] - 1).sign())
+    assert torch.equal(y[0, w // 3:w // 3 + 5000], (table[0, w // 3:w // 3 + 5000] - 1).sign())
+
+
+def test_sample_more_rows_than_a_launch_takes():
+    n = (1 << 20) + 77
+    z, u = _normal(1, n, 3), torch.rand(n, device="cuda", generator=_gen(2))
+    ids, _ = B.sample(z, u)
+    w = torch.cumsum(torch.softmax(z.double(), 1), 1)
+    want = (w <= u.double()[:, None]).sum(1).clamp(max=2)
+    near = (w - u.double()[:, None]).abs().min(1).values < 1e-12
+    assert bool(((ids == want) | near).all())
+
+
+def test_refused_tensors():
+    x, ids, w = _normal(1, 6, 8), torch.zeros(6, 2, dtype=torch.int32, device="cuda"), _normal(2, 8)
+    seed, u, stats = _seed(), torch.rand(6, device="cuda"), torch.empty(6, 3, device="cuda")
+    half = x.half()
+    wrong = [
+        (TypeError, lambda: B.embed(ids.long(), x)), (TypeError, lambda: B.embed(ids, x.double())),
+        (TypeError, lambda: B.embed(ids, x.int())), (ValueError, lambda: B.embed(ids, x.t())),
+        (ValueError, lambda: B.embed(ids.t(), x)), (ValueError, lambda: B.embed(ids, x[0])),
+        (ValueError, lambda: B.embed(ids, x, offsets=torch.zeros(2, dtype=torch.int64, device="cuda"))),
+        (TypeError, lambda: B.embed(ids, x, offsets=torch.zeros(3, device="cuda"))),
+        (ValueError, lambda: B.embed(ids[:1, 0].expand(6), x)),
+        (ValueError, lambda: B.embed(ids, x, out=torch.empty(5, 8, device="cuda"))),
+        (TypeError, lambda: B.embed(ids, x, out=half)), (B.BridgerError, lambda: B.embed(ids, x, out=x)),
+        (B.BridgerError, lambda: B.embed(ids, x, scale=inf)), (B.BridgerError, lambda: B.embed(ids[:, :0], x)),
+        (ValueError, lambda: B.embed_grad(ids, x, 0)), (ValueError, lambda: B.embed_grad(ids, x, 2 ** 31)),
+        (ValueError, lambda: B.embed_grad(ids, x[:5], 4)), (ValueError, lambda: B.embed_grad(ids, x, 4, out=x)),
+        (B.BridgerError, lambda: B.embed_grad(ids, x, 6, out=x)),
+        (TypeError, lambda: B.dropout(x, 0.5, seed.int())), (ValueError, lambda: B.dropout(x, 0.5, seed[:1])),
+        (TypeError, lambda: B.dropout(x, 0.5, 7)), (B.BridgerError, lambda: B.dropout(x, 1.5, seed)),
+        (B.BridgerError, lambda: B.dropout(x, nan, seed)), (ValueError, lambda: B.dropout(x, 0.5, seed, layer=-1)),
+        (ValueError, lambda: B.dropout(x, 0.5, seed, layer=2 ** 31)), (TypeError, lambda: B.dropout(x, 0.5, seed, half)),
+        (ValueError, lambda: B.dropout(x, 0.5, seed, x[:, :7])), (TypeError, lambda: B.dropout(x.double(), 0.5, seed)),
+        (ValueError, lambda: B.dropout(x[:1].expand(6, 8), 0.5, seed)), (ValueError, lambda: B.dropout(x[:, ::2], 0.5, seed)),
+        (TypeError, lambda: B.layer_norm(x, w.half())), (ValueError, lambda: B.layer_norm(x, w[:7])),
+        (ValueError, lambda: B.layer_norm(x, w, w[:7])), (B.BridgerError, lambda: B.layer_norm(x, eps=-1.0)),
+        (ValueError, lambda: B.layer_norm(x, stats=stats[:, :2])), (TypeError, lambda: B.layer_norm(x, stats=stats.half())),
+        (B.BridgerError, lambda: B.layer_norm(x, out=x)), (TypeError, lambda: B.layer_norm(x, residual=half)),
+        (ValueError, lambda: B.layer_norm_grad(x, x[:5], stats)), (TypeError, lambda: B.layer_norm_grad(x, half, stats)),
+        (ValueError, lambda: B.layer_norm_grad(x, x, stats[:5])), (B.BridgerError, lambda: B.layer_norm_grad(x, x, stats, out=x)),
+        (TypeError, lambda: B.layer_norm_grad(x, x, stats, grad_total=half)),
+        (TypeError, lambda: B.sample(x, u.double())), (ValueError, lambda: B.sample(x, u[:5])),
+        (B.BridgerError, lambda: B.sample(x, u, temperature=-1.0)), (ValueError, lambda: B.sample(x, u, top_k=-1)),
+        (ValueError, lambda: B.sample(x, u, top_k=2 ** 31)), (B.BridgerError, lambda: B.sample(x, u, top_p=1.5)),
+        (B.BridgerError, lambda: B.sample(x, u, min_p=nan)), (TypeError, lambda: B.sample(x, u, top_k=u)),
+        (TypeError, lambda: B.sample(x, u, temperature=u.double())), (ValueError, lambda: B.sample(x, u, top_p=u[:3])),
+        (TypeError, lambda: B.sample(x.long(), u)), (ValueError, lambda: B.sample(x, u, ids=ids[:, 0])),
+        (B.BridgerError, lambda: B.sample(x, u, logp=u)),
+    ]
+    for i, (error, call) in enumerate(wrong):
+        with pytest.raises(error):
+            call()
+            pytest.fail(f"call {i} was not refused")
+    torch.cuda.synchronize()
+
+
+def test_outputs_that_autograd_tracks_or_saves():
+    """What is written counts as written in place; what requires grad is refused."""
+    x, u, ids = _normal(1, 6, 8), torch.rand(6, device="cuda"), torch.zeros(6, dtype=torch.int32, device="cuda")
+    stats = torch.empty(6, 3, device="cuda")
+    B.layer_norm(x, stats=stats)
+    for make in (lambda o: B.embed(ids, x, out=o), lambda o: B.embed_grad(ids, x, 6, out=o),
+                 lambda o: B.dropout(x, 0.5, _seed(), out=o), lambda o: B.layer_norm(x, out=o),
+                 lambda o: B.layer_norm(x, total=o), lambda o: B.layer_norm_grad(x, x, stats, out=o)):
+        out = torch.zeros(6, 8, device="cuda")
+        before = out._version
+        make(out)
+        assert out._version > before
+        leaf = torch.zeros(6, 8, device="cuda", requires_grad=True)
+        with pytest.raises(RuntimeError, match="requires grad"):
+            make(leaf)
+        with torch.no_grad():
+            make(leaf)
+    logp, drawn = torch.zeros(6, device="cuda"), torch.zeros(6, dtype=torch.int32, device="cuda")
+    before = logp._version, drawn._version
+    B.sample(x, u, ids=drawn, logp=logp)
+    assert logp._version > before[0] and drawn._version > before[1]
+    with pytest.raises(RuntimeError, match="requires grad"):
+        B.sample(x, u, logp=torch.zeros(6, device="cuda", requires_grad=True))
+    # an input changed between forward and backward
+    leaf = _normal(2, 6, 8).requires_grad_()
+    h = leaf * 1
+    y, _ = B.layer_norm(h)
+    h.mul_(2)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    some = ids.clone()
+    y = B.embed(some, leaf)
+    some.add_(1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
