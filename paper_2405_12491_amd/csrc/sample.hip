@@ -351,37 +351,45 @@ struct Listed {
 
 // ------------------------------------------------------------------- cuts of whole rows
 // The general way to a row's target-th score in the order (by weight: to the last one before which
-// less than `target` of the weight stands), of those of order `lo` or more: parts the range [lo, up)
-// that holds it into kBins, until LDS holds the range or one score is left, that of many classes.
+// less than the target stands), among those of order [lo, up): parts the range into bins and goes on with
+// the one that holds it, until LDS holds its scores or one score is left, that of many classes.  What is
+// left of the target below `up` lies in [least, most]: by quick weights, in floats, it is an interval,
+// and false is returned where that does not tell.
 struct Range {
   uint32_t lo, up;
-  double base;  // the measure of what reaches up
-  int within;   // classes in the range (INT32_MAX: not known)
+  double least, most;
+  int within;  // classes in the range (INT32_MAX: not known)
 };
+enum class Measure { kCount, kWeight, kQuickWeight };
 template <typename T, int G, int A>
-__device__ inline void cut(const Scores<T, G, A> &x, SampleShared<G> &s, Kept &kept, const Weights &weight,
-                           const Range &range, bool by_weight, double target) {
-  uint32_t lo = range.lo, up = range.up;
-  double base = range.base;
-  int within = range.within;
+__device__ inline bool cut(const Scores<T, G, A> &x, SampleShared<G> &s, Kept &kept,
+                           const Weights &weight, Range r, Measure by) {
+  const float top = (float)weight.top, high = (float)weight.factor;
+  const float low = (float)(weight.factor - (double)high);
   for (;;) {
-    const bool one = up - lo == 1;
-    if (one || within <= kSorted<G>) {
-      const int count = collect<T, G, A>(x, s, kept, lo, up);
-      if (count == 0) return;  // all of it stays: rounding leaves the target past the last
+    const bool one = r.up - r.lo == 1;
+    if (one || r.within <= kSorted<G>) {
+      const int count = collect<T, G, A>(x, s, kept, r.lo, r.up);
+      if (count == 0) return true;  // all of it stays: rounding leaves the target past the last
       if (count <= kSorted<G>) {
         sort_candidates<G>(s, count);
-        int stay = target - base < count ? (int)(target - base) : count;
-        if (by_weight) stay = Listed<G>(s, count, weight, 32).leading(s, count, target - base);
+        int stay = r.most < count ? (int)r.most : count;
+        if (by != Measure::kCount) {
+          const Listed<G> l(s, count, weight, 32);
+          stay = l.leading(s, count, r.most);
+          if (by == Measure::kQuickWeight && stay != l.leading(s, count, r.least)) return false;
+        }
         const uint64_t key = s.key[stay > 0 ? stay - 1 : 0];
         kept.score = value_of((uint32_t)(key >> 32));
         kept.cls = class_of(key);
-        return;
+        return true;
       }
     }
     if (one) {
-      const float v = value_of(lo);
-      double want = __builtin_ceil((target - base) / (by_weight ? weight(v) : 1.0));
+      const float v = value_of(r.lo);
+      const double each = by == Measure::kCount ? 1.0 : weight(v);
+      double want = __builtin_ceil(r.most / each);
+      if (want != __builtin_ceil(r.least / each)) return false;
       if (!(want >= 1.0)) want = 1.0;  // of its classes
       int32_t cls = 0;
       for (int bit = 30; bit >= 0; --bit) {  // the largest class with fewer than those before it
@@ -396,11 +404,11 @@ __device__ inline void cut(const Scores<T, G, A> &x, SampleShared<G> &s, Kept &k
       }
       kept.score = v;
       kept.cls = cls;
-      return;
+      return true;
     }
     int shift = 0;
-    while ((up - 1 - lo) >> shift >= kBins<G>) ++shift;
-    const int bins = (int)((up - 1 - lo) >> shift) + 1;
+    while ((r.up - 1 - r.lo) >> shift >= kBins<G>) ++shift;
+    const int bins = (int)((r.up - 1 - r.lo) >> shift) + 1;
     __syncthreads();
     for (int b = 0; b < bins; ++b) {
       s.bin.weight[b][threadIdx.x] = 0.0;
@@ -409,26 +417,39 @@ __device__ inline void cut(const Scores<T, G, A> &x, SampleShared<G> &s, Kept &k
     x.each_again([&](int j, const u32x4 &raw) __attribute__((always_inline)) {
       each_score<T>(raw, [&](float e, int i) {
         const uint32_t o = order_of(e);
-        if (o >= lo && o < up && kept(e, j + i)) {
-          const uint32_t b = (o - lo) >> shift;
+        if (o >= r.lo && o < r.up && kept(e, j + i)) {
+          const uint32_t b = (o - r.lo) >> shift;
           s.bin.count[b][threadIdx.x] += 1;
-          if (by_weight) s.bin.weight[b][threadIdx.x] += weight(e);
+          if (by == Measure::kQuickWeight) {
+            const float d = e - top;
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(d, low, d * high));
+            s.bin.weight[b][threadIdx.x] += (double)w;
+          } else if (by == Measure::kWeight) {
+            s.bin.weight[b][threadIdx.x] += weight(e);
+          }
         }
       });
     });
+    // a quick weight is off by 2^-23 times 1.1 of its exponent and 2 (see sample_row)
+    const double off = by != Measure::kQuickWeight ? 0.0
+                       : 0x1p-23 * (1.2 * (weight.top - (double)value_of(r.lo)) * weight.factor + 3.0);
     // from the largest scores down: the bin that reaches the target, or the last
-    int b = bins;
-    double reach = base;
-    do {
-      --b;
-      base = reach;
-      within = sum_all<G>(s.bin.count[b][threadIdx.x], s.found);
-      reach += by_weight ? sum_all<G>(s.bin.weight[b][threadIdx.x], s.wave[0]) : (double)within;
-    } while (reach < target && b > 0);
-    const uint32_t begin = lo + ((uint32_t)b << shift);
+    int b = bins - 1;
+    for (;; --b) {
+      r.within = sum_all<G>(s.bin.count[b][threadIdx.x], s.found);
+      const double reach = by == Measure::kCount
+                               ? (double)r.within
+                               : sum_all<G>(s.bin.weight[b][threadIdx.x], s.wave[0]);
+      if (reach * (1.0 - off) >= r.most) break;
+      if (!(reach * (1.0 + off) < r.least) || (b == 0 && by == Measure::kQuickWeight)) return false;
+      if (b == 0) break;
+      r.most -= reach * (1.0 - off);
+      r.least -= reach * (1.0 + off);
+    }
+    const uint32_t begin = r.lo + ((uint32_t)b << shift);
     const uint64_t end = (uint64_t)begin + (uint64_t(1) << shift);
-    up = end < up ? (uint32_t)end : up;
-    lo = begin;
+    r.up = end < r.up ? (uint32_t)end : r.up;
+    r.lo = begin;
     __syncthreads();  // the bins are read
   }
 }
@@ -702,7 +723,10 @@ __device__ inline void sample_row(const SampleArgs &a, int64_t row, SampleShared
   int count = collect<T, G, A>(
       x, s, [&](float v, int) { return true; }, from, all_up);
   bool listed = count <= kSorted<G>;
-  Range range = {lo, all_up, 0.0, INT32_MAX};  // where a general cut by top_p is looked for
+  // where a general cut by top_p is looked for
+  Range range = {lo, all_up, p * (all - off), p * (all + off), INT32_MAX};
+  bool exact = !(off < all);  // (sums of double weights are needed)
+  double above = 0.0;         // what reaches range.up
   if (listed) {
     sort_candidates<G>(s, count);
     if (by_k && count > k) count = k;
@@ -710,18 +734,25 @@ __device__ inline void sample_row(const SampleArgs &a, int64_t row, SampleShared
       const Listed<G> l(s, count, weight, 32);
       if (by_k) all = l.all;
       const double least = p * (all - off), greatest = p * (all + off);
-      if (off >= all) {
+      if (!(off < all)) {
         listed = false;
       } else if (l.all >= greatest || from == lo) {
         const int stay = l.leading(s, count, least);
         if (off > 0.0 && stay != l.leading(s, count, greatest)) {
           listed = false;
-          range = {from, all_up, 0.0, count};
+          exact = true;
+          range.lo = from;
+          range.within = count;
         }
         count = stay;
       } else {
         listed = false;
-        if (l.all < least) range.up = from, range.base = l.all;
+        if (l.all < least) {
+          range.up = from;
+          above = l.all;
+          range.least -= above;
+          range.most -= above;
+        }
       }
     }
   }
@@ -731,17 +762,21 @@ __device__ inline void sample_row(const SampleArgs &a, int64_t row, SampleShared
     draw_listed<G>(a, row, s, sum_all<G>(reach, s.found), weight);
     return;
   }
-  // top_k, then top_p of what that keeps, then the draw
-  for (int turn = by_k ? 0 : 1; turn < 3; ++turn) {
-    if (turn == 1 && !by_p) continue;
-    kept.floor = turn == 2 ? value_of(reach_m) : -inf;
+  // top_k, then top_p of what that keeps (by quick sums first, where no top_k is), then the draw
+  for (int turn = by_k ? 0 : exact ? 2 : 1; turn < 4; ++turn) {
+    if ((turn == 1 && by_k) || (turn == 2 && !by_p) || (turn == 1 && !by_p)) continue;
+    kept.floor = turn == 3 ? value_of(reach_m) : -inf;
     double weights = 0.0;
-    if (turn > 0) weights = weigh_row<T, G, A>(x, s, kept, weight, steps, each);
-    if (turn == 2) {
+    if (turn > 1) weights = weigh_row<T, G, A>(x, s, kept, weight, steps, each);
+    if (turn == 3) {
       draw_row<T, G>(a, row, s, kept, weight, weights, steps, each);
+    } else if (turn == 1) {
+      if (cut<T, G, A>(x, s, kept, weight, range, Measure::kQuickWeight)) turn = 2;
     } else {
-      if (by_k) range = {turn == 0 ? lowest : reach_m, all_up, 0.0, INT32_MAX};
-      cut<T, G, A>(x, s, kept, weight, range, turn == 1, turn == 1 ? p * weights : (double)k);
+      Range r = {by_k && turn == 0 ? lowest : by_k ? reach_m : range.lo, by_k ? all_up : range.up,
+                 turn == 0 ? (double)k : p * weights - above, 0.0, by_k ? INT32_MAX : range.within};
+      r.most = r.least;  // (`above` is 0 where top_k is)
+      cut<T, G, A>(x, s, kept, weight, r, turn == 0 ? Measure::kCount : Measure::kWeight);
     }
   }
 }
