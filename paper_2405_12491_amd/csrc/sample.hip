@@ -56,16 +56,37 @@ struct Weights {
     for (int i = 0; i < N; ++i)
       w[i] = __builtin_ldexp(s[i], (int)(uint32_t)__builtin_bit_cast(uint64_t, t[i]));
   }
-  // The sum of the weights of four scores, those that are `in`.
-  __device__ double sum(const float (&v)[4], const bool (&in)[4]) const {
-    double d[4], w[4];
+  // The weights of four scores, those that are `in` (0 for others); their sum.
+  __device__ void four(const float (&v)[4], const bool (&in)[4], double (&w)[4]) const {
+    double d[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       d[i] = in[i] ? (double)v[i] - top : last;
       d[i] = (double)v[i] == top && in[i] ? 0.0 : d[i];
     }
     of<4>(d, w);
+  }
+  __device__ double sum(const float (&v)[4], const bool (&in)[4]) const {
+    double w[4];
+    four(v, in, w);
     return (w[0] + w[1]) + (w[2] + w[3]);
+  }
+};
+
+// The same relative to another score, quickly: the exponent in two floats, the exponential in one.  Off
+// by 2^-23 times 0.36 of the exponent (the difference rounds by 2^-24 of it, times ln 2), 1 for the
+// exponential and 1 for the product that follows.
+struct QuickWeights {
+  float high, low;  // log2(e) / T
+  __device__ explicit QuickWeights(double factor)
+      : high(uniform((float)factor)), low(uniform((float)(factor - (double)(float)factor))) {}
+  // d = v - score (NaN: no weight); the exponent in `e`
+  __device__ float operator()(float d, float *e) const {
+    const float a = fmaxf(d * high, -200.0f);
+    const float b = __builtin_fmaf(d, low, __builtin_fmaf(d, high, -a));
+    const float w = __builtin_amdgcn_exp2f(a);
+    *e = a;
+    return a > -200.0f ? __builtin_fmaf(w, b * 0.693147181f, w) : 0.0f;
   }
 };
 
@@ -353,19 +374,24 @@ struct Listed {
 // The general way to a row's target-th score in the order (by weight: to the last one before which
 // less than the target stands), among those of order [lo, up): parts the range into bins and goes on with
 // the one that holds it, until LDS holds its scores or one score is left, that of many classes.  What is
-// left of the target below `up` lies in [least, most]: by quick weights, in floats, it is an interval,
-// and false is returned where that does not tell.
+// left of the target below `up` lies in [least, most]: by quick weights it is an interval, and false is
+// returned where that does not tell, with the range so far.
 struct Range {
   uint32_t lo, up;
   double least, most;
   int within;  // classes in the range (INT32_MAX: not known)
 };
+// *at += v in LDS, without waiting for what was there; no other lane adds to it.
+template <typename V>
+__device__ inline void lane_add(V *at, V v) {
+  __hip_atomic_fetch_add(at, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
 enum class Measure { kCount, kWeight, kQuickWeight };
 template <typename T, int G, int A>
 __device__ inline bool cut(const Scores<T, G, A> &x, SampleShared<G> &s, Kept &kept,
-                           const Weights &weight, Range r, Measure by) {
-  const float top = (float)weight.top, high = (float)weight.factor;
-  const float low = (float)(weight.factor - (double)high);
+                           const Weights &weight, Range &r, Measure by) {
+  const float top = (float)weight.top;
+  const QuickWeights quick(weight.factor);
   for (;;) {
     const bool one = r.up - r.lo == 1;
     if (one || r.within <= kSorted<G>) {
@@ -419,20 +445,18 @@ __device__ inline bool cut(const Scores<T, G, A> &x, SampleShared<G> &s, Kept &k
         const uint32_t o = order_of(e);
         if (o >= r.lo && o < r.up && kept(e, j + i)) {
           const uint32_t b = (o - r.lo) >> shift;
-          s.bin.count[b][threadIdx.x] += 1;
+          lane_add(&s.bin.count[b][threadIdx.x], 1);
           if (by == Measure::kQuickWeight) {
-            const float d = e - top;
-            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(d, low, d * high));
-            s.bin.weight[b][threadIdx.x] += (double)w;
+            float exponent;
+            lane_add(&s.bin.weight[b][threadIdx.x], (double)quick(e - top, &exponent));
           } else if (by == Measure::kWeight) {
-            s.bin.weight[b][threadIdx.x] += weight(e);
+            lane_add(&s.bin.weight[b][threadIdx.x], weight(e));
           }
         }
       });
     });
-    // a quick weight is off by 2^-23 times 1.1 of its exponent and 2 (see sample_row)
     const double off = by != Measure::kQuickWeight ? 0.0
-                       : 0x1p-23 * (1.2 * (weight.top - (double)value_of(r.lo)) * weight.factor + 3.0);
+                       : 0x1p-23 * (0.4 * (weight.top - (double)value_of(r.lo)) * weight.factor + 2.5);
     // from the largest scores down: the bin that reaches the target, or the last
     int b = bins - 1;
     for (;; --b) {
@@ -497,6 +521,25 @@ __device__ inline double weigh_row(const Scores<T, G, A> &x, SampleShared<G> &s,
 __device__ inline double target_of(const SampleArgs &a, int64_t row, double all) {
   const double u = (double)a.u[row];
   return (u > 0.0 ? (u < 1.0 ? u : 1.0 - 0x1p-24) : 0.0) * all;
+}
+
+// The weights of a row's kept classes, and of those among them that reach `from`.
+template <typename T, int G, int A>
+__device__ inline double weigh_from(const Scores<T, G, A> &x, SampleShared<G> &s, const Kept &kept,
+                                    const Weights &weight, float from, double *reach) {
+  double all = 0.0, part = 0.0;
+  x.each_again([&](int j, const u32x4 &raw) __attribute__((always_inline)) {
+    each_four<T>(raw, [&](const float(&v)[4], int i) {
+      double w[4];
+      weight.four(v, {kept(v[0], j + i), kept(v[1], j + i + 1), kept(v[2], j + i + 2),
+                      kept(v[3], j + i + 3)}, w);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) part += v[q] >= from ? w[q] : 0.0;
+      all += (w[0] + w[1]) + (w[2] + w[3]);
+    });
+  });
+  *reach = sum_all<G>(part, s.wave[0]);
+  return sum_all<G>(all, s.wave[1]);
 }
 
 // The first class whose weight, with that of the kept ones before it, passes the target, from the sums
@@ -624,7 +667,7 @@ __device__ inline void sample_row(const SampleArgs &a, int64_t row, SampleShared
   // in quick floats: exact enough for most cuts by top_p, and done while the row's loads arrive.
   float from_score = 0.0f, lane_size = 0.0f;
   double lane_all = 0.0;
-  const float high = (float)factor, low = (float)(factor - (double)high);
+  const QuickWeights quick(factor);
   bool first = true;
   x.each([&](int, const u32x4 &raw) __attribute__((always_inline)) {
 #pragma unroll
@@ -632,16 +675,17 @@ __device__ inline void sample_row(const SampleArgs &a, int64_t row, SampleShared
     if (first && most > -inf) from_score = most;
     first = false;
     if (by_p && !by_k) {
-      float sum = 0.0f;
+      float w[V], e[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float d = element<T>(raw, i) - from_score;
-        const float e = fmaxf(__builtin_fmaf(d, low, d * high), -200.0f);  // (NaN: no weight)
-        const float w = __builtin_amdgcn_exp2f(e);
-        sum += w;
-        lane_size = __builtin_fmaf(w, fabsf(e), lane_size);
+        w[i] = quick(element<T>(raw, i) - from_score, &e[i]);
+        lane_size = __builtin_fmaf(w[i], fabsf(e[i]), lane_size);
       }
-      lane_all += (double)sum;
+#pragma unroll
+      for (int n = V / 2; n > 0; n /= 2)
+#pragma unroll
+        for (int i = 0; i < n; ++i) w[i] += w[i + n];
+      lane_all += (double)w[0];
     }
   });
   float top = lanes_reduce<Max, 64>(most);
@@ -681,23 +725,22 @@ __device__ inline void sample_row(const SampleArgs &a, int64_t row, SampleShared
     return;
   }
 
-  // Where the candidates begin.  By top_p: the quick sum is off by 2^-23 times 1.1 of each weight's
-  // exponent (the difference, its product and the second one round by 2^-24 of it each, times ln 2), 2
-  // for the exponential and 4 for the sum of a load's weights, taken as 8.  Classes of a weight below
+  // Where the candidates begin.  By top_p: the quick sum is off by what its weights are, and 2^-23 times
+  // 1.5 for the sums of a load's weights (0.4 and 4 stand for 0.36 and 3.5).  Classes of a weight below
   // (1 - p) all / n hold less than 1 - p of it together: no cut below.
   uint32_t lo = by_k ? lowest : reach_m;
   double all = 0.0, off = 0.0;
-  const bool quick = by_p && !by_k && lane_all <= 0x1p100;
+  const bool finite = lane_all <= 0x1p100;
   if (by_p && !by_k) {
     // (rows whose first scores say nothing of the others: infinite sums are not quick)
     const double shift = ((double)from_score - (double)top) * factor;
     const double down = Weights(0.0f, factor).of((double)from_score - (double)top);
     const double lane_off = (double)lane_size + lane_all * fabs(shift);
-    const bool held = __all(quick && shift <= 60.0);  // (false for NaN)
+    const bool held = __all(finite && shift <= 60.0);  // (false for NaN)
     all = held ? lane_all * down : (double)inf;
     off = held ? lane_off * down : (double)inf;
     all = uniform(sum_all<G>(all, s.wave[0]));
-    off = uniform(0x1p-23 * (1.2 * sum_all<G>(off, s.wave[1]) + 8.0 * all));
+    off = uniform(0x1p-23 * (0.4 * sum_all<G>(off, s.wave[1]) + 4.0 * all));
     if (all < (double)inf && off < all) {
       const uint32_t o =
           order_from((double)top + temperature * (log((1.0 - p) * all / a.n_classes) - 1.0));
@@ -726,7 +769,6 @@ __device__ inline void sample_row(const SampleArgs &a, int64_t row, SampleShared
   // where a general cut by top_p is looked for
   Range range = {lo, all_up, p * (all - off), p * (all + off), INT32_MAX};
   bool exact = !(off < all);  // (sums of double weights are needed)
-  double above = 0.0;         // what reaches range.up
   if (listed) {
     sort_candidates<G>(s, count);
     if (by_k && count > k) count = k;
@@ -749,9 +791,8 @@ __device__ inline void sample_row(const SampleArgs &a, int64_t row, SampleShared
         listed = false;
         if (l.all < least) {
           range.up = from;
-          above = l.all;
-          range.least -= above;
-          range.most -= above;
+          range.least -= l.all;
+          range.most -= l.all;
         }
       }
     }
@@ -764,20 +805,24 @@ __device__ inline void sample_row(const SampleArgs &a, int64_t row, SampleShared
   }
   // top_k, then top_p of what that keeps (by quick sums first, where no top_k is), then the draw
   for (int turn = by_k ? 0 : exact ? 2 : 1; turn < 4; ++turn) {
-    if ((turn == 1 && by_k) || (turn == 2 && !by_p) || (turn == 1 && !by_p)) continue;
+    if ((turn == 1 && by_k) || (turn < 3 && turn > 0 && !by_p)) continue;
     kept.floor = turn == 3 ? value_of(reach_m) : -inf;
-    double weights = 0.0;
-    if (turn > 1) weights = weigh_row<T, G, A>(x, s, kept, weight, steps, each);
     if (turn == 3) {
+      const double weights = weigh_row<T, G, A>(x, s, kept, weight, steps, each);
       draw_row<T, G>(a, row, s, kept, weight, weights, steps, each);
-    } else if (turn == 1) {
-      if (cut<T, G, A>(x, s, kept, weight, range, Measure::kQuickWeight)) turn = 2;
-    } else {
-      Range r = {by_k && turn == 0 ? lowest : by_k ? reach_m : range.lo, by_k ? all_up : range.up,
-                 turn == 0 ? (double)k : p * weights - above, 0.0, by_k ? INT32_MAX : range.within};
-      r.most = r.least;  // (`above` is 0 where top_k is)
-      cut<T, G, A>(x, s, kept, weight, r, turn == 0 ? Measure::kCount : Measure::kWeight);
+      return;
     }
+    if (turn == 0) range = {lowest, all_up, (double)k, (double)k, INT32_MAX};
+    if (turn == 2) {
+      if (by_k) range = {reach_m, all_up, 0.0, 0.0, INT32_MAX};
+      double reach;
+      const double weights = weigh_from<T, G, A>(x, s, kept, weight, value_of(range.up), &reach);
+      range.least = range.most = p * weights - reach;
+    }
+    const Measure by = turn == 0   ? Measure::kCount
+                       : turn == 1 ? Measure::kQuickWeight
+                                   : Measure::kWeight;
+    if (cut<T, G, A>(x, s, kept, weight, range, by) && turn == 1) turn = 2;
   }
 }
 
