@@ -30,7 +30,8 @@ struct Weights {
     of<1>({d}, w);
     return w[0];
   }
-  // N at a time, step by step: one alone waits for its own results (1 x 128,000 unfiltered: XX us).
+  // N at a time, step by step, so that none waits for its own results.  Double instructions bound the
+  // rows that need them for every class: 1 x 128,000 without cuts 69 us, a maximum alone 15.
   template <int N>
   __device__ void of(const double (&d)[N], double (&w)[N]) const {
     constexpr double round = 0x1.8p52;  // leaves whole numbers, in the lower word
@@ -392,6 +393,7 @@ __device__ inline bool cut(const Scores<T, G, A> &x, SampleShared<G> &s, Kept &k
                            const Weights &weight, Range &r, Measure by) {
   const float top = (float)weight.top;
   const QuickWeights quick(weight.factor);
+  const bool whole = kept.score == -__builtin_inff() && kept.floor == -__builtin_inff();
   for (;;) {
     const bool one = r.up - r.lo == 1;
     if (one || r.within <= kSorted<G>) {
@@ -435,6 +437,7 @@ __device__ inline bool cut(const Scores<T, G, A> &x, SampleShared<G> &s, Kept &k
     int shift = 0;
     while ((r.up - 1 - r.lo) >> shift >= kBins<G>) ++shift;
     const int bins = (int)((r.up - 1 - r.lo) >> shift) + 1;
+    const float first = value_of(r.lo), past = value_of(r.up);
     __syncthreads();
     for (int b = 0; b < bins; ++b) {
       s.bin.weight[b][threadIdx.x] = 0.0;
@@ -442,8 +445,9 @@ __device__ inline bool cut(const Scores<T, G, A> &x, SampleShared<G> &s, Kept &k
     }
     x.each_again([&](int j, const u32x4 &raw) __attribute__((always_inline)) {
       each_score<T>(raw, [&](float e, int i) {
-        const uint32_t o = order_of(e);
-        if (o >= r.lo && o < r.up && kept(e, j + i)) {
+        if (e >= first && !(e >= past) && (whole || kept(e, j + i))) {  // (past +infinity: a NaN)
+          const uint32_t bits = __float_as_uint(e + 0.0f);  // order_of a number
+          const uint32_t o = bits ^ ((uint32_t)((int32_t)bits >> 31) | 0x80000000u);
           const uint32_t b = (o - r.lo) >> shift;
           lane_add(&s.bin.count[b][threadIdx.x], 1);
           if (by == Measure::kQuickWeight) {
@@ -752,15 +756,21 @@ __device__ inline void sample_row(const SampleArgs &a, int64_t row, SampleShared
   uint32_t from = lo;
   const int share = by_k ? (k + W - 1) / W : 32;
   if (by_k ? share <= 64 : by_p && a.n_classes > kSorted<G>) {
-    // at least that many lanes a wave, so W times as many classes, reach the wave's bound
-    float b = wave_jth(most, share);
+    // at least that many lanes a wave, so W times as many classes, reach the wave's bound: the upper
+    // half of the order of its share-th largest maximum
+    const uint32_t mine = order_of(most);
+    uint32_t o = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 16; --bit)
+      if (__popcll(__ballot(mine >= (o | 1u << bit))) >= share) o |= 1u << bit;
     if constexpr (G > 64) {
       __syncthreads();
-      if (lane == 0) s.bound[wave] = b;
+      if (lane == 0) s.found[wave] = (int)(o >> 16);
       __syncthreads();
-      b = -lanes_reduce<Max, W>(-s.bound[threadIdx.x & (W - 1)]);
+      o = (uint32_t)-lanes_reduce<Max, W>(-s.found[threadIdx.x & (W - 1)]) << 16;
+      __syncthreads();
     }
-    const uint32_t o = order_of(uniform(b));
+    o = uniform(o);
     from = o > from ? o : from;
   }
   int count = collect<T, G, A>(
@@ -849,9 +859,11 @@ int launch_sample(const SampleArgs &a, int32_t dtype, void *stream) {
     using T = decltype(t);
     const int64_t bytes = (int64_t)a.n_classes * (int)sizeof(T);
     auto of = [&](auto k, int threads) { return launch_each_row(k, threads, a, stream); };
-    // top_k of a wave's 64 maxima or more: more waves, or the bound finds nothing
+    // top_k of more than a wave's 64 maxima, of more classes than its LDS holds: more waves, or there is
+    // no bound (us, one wave / four: 8192 x 4000 bfloat16, top_k 200 326 / 272; 50,000 x 500 float, which
+    // LDS holds, 630 / 1400)
     const int k = a.top_ks || a.top_k >= a.n_classes ? 0 : a.top_k;
-    const int64_t most = k > 64 && bytes > 1024 && bytes <= 16384 ? 16384 : bytes;
+    const int64_t most = k > 64 && a.n_classes > kSorted<64> && bytes <= 16384 ? 16384 : bytes;
     if (most <= 4096) return of(sample_kernel<T, 64, 4>, 64);
     if (most <= 8192) return of(sample_kernel<T, 128, 4>, 128);
     if (a.n_rows <= 256) return of(sample_kernel<T, 1024, 8>, 1024);
