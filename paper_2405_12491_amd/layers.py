@@ -135,6 +135,20 @@ def _once(torch, backward):
     return staticmethod(run)
 
 
+# Backward passes run on autograd's own thread, where every step costs several times its usual time: what
+# the forward pass checked serves again, unless hooks on saved tensors gave other ones, and autograd has
+# set the device.
+def _dense_grad(grad):
+    grad = grad.contiguous()  # (a broadcast one, too)
+    return grad.resolve_neg() if grad.numel() == 1 else grad  # (what contiguous leaves negated)
+
+
+def _launch(name, like, *args):
+    st = getattr(_B._lib, name)(*args, _B._launch_stream(like.device))
+    if st != _B.BRIDGER_OK:
+        _B._check(st, name)
+
+
 # ---------------------------------------------------------------------------- embed
 def _check_ids(ids, offsets, device):
     """(rows, slots, ids' and offsets' arguments)."""
@@ -189,14 +203,28 @@ def _make_embed(torch):
     class Embed(torch.autograd.Function):
         @staticmethod
         def forward(ctx, table, ids, offsets, scale):
+            out = _embed(ids, table, scale, offsets, None)
             ctx.save_for_backward(ids, offsets)
-            ctx.scale, ctx.entries = scale, table.shape[0]
-            return _embed(ids, table, scale, offsets, None)
+            n, w = out.shape
+            k, ldi = (1, ids.stride(0)) if ids.dim() == 1 else (ids.shape[1], ids.stride(0))
+            entries = table.shape[0]
+            bytes_ = _B._lib.bridger_embed_backward_workspace(n, k, entries, w)
+            ctx.args = (ids.data_ptr(), ldi, _ptr(offsets), _code(table.dtype), n, k, entries, w, scale,
+                        bytes_, ids.stride())
+            return out
 
         def backward(ctx, grad):
             ids, offsets = ctx.saved_tensors
-            return (_embed_grad(ids, grad.contiguous(), ctx.entries, ctx.scale, offsets, None),
-                    None, None, None)
+            ids_ptr, ldi, off_ptr, code, n, k, entries, w, scale, bytes_, stride = ctx.args
+            grad = _dense_grad(grad)
+            if bytes_ == 0 or n <= 1 or ids.data_ptr() != ids_ptr or ids.stride() != stride or \
+                    _ptr(offsets) != off_ptr:
+                return _embed_grad(ids, grad, entries, scale, offsets, None), None, None, None
+            out = grad.new_empty((entries, w))
+            workspace = grad.new_empty(bytes_, dtype=torch.uint8)
+            _launch("bridger_embed_backward", grad, ids_ptr, ldi, off_ptr, grad.data_ptr(), w, code, n,
+                    k, entries, w, scale, out.data_ptr(), w, workspace.data_ptr(), bytes_)
+            return out, None, None, None
         backward = _once(torch, backward)
     return Embed
 
@@ -249,16 +277,24 @@ def _make_dropout(torch):
     class Dropout(torch.autograd.Function):
         @staticmethod
         def forward(ctx, x, residual, seed, p, layer):
+            out = _dropout(x, p, seed, residual, layer, None)
             ctx.save_for_backward(seed)
-            ctx.p, ctx.layer = p, layer
-            return _dropout(x, p, seed, residual, layer, None)
+            ctx.args = (seed.data_ptr(), _code(x.dtype), *out.shape, p, layer)
+            return out
 
         def backward(ctx, grad):
             seed, = ctx.saved_tensors
-            dx = None
-            if ctx.needs_input_grad[0]:
-                dx = _dropout(grad.contiguous(), ctx.p, seed, None, ctx.layer, None)
-            return dx, grad if ctx.needs_input_grad[1] else None, None, None, None
+            seed_ptr, code, n, w, p, layer = ctx.args
+            dx, (want_x, want_residual, _, _, _) = None, ctx.needs_input_grad
+            if want_x:
+                rows = _dense_grad(grad)
+                if seed.data_ptr() != seed_ptr:
+                    dx = _dropout(rows, p, seed, None, layer, None)
+                else:
+                    dx = torch.empty_like(rows)
+                    _launch("bridger_dropout", rows, rows.data_ptr(), w, None, 0, code, n, w, p,
+                            seed_ptr, layer, dx.data_ptr(), w)
+            return dx, grad if want_residual else None, None, None, None
         backward = _once(torch, backward)
     return Dropout
 
@@ -346,26 +382,40 @@ def _make_layer_norm(torch):
             _rows(x, "x", None, None, None, None)
             stats = x.new_empty((x.shape[0], 3), dtype=torch.float32)
             out, total = _layer_norm(x, weight, bias, residual, eps, None, None, stats)
-            ctx.save_for_backward(x if total is None else total, weight, stats)
+            t = x if total is None else total
+            ctx.save_for_backward(t, weight, stats)
             ctx.set_materialize_grads(False)
+            n, w = out.shape
+            code = _code(x.dtype)
+            ctx.args = (t.data_ptr(), t.stride(), _ptr(weight), stats.data_ptr(), code, n, w,
+                        _B._lib.bridger_layer_norm_backward_workspace(n, w, code))
             return out, total
 
         def backward(ctx, grad, grad_total):
             t, weight, stats = ctx.saved_tensors
-            rows = ctx.needs_input_grad[0] or ctx.needs_input_grad[3]
+            want_x, want_weight, want_bias, want_residual, _ = ctx.needs_input_grad
+            t_ptr, stride, weight_ptr, stats_ptr, code, n, w, bytes_ = ctx.args
             if grad is None:  # the sum alone was used
-                none = t.new_zeros(t.shape[1])
+                none = t.new_zeros(w)
                 dx = t.new_zeros(t.shape) if grad_total is None else grad_total
-                dweight, dbias = none, none
+                return (dx if want_x else None, none if want_weight else None,
+                        none if want_bias else None, dx if want_residual else None, None)
+            grad = _dense_grad(grad)
+            grad_total = None if grad_total is None else _dense_grad(grad_total)
+            if n <= 1 or t.data_ptr() != t_ptr or t.stride() != stride or \
+                    _ptr(weight) != weight_ptr or stats.data_ptr() != stats_ptr:
+                dx, dweight, dbias = _layer_norm_grad(grad, t, stats, weight, grad_total, None,
+                                                      want_x or want_residual, want_weight, want_bias)
             else:
-                dx, dweight, dbias = _layer_norm_grad(
-                    grad.contiguous(), t, stats, weight,
-                    None if grad_total is None else grad_total.contiguous(), None, rows,
-                    ctx.needs_input_grad[1], ctx.needs_input_grad[2])
-            return (dx if ctx.needs_input_grad[0] else None,
-                    dweight if ctx.needs_input_grad[1] else None,
-                    dbias if ctx.needs_input_grad[2] else None,
-                    dx if ctx.needs_input_grad[3] else None, None)
+                dx = torch.empty_like(grad) if want_x or want_residual else None
+                dweight = grad.new_empty((w,)) if want_weight else None
+                dbias = grad.new_empty((w,)) if want_bias else None
+                workspace = grad.new_empty(bytes_, dtype=torch.uint8) if want_weight or want_bias \
+                    else None
+                _launch("bridger_layer_norm_backward", grad, grad.data_ptr(), w, t_ptr, stride[0],
+                        stats_ptr, weight_ptr, _ptr(grad_total), w, code, n, w, _ptr(dx), w,
+                        _ptr(dweight), _ptr(dbias), _ptr(workspace), 0 if workspace is None else bytes_)
+            return (dx if want_x else None, dweight, dbias, dx if want_residual else None, None)
         backward = _once(torch, backward)
     return LayerNorm
 

@@ -968,3 +968,61 @@ def test_outputs_that_autograd_tracks_or_saves():
     some.add_(1)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.sum().backward()
+
+
+def test_negated_views():
+    """Rows of one element, the only ones whose negated views look dense, are refused; as gradients they are
+    resolved."""
+    z = torch.complex(_normal(1, 6, 1), _normal(2, 6, 1))
+    neg, seed, u = z.conj().imag, _seed(), torch.rand(6, device="cuda")
+    ids, stats = torch.zeros(6, dtype=torch.int32, device="cuda"), torch.empty(6, 3, device="cuda")
+    for call in (lambda: B.dropout(neg, 0.5, seed), lambda: B.layer_norm(neg), lambda: B.embed(ids, neg),
+                 lambda: B.embed_grad(ids, neg, 3), lambda: B.layer_norm_grad(neg, neg, stats), lambda: B.sample(neg, u)):
+        with pytest.raises(ValueError, match="resolve_neg"):
+            call()
+    for n in (1, 6):
+        up, x = z[:n].conj().imag, _normal(3, n, 1).requires_grad_()
+        assert up.is_neg()
+        plain = up.resolve_neg()
+        for f in (lambda: B.dropout(x, 0.0, seed), lambda: B.layer_norm(x, x[0])[0], lambda: B.layer_norm(x, None, x[0])[0],
+                  lambda: B.embed(ids[:1].expand(n).contiguous(), x)):
+            got, = torch.autograd.grad(f(), x, up)
+            want, = torch.autograd.grad(f(), x, plain)
+            assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("gap", [0, 3])
+def test_hooks_on_saved_tensors(gap):
+    """Gradients from saved tensors that hooks gave in place of the ones saved, laid out otherwise."""
+    def pack(t):
+        return t.clone()
+
+    def unpack(t):
+        if t.dim() == 2 and t.is_floating_point() and gap and t.shape[1] > 3:
+            return _strided(t, gap)[1]
+        return t.clone()
+    x, res, w, b = (t.requires_grad_() for t in _norm_inputs(1, 12, 20, torch.float32))
+    ids, seed, up = _ids(2, 12, 3, [4, 5, 3]), _seed(), _normal(3, 12, 20)
+    calls = [(lambda: B.layer_norm(x, w, b, residual=res)[0], (x, res, w, b)), (lambda: B.dropout(x, 0.3, seed, res), (x, res)),
+             (lambda: B.embed(ids, x, 0.5), (x,)), (lambda: B.layer_norm(x, w)[0], (x, w))]
+    for f, leaves in calls:
+        want = torch.autograd.grad(f(), leaves, up)
+        with torch.autograd.graph.saved_tensors_hooks(pack, unpack):
+            out = f()
+        got = torch.autograd.grad(out, leaves, up)
+        assert all(_same_bits(a, v) for a, v in zip(got, want))
+
+
+def test_backward_twice_and_in_another_stream():
+    """A graph that is kept gives the same gradients again, in tensors of their own."""
+    x, res, w, b = (t.requires_grad_() for t in _norm_inputs(1, 300, 257, torch.bfloat16))
+    up = _normal(3, 300, 257, dtype=torch.bfloat16)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        y, _ = B.layer_norm(B.dropout(x, 0.2, _seed(), res), w, b)
+    first = torch.autograd.grad(y, (x, res, w, b), up, retain_graph=True)
+    second = torch.autograd.grad(y, (x, res, w, b), up)
+    torch.cuda.synchronize()
+    for p, q in zip(first, second):
+        assert p.data_ptr() != q.data_ptr() and _same_bits(p, q)
