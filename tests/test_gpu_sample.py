@@ -39,9 +39,9 @@ def _u(seed, n):
     return torch.rand(n, generator=_gen(seed), device="cuda")
 
 
-def _check(z, u, what="", **how):
-    """Ids equal, but for draws nearer to another class than sums in double tell apart; logp off by its
-    rounding to float, and by that of the weights and sums in double."""
+def _check(z, u, what="", undecided=1, **how):
+    """Ids equal, but for draws nearer to another class than sums in double tell apart (`undecided` rows at
+    most); logp off by its rounding to float, and by that of the weights and sums in double."""
     ids, logp = B.sample(z, u, **how)
     zn, un, got, lp = np64(z), np64(u), ids.cpu().numpy(), np64(logp)
     per = {k: np64(v) if torch.is_tensor(v) else [v] * len(zn) for k, v in how.items()}
@@ -58,7 +58,7 @@ def _check(z, u, what="", **how):
             assert lp[r] == ref
         else:
             assert abs(lp[r] - ref) <= R.U * abs(ref) + 1e-11, f"{what} row {r}: {lp[r]}, not {ref}"
-    assert sure >= len(zn) - 1, what
+    assert sure >= len(zn) - undecided, what
     return ids, logp
 
 
@@ -233,3 +233,39 @@ def test_sample_agrees_with_top_k():
     assert torch.equal(B.sample(z, u, temperature=0.0)[0], top[:, 0])
     ids, _ = B.sample(z, u, top_k=20)
     assert bool((top == ids[:, None]).any(1).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids_of)
+@pytest.mark.parametrize("width", [257, 300, 500, 1000, 1025, 5000, 50_257, 140_000])
+def test_sample_cuts_below_what_is_ranked(width, dtype):
+    """More classes stay than are ranked by counting: by top_p, by min_p, and by the one although the other
+    would leave more; whole numbers (many equal scores at the cut), masked rows, far ranges."""
+    n = 8 if width > 10_000 else 60
+    z, u = _logits(width + 7, n, width, dtype, scale=2.0), _u(width + 8, n)
+    z[1] = z[1].round()
+    z[2, ::2] = -inf
+    z[3, 1:] -= 60.0
+    z[4] *= 20.0
+    z[5] = torch.where(z[5] > 0, 3.0, -3.0).to(dtype)
+    z[6, :width // 2] = nan
+    z[7] = z[7] * 0.001 + 40.0
+    for how in (dict(temperature=1.5, min_p=0.001), dict(temperature=3.0, min_p=0.01),
+                dict(temperature=1.5, top_p=0.95), dict(temperature=2.0, top_p=0.999, min_p=0.02),
+                dict(temperature=4.0, top_p=0.7, min_p=1e-4), dict(temperature=50.0, top_p=0.4),
+                dict(temperature=0.05, top_p=0.9999999), dict(top_p=1e-6, min_p=1e-6),
+                dict(temperature=1e6, top_p=0.5), dict(temperature=1e-5, top_p=0.5)):
+        # at 1e-5 the classes of the largest score weigh 1 and all others nearly nothing: with an even
+        # number of them the weight before one is top_p of all, exactly
+        top = (z == z.nan_to_num(-inf).amax(1, keepdim=True)).sum(1)
+        halves = int((top % 2 == 0).sum()) if how.get("temperature") == 1e-5 else 0
+        _check(z, u, f"{how}", undecided=1 + halves, **how)
+
+
+def test_sample_shares_of_bins():
+    """Cuts by top_p at each class in turn, of scores that are spread evenly, stay where the definition has
+    them."""
+    n, c = 700, 900
+    z = (torch.arange(c, device="cuda") * -0.004).expand(n, c).contiguous()
+    p = (torch.arange(n, device="cuda") + 0.5) / n
+    _check(z, _u(1, n), top_p=p)
+    _check(z.flip(1).contiguous(), _u(1, n), top_p=p, min_p=0.2)
