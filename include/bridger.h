@@ -558,6 +558,8 @@ bridger_status bridger_layer_norm(const void *x, int64_t ldx, const void *residu
  *   weight      as above;  grad_total  the gradient of total, rows lds apart, or NULL
  *   dx          of dtype, rows ldd apart, or NULL
  *   dweight, dbias  [n_features] of dtype, or NULL; written with n_rows == 0 too
+ * t - mean and factor are floats here: a row where one of them leaves float's range (elements of both
+ * signs past 2^126, a variance + eps below 2^-254) has no finite gradient.
  *   workspace   bridger_layer_norm_backward_workspace bytes, aligned to 16, of this call alone until
  *               it has run; NULL with dweight and dbias NULL
  * At least one output is given.

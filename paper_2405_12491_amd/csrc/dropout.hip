@@ -28,7 +28,9 @@ constexpr int kUnit = 8;  // elements of a row that share a block of words
 
 // A lane takes the kUnit elements from j on.  An element's 32 random bits are compared with
 // p 2^32: the upper 16 decide but for one in 65536, so that one block of words serves kUnit elements;
-// the lower 16 come from another block, which is made where some element needs it.
+// the lower 16 come from another block, which is made where some element needs it: ten rounds for 8
+// elements leave memory as the bound.  8192 x 8192 bfloat16 with a residual 69 us (5.8 TB/s, part of what
+// is written stays in the last cache), 100,000 x 347 float 54 to 56 (5.0 TB/s).
 template <typename T, int G>
 __global__ __launch_bounds__(kRowThreads<G>) void dropout_kernel(DropoutArgs a) {
   constexpr int V = kPerLoad<T>, L = kUnit / V;

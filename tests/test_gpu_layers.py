@@ -120,6 +120,20 @@ def test_embed_slots(k, width, dtype):
         _check_embed_grad(ids, grad, sum(nodes), 1.0 / k, None, f"{n}, one table")
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=ids_of)
+@pytest.mark.parametrize("width", [33, 64, 65, 130, 515, 1024, 2300, 4097])
+def test_embed_slots_of_large_tables(width, dtype):
+    """Tables past an L2 of 4 MB, and just below, whose rows are split into tiles of 128 to 512 bytes."""
+    whole = 2 ** 22 // (width * torch.empty(0, dtype=dtype).element_size())
+    for n, entries in ((1, whole + 1), (5, whole), (120, 2 * whole)):
+        table = _normal(1, entries, width, dtype=dtype)
+        cut = torch.tensor([0, entries // 3, entries // 3, entries // 2, entries], device="cuda")
+        ids = _ids(n, n, 4, (cut[1:] - cut[:-1]).clamp(min=1).tolist())
+        _check_embed(ids, table, 0.25, cut, f"{n} {entries}")
+        buf, view = _strided(table, 3, 1)
+        assert _same_bits(B.embed(ids, view, 0.25, cut), B.embed(ids, table, 0.25, cut))
+
+
 @pytest.mark.parametrize("entries", [1, 2, 3, 255, 256, 2046, 2047, 2048, 5000, 300_000, 5_000_000])
 def test_embed_grad_numbers_of_entries(entries):
     """One to three passes of the sort, and the numbers where another begins."""
