@@ -134,6 +134,24 @@ def test_embed_slots_of_large_tables(width, dtype):
         assert _same_bits(B.embed(ids, view, 0.25, cut), B.embed(ids, table, 0.25, cut))
 
 
+@pytest.mark.parametrize("n", [17, 63, 1000, 1024, 1025, 16_383, 16_384, 16_385])
+@pytest.mark.parametrize("sizes", [(1, 0, 1023, 1024, 1025, 511, 512), (0, 0, 5), (200_000, 1, 60_000), (2, 300_000)],
+                         ids=str)
+def test_embed_grad_sizes_of_slots(sizes, n):
+    """Slots of one entry to many, and of none, rows up to where slots are sorted one by one and past it."""
+    sizes = list(sizes) * max(1, 1020 // n)
+    off = torch.tensor([0, *np.cumsum(sizes)], device="cuda")
+    entries = int(off[-1])
+    ids = _ids(n, n, len(sizes), [max(v, 1) for v in sizes])
+    grad = _normal(2, n, 9)
+    _check_embed_grad(ids, grad, entries, 0.5, off, f"{n}")
+    # a table that ends inside a slot; ids that lie apart
+    short = entries - sizes[-1] // 2
+    out = _check_embed_grad(ids, grad, short, 0.5, off, f"{n}, cut")
+    _, apart = _strided(ids, 3, 1)
+    assert _same_bits(B.embed_grad(apart, grad, short, 0.5, off), out)
+
+
 @pytest.mark.parametrize("entries", [1, 2, 3, 255, 256, 2046, 2047, 2048, 5000, 300_000, 5_000_000])
 def test_embed_grad_numbers_of_entries(entries):
     """One to three passes of the sort, and the numbers where another begins."""
