@@ -390,7 +390,7 @@ struct Range {
 // One walk for a cut by quick weights: parts the scores of the range into bins of equal width, of which
 // those that may hold the cut are left.  The weights are added up as whole numbers, whose sums do not
 // depend on the order.  (512 x 50,257 float, top_p 0.95: 354 us with cut()'s bins alone, which take
-// several walks, 257 with this one first.)
+// several walks, 242 with this one first.)
 enum class Found { kRange, kUnclear, kPast };  // kPast: the whole range is less than the target
 template <typename T, int G, int A>
 __device__ inline Found narrow(const Scores<T, G, A> &x, SampleShared<G> &s, const Weights &weight,
@@ -941,8 +941,10 @@ __device__ inline void store_draw(const SampleArgs &a, int64_t row, const Sample
 }
 
 // A workgroup of G lanes a row, with kRing loads on their way.  Many rows: few of them, in so few
-// registers that two workgroups of 1024 lanes share a compute unit (2048 x 128,000 bfloat16, top_k 50:
-// 230 us, one at a time 266).  A row or two for each compute unit: more (1 x 128,000: 22 us, 28).
+// registers that two workgroups of 1024 lanes share a compute unit and hide each other's waits, though some
+// registers spill (512 x 50,257 float, top_k 50: two loads 49 us, four 51, four with twice the registers 57;
+// top_p 0.95: 242, 258, 260; 2048 x 128,000 without cuts 682, 744, 776).  A row or two for each compute
+// unit: more (1 x 128,000 bfloat16: 22 us, 28).
 template <typename T, int G, int kRing>
 __global__ __launch_bounds__(G, G >= 512 && kRing < 8 ? 8 : 4) void sample_kernel(SampleArgs a) {
   __shared__ __attribute__((aligned(16))) SampleShared<G> s;
@@ -965,8 +967,8 @@ int launch_sample(const SampleArgs &a, int32_t dtype, void *stream) {
     if (most <= 8192) return of(sample_kernel<T, 128, 4>, 128);
     if (a.n_rows <= 256) return of(sample_kernel<T, 1024, 8>, 1024);
     if (most <= 32768) return of(sample_kernel<T, 256, 4>, 256);
-    if (most <= 65536) return of(sample_kernel<T, 512, 4>, 512);
-    return of(sample_kernel<T, 1024, 4>, 1024);
+    if (most <= 65536) return of(sample_kernel<T, 512, 2>, 512);
+    return of(sample_kernel<T, 1024, 2>, 1024);
   });
 }
 
