@@ -742,35 +742,37 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(GradArgs a) {
   const Place p = place_of<G, W>(a.e, a.first);
   const int group = threadIdx.x / G, width = a.e.n_features;
   const int64_t block0 = p.block * kHeads;
-  if (threadIdx.x < kHeads) {
-    const int64_t block = block0 + threadIdx.x, end = (block + 1) * a.length;
+  {
+    constexpr int lanes = kThreads / kHeads;  // of a block
+    static_assert(lanes == 16, "a step's results are 16 bits of a ballot");
+    const int h = threadIdx.x / lanes, r = threadIdx.x % lanes;
+    const int64_t block = block0 + h, begin = block * a.length, end = begin + a.length;
     int32_t count = 0;
     uint32_t key = 0;
     if (end < a.pairs) {
       key = a.sorted[end - 1].key;
-      const int64_t begin = block * a.length;
-      if (key < (uint32_t)a.e.n_entries && a.sorted[end].key == key &&
-          (begin == 0 || a.sorted[begin - 1].key != key)) {
-        // the last block that begins with the entry: in growing steps, then by halves
-        int64_t lo = block + 1, step = 1;
-        while (lo + step < a.blocks && a.sorted[(lo + step) * a.length].key == key) {
-          lo += step;
-          step *= 2;
+      const uint32_t after = a.sorted[end].key;
+      const uint32_t before = begin > 0 ? a.sorted[begin - 1].key : ~key;
+      if (key < (uint32_t)a.e.n_entries && after == key && before != key) {
+        // the last block that begins with the entry: 16 probes a step, growing steps, then shrinking
+        int64_t last_block = block + 1, step = 1;
+        auto go = [&] {
+          const int64_t probe = last_block + (r + 1) * step;
+          const bool hit = probe < a.blocks && a.sorted[probe * a.length].key == key;
+          const uint32_t hits = (uint32_t)(__ballot(hit) >> (threadIdx.x & 48)) & 0xFFFFu;
+          const int n = __builtin_ctz(~hits);
+          last_block += n * step;
+          return n;
+        };
+        while (go() == lanes) step *= lanes;
+        while (step > 1) {
+          step /= lanes;
+          go();
         }
-        int64_t hi = lo + step < a.blocks ? lo + step : a.blocks;  // the first that does not, or later
-        while (hi - lo > 1) {
-          const int64_t mid = (lo + hi) / 2;
-          if (a.sorted[mid * a.length].key == key) {
-            lo = mid;
-          } else {
-            hi = mid;
-          }
-        }
-        count = (int32_t)(lo - block);
+        count = (int32_t)(last_block - block);
       }
     }
-    last[threadIdx.x] = count;
-    entry[threadIdx.x] = key;
+    if (r == 0) last[h] = count, entry[h] = key;
   }
   __syncthreads();
   // sum += those of blocks [c, end)
