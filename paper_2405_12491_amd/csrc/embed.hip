@@ -131,7 +131,8 @@ __global__ __launch_bounds__(kThreads) void embed_bag_kernel(EmbedArgs a) {
   for (int64_t s0 = part * U; s0 < a.n_slots; s0 += (int64_t)a.parts * U) {
     int32_t at = -1;
     if (lane < U && s0 + lane < a.n_slots) at = entry_of(a, row, (int)(s0 + lane));
-    const int64_t offset = at * a.ldt * (int64_t)sizeof(T);  // (below 0: none)
+    // below 0: none (whatever the distance of a table's only entry is)
+    const int64_t offset = at < 0 ? -1 : at * a.ldt * (int64_t)sizeof(T);
     Elements<T, W> e[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {

@@ -238,6 +238,34 @@ def test_embed_offsets_past_the_table():
     assert bool((grad[4:] == 0).all())
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=ids_of)
+@pytest.mark.parametrize("width", [1, 5, 64, 130, 700])
+def test_embed_one_entry_at_any_distance(width, dtype):
+    """The distance between rows counts for nothing where there is one: a table of one entry, and one row."""
+    code = list(NAMES).index(dtype)
+    table, grad = _normal(1, 1, width, dtype=dtype), _normal(2, 9, width, dtype=dtype)
+    ids = torch.tensor([[0, -1, 0], [-1, -1, -1], [1, 0, 2 ** 31 - 1]] * 3, dtype=torch.int32, device="cuda")
+    off = torch.tensor([0, 1, 1, 1], device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    for n, k in ((9, 3), (1, 3), (9, 1)):
+        own, g = ids[:n, :k].contiguous(), grad[:n]
+        for offsets in (None, off[:k + 1]):
+            ref, tol = L.embed(own, table, 1.5, offsets)
+            gref, gtol = L.embed_grad(own, g, 1, 1.5, offsets)
+            bytes_ = B.bridger_embed_backward_workspace(n, k, 1, width)
+            workspace = torch.empty(bytes_, dtype=torch.uint8, device="cuda")
+            for ld in (0, -1, width - 1, 10 ** 12, 2 ** 62, -2 ** 62):
+                out, got = torch.full((n, width), nan, dtype=dtype, device="cuda"), torch.full_like(table, nan)
+                row = [k, width, width] if n > 1 else [ld] * 3
+                at = None if offsets is None else offsets.data_ptr()
+                B.bridger_embed(own.data_ptr(), row[0], at, table.data_ptr(), ld, code, n, k, 1, width, 1.5,
+                                out.data_ptr(), row[1], stream)
+                R.assert_near(out, ref, tol, dtype, f"{n} {k} {ld}")
+                B.bridger_embed_backward(own.data_ptr(), row[0], at, g.data_ptr(), row[2], code, n, k, 1, width, 1.5,
+                                         got.data_ptr(), ld, workspace.data_ptr(), bytes_, stream)
+                R.assert_near(got, gref, gtol, dtype, f"{n} {k} {ld}: gradient")
+
+
 def test_embed_no_rows():
     table = _normal(1, 9, 12)
     none = torch.empty(0, 4, dtype=torch.int32, device="cuda")
