@@ -34,10 +34,14 @@ struct RowLoads {
       }
     }
   }
-  __device__ void take(int lane, int n) {
+  // Past the row's end stand zeros, or where `repeat` is set its last element (zeros with G = 1).
+  __device__ void take(int lane, int n, bool repeat = false) {
     if constexpr (G > 1) {
 #pragma unroll
-      for (int c = 0; c < C; ++c) l[c].take((c * G + lane) * kPerLoad<T>, n, 0);
+      for (int c = 0; c < C; ++c) {
+        const uint32_t last = sizeof(T) == 4 ? l[c].raw[3] : (l[c].raw[3] >> 16) * 0x10001u;
+        l[c].take((c * G + lane) * kPerLoad<T>, n, repeat ? last : 0);
+      }
     }
   }
   __device__ float at(int c, int i) const { return element<T>(l[c].raw, i); }
@@ -263,14 +267,14 @@ __global__ __launch_bounds__(kRowThreads<G>) void layer_norm_backward_kernel(Lay
     if (a.grad_total) s.issue((const T *)a.grad_total + row * a.lds, lane, n);
     const float *k = a.stats + 3 * row;
     const float high = k[0], low = k[1], inverse = k[2];
-    x.take(lane, n);
+    x.take(lane, n, true);  // (a zero's h may be infinite)
     g.take(lane, n);
     float sum = 0.0f, along = 0.0f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float h = (x.at(c, i) - high - low) * inverse;
+        const float h = G > 1 || i < n ? (x.at(c, i) - high - low) * inverse : 0.0f;
         const float v = a.weight ? g.at(c, i) * w.at(c, i) : g.at(c, i);
         sum += v;
         along += v * h;
@@ -367,7 +371,7 @@ __global__ __launch_bounds__(kLong) void layer_norm_backward_long_kernel(LayerNo
       float h[V], v[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        h[i] = (element<T>(xl.raw, i) - high - low) * inverse;
+        h[i] = j + i < n ? (element<T>(xl.raw, i) - high - low) * inverse : 0.0f;
         v[i] = element<T>(gl.raw, i);
         if (w) v[i] *= element<T>(wl.raw, i);
       }

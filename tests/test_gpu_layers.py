@@ -495,6 +495,24 @@ def test_layer_norm_equal_and_broken_rows(width, dtype):
     R.assert_near(db, rb, tb, dtype)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=ids_of)
+@pytest.mark.parametrize("width", [1, 3, 5, 28, 32, 100, 700, 1030, 4100, 9000, 40_000, 70_001])
+def test_layer_norm_grad_of_equal_rows(width, dtype):
+    """Rows of one value have a finite gradient, factor (s - mean(s)), however large the value is: what stands
+    past a row's end takes no part in it."""
+    low = float(torch.finfo(dtype).min)
+    for residual in (False, True):
+        x = torch.tensor([1e37, 3e36, -2.0 ** 120, low / 2, low, 3.0, 0.0], device="cuda")[:, None].expand(7, width).to(dtype)
+        x = x.contiguous()
+        _, _, w, b = _norm_inputs(1, 7, width, dtype)
+        res = torch.zeros_like(x) if residual else None
+        _check_norm(x, res, w, b)
+        _check_norm(x, res, None, None)
+        stats = torch.empty(7, 3, device="cuda")
+        B.layer_norm(x, w, b, stats=stats)
+        assert all(bool(torch.isfinite(v).all()) for v in B.layer_norm_grad(_normal(2, 7, width, dtype=dtype), x, stats, w))
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=ids_of)
 @pytest.mark.parametrize("width,gap,lead", [(1, 1, 1), (5, 3, 1), (64, 7, 3), (515, 1, 0), (5003, 2, 5), (70_001, 3, 1)])
 def test_layer_norm_strided_and_in_place(width, gap, lead, dtype):
