@@ -842,7 +842,7 @@ __device__ inline void sample_row(const SampleArgs &a, int64_t row, SampleShared
     }
   }
   uint32_t from = lo;
-  const int share = by_k ? (k + W - 1) / W : 32;
+  const int share = by_k ? (k - 1) / W + 1 : 32;
   if (by_k ? share <= 64 : by_p && a.n_classes > kSorted<G>) {
     // at least that many lanes a wave, so W times as many classes, reach the wave's bound: the upper
     // half of the order of its share-th largest maximum

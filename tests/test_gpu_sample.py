@@ -269,3 +269,21 @@ def test_sample_shares_of_bins():
     p = (torch.arange(n, device="cuda") + 0.5) / n
     _check(z, _u(1, n), top_p=p)
     _check(z.flip(1).contiguous(), _u(1, n), top_p=p, min_p=0.2)
+
+
+@pytest.mark.parametrize("own", [False, True])
+def test_sample_top_k_near_its_largest(own):
+    """top_k within a step of 2^31, of a row with more classes, nearly all of them masked."""
+    n = 2 ** 31 - 1
+    z = torch.full((1, n), -inf, dtype=torch.bfloat16, device="cuda")
+    at = torch.cat([torch.randint(0, n, (97,), generator=_gen(1), device="cuda"), torch.tensor([0, n - 1], device="cuda")])
+    z[0, at] = _logits(2, 1, 99, torch.bfloat16)[0]
+    some = torch.unique(at)
+    scores = np64(z[0, some])
+    for k in (n - 15, n - 1, n // 2 + 3):
+        for u in (0.0, 0.3, 0.9999):
+            top_k = torch.tensor([k], dtype=torch.int32, device="cuda") if own else k
+            ids, logp = B.sample(z, torch.tensor([u], device="cuda"), temperature=1.3, top_k=top_k, top_p=0.9)
+            want, ref, _, gap = L.sample_row(scores, float(np.float32(u)), temperature=1.3, top_k=k, top_p=0.9)
+            assert gap > 1e-11
+            assert int(ids) == int(some[want]) and abs(float(logp) - ref) <= R.U * abs(ref) + 1e-11
