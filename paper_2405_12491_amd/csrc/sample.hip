@@ -486,7 +486,11 @@ __device__ inline bool cut(const Scores<T, G, A> &x, SampleShared<G> &s, Kept &k
     const bool one = r.up - r.lo == 1;
     if (one || r.within <= kSorted<G>) {
       const int count = collect<T, G, A>(x, s, kept, r.lo, r.up);
-      if (count == 0) return true;  // all of it stays: rounding leaves the target past the last
+      if (count == 0) {  // rounding leaves the target past the range's last: it stays, and nothing below
+        const float last = value_of(r.lo);
+        if (last > kept.score) kept.score = last, kept.cls = INT32_MAX;
+        return true;
+      }
       if (count <= kSorted<G>) {
         sort_candidates<G>(s, count);
         int stay = r.most < count ? (int)r.most : count;

@@ -1,5 +1,7 @@
 """sample on the GPU against its definition in 64 bits (layers_ref.sample_row): widths from one class to
 long rows, every cut alone and with others, equal scores, masked and broken rows, parameters by row."""
+import math
+
 import numpy as np
 import pytest
 
@@ -287,3 +289,64 @@ def test_sample_top_k_near_its_largest(own):
             want, ref, _, gap = L.sample_row(scores, float(np.float32(u)), temperature=1.3, top_k=k, top_p=0.9)
             assert gap > 1e-11
             assert int(ids) == int(some[want]) and abs(float(logp) - ref) <= R.U * abs(ref) + 1e-11
+
+
+def _check_consistent(z, u, what="", **how):
+    """Every row's class and logp are those of sums that are off by 1e-11 of all at most, near a border too."""
+    ids, logp = B.sample(z, u, **how)
+    zn, un, got, lp = np64(z), np64(u), ids.cpu().numpy(), np64(logp)
+    top_k, p, T, m = (how.get(k, d) for k, d in (("top_k", 0), ("top_p", 1.0), ("temperature", 1.0), ("min_p", 0.0)))
+    for r in range(len(zn)):
+        cls = np.flatnonzero(zn[r] > -np.inf)
+        cls = cls[np.argsort(-zn[r, cls], kind="stable")]
+        v = zn[r, cls[:top_k or None]]
+        w = np.exp((v - v[0]) / T)
+        before = np.concatenate([[0.0], np.cumsum(w)])
+        limit, doubt = p * before[-1], 1e-11 * before[-1]
+        # the classes that may be the last to stay, and what stays for the fewest and the most
+        fewest, most = (max(1, int((before[:-1] < limit + d).sum())) for d in (-doubt, doubt)) if p < 1 else (len(w),) * 2
+        above = int((v >= v[0] + T * np.log(m)).sum()) if m > 0 else len(w)
+        rank = np.flatnonzero(cls == got[r])
+        assert len(rank) == 1 and rank[0] < min(most, above), f"{what} row {r}: class {got[r]} does not stay"
+        fits = []
+        for stay in sorted({min(s, above) for s in (fewest, max(fewest, rank[0] + 1), most)}):
+            if stay > rank[0]:
+                order = np.argsort(cls[:stay])
+                sums = np.cumsum(w[:stay][order])
+                at = int(np.flatnonzero(cls[:stay][order] == got[r])[0])
+                begin, target = sums[at] - w[rank[0]], un[r] * sums[-1]
+                fits.append(begin - doubt <= target <= sums[at] + doubt and
+                            abs(lp[r] - np.log(w[rank[0]] / sums[-1])) <= R.U * abs(lp[r]) + 1e-10)
+        assert any(fits), f"{what} row {r}: class {got[r]}, logp {lp[r]}"
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids_of)
+@pytest.mark.parametrize("width", [257, 1025, 5000, 50_257, 140_000])
+def test_sample_near_borders(width, dtype):
+    """Halves that are exact but for rounding, and draws at a class's edge: one of the two neighbours."""
+    z = _logits(width + 7, 8, width, dtype, scale=2.0)
+    z[1] = z[1].round()
+    z[2, ::2] = -inf
+    z[3, :width // 2] = z[3, 0]
+    u = _u(width, 8)
+    u[::3] = 0.5
+    for how in (dict(temperature=1e-5, top_p=0.5), dict(temperature=1e6, top_p=0.5), dict(top_p=0.5, temperature=50.0),
+                dict(temperature=1e6, top_k=width // 2 * 2, top_p=0.25), dict(temperature=1e6), dict(top_p=0.5, min_p=0.3)):
+        _check_consistent(z, u, f"{how}", **how)
+
+
+@pytest.mark.parametrize("width,head", [(9000, 3000), (20_000, 2500), (50_257, 4000)])
+def test_sample_cut_at_the_end_of_a_cluster(width, head):
+    """A share of the classes stands close together, and top_p is their share of the mass, to the last bits:
+    they stay, and one more at most."""
+    rng = np.random.default_rng(width)
+    for turn in range(8):
+        z = rng.uniform(-1.0, 0.0, width).astype(np.float32)
+        place = rng.permutation(width)[:head]
+        z[place] = np.float32(4.0) + np.float32(2.0 ** -21) * rng.integers(0, 1500 * (turn + 1), head).astype(np.float32)
+        w = np.exp(z.astype(np.float64) - z.max())
+        p = math.fsum(w[place]) / math.fsum(w)
+        rows = torch.from_numpy(z).cuda().expand(3, width).contiguous()
+        u = torch.tensor([0.1, 0.5, 0.999], device="cuda")
+        for ulps in range(-4, 5):
+            _check_consistent(rows, u, f"{turn} {ulps}", top_p=p + ulps * np.spacing(p))
