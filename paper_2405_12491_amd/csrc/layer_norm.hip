@@ -50,7 +50,8 @@ struct RowLoads {
 // G lanes a row, C loads a lane; the row stays in registers from its one read to the store.  Sums
 // in float: the first gives a mean m near the true one, the second those of t - m and its square,
 // from which the mean's rest and the variance follow without cancellation.  Where a sum leaves
-// float's middle range (rows of huge or tiny elements, broken ones) both are taken in double.
+// float's middle range (rows of huge or tiny elements, broken ones), or m is off by more than a quarter
+// of the deviation (elements 2^19 deviations and more from zero), both are taken in double.
 // Bound by memory: 8192 x 4096 bfloat16 with a residual and its total 45 us (5.9 TB/s, part of it stays in
 // the last cache), 1,000,000 x 28 float 50 (4.5 TB/s).
 template <typename T, int G, int C>
@@ -93,9 +94,11 @@ __global__ __launch_bounds__(kRowThreads<G>) void layer_norm_kernel(LayerNormArg
   }
   rest = row_reduce<Sum, G>(rest, lds_rest);
   square = row_reduce<Sum, G>(square, lds_square);
-  const float low = rest / (float)n, variance = square / (float)n - low * low + a.eps;
+  const float low = rest / (float)n, spread = square / (float)n - low * low;
+  const float variance = spread + a.eps;
   Moments k = {m, low, 1.0f / __builtin_sqrtf(variance)};
-  const bool fine = moderate(variance) && fabsf(m) < 0x1p100f;
+  // (where the first sum misses the mean by much of the deviation, too little of both is left)
+  const bool fine = moderate(variance) && fabsf(m) < 0x1p100f && 16.0f * low * low <= spread;
   double mean = 0.0, inverse = 0.0;
   if (!fine) {  // of the whole row
     double s = 0.0, q = 0.0;

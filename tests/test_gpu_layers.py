@@ -458,6 +458,20 @@ def test_layer_norm_far_from_zero(width):
     _check_norm(x, None, None, None, eps=1e-9)
 
 
+@pytest.mark.parametrize("eps", [1e-5, 1e-12])
+@pytest.mark.parametrize("width", [28, 1023, 4099, 8001, 13_001, 16_001])
+def test_layer_norm_far_rows_of_nearly_equal_elements(width, eps):
+    """Rows whose sum in float misses the mean by more than their spread: a few elements one step above the
+    others."""
+    rng = np.random.default_rng(width)
+    first = np.array([12552103.544, 1814612.83, 843109.795, 259470249.0, 7512806.0, 1794.0023, -3.3e8, 77.7], np.float32)
+    share = np.array([0.01, 0.001, 0.5])
+    step = np.spacing(np.abs(first))
+    x = np.concatenate([first[:, None] + step[:, None] * (rng.random((8, width)) < p) for p in share]).astype(np.float32)
+    assert np.all((x == np.tile(first, 3)[:, None]) | (x == np.tile(first + step, 3)[:, None]))
+    _check_norm(torch.from_numpy(x).cuda(), None, None, None, eps=eps)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=ids_of)
 @pytest.mark.parametrize("width", [3, 5, 28, 700, 9000, 70_000])
 def test_layer_norm_extremes(width, dtype):
