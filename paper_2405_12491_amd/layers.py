@@ -6,10 +6,12 @@ gradients ``embed_grad`` and ``layer_norm_grad`` follow the rules of the row ope
 2-D tensors whose rows are contiguous, at any distance, on any device, launched on torch's current
 stream of that device, no CPU fallback.
 
-A call whose inputs need a gradient is differentiated (once).  A stream that is being captured
-refuses such calls: autograd keeps nodes on the streams they were made on, and a captured backward
-pass that meets one of an eager graph ends the process.  There call the layer and then its gradient's
-function (dropout's is dropout of the gradient) under ``torch.no_grad()``.
+A call of ``embed``, ``dropout`` or ``layer_norm`` whose inputs need a gradient is differentiated, in
+reverse mode, once; tensors with a tangent of forward mode are refused.  ``embed_grad`` and
+``layer_norm_grad`` pass no gradient and no tangent on, whatever their inputs.  A stream that is being
+captured refuses calls that autograd tracks: it keeps nodes on the streams they were made on, and a
+captured backward pass that meets one of an eager graph ends the process.  There call the layer and
+then its gradient's function (dropout's is dropout of the gradient) under ``torch.no_grad()``.
 """
 from __future__ import annotations
 
@@ -97,6 +99,15 @@ def bridger_layer_norm_backward(grad_ptr, ldg, t_ptr, ldt, stats_ptr, weight_ptr
 
 
 # ------------------------------------------------------------------------- autograd
+def _no_tangents(name, *tensors):
+    """Refuses tensors with a tangent, which would be lost (outputs: left as it was).  (Asked within a
+    level of forward mode only: unpack_dual takes 0.3 us a tensor outside, too.)"""
+    for t in tensors:
+        if isinstance(t, _O._torch.Tensor) and _O._forward_ad.unpack_dual(t).tangent is not None:
+            raise NotImplementedError(f"{name} has no derivative in forward mode: it takes no tensor "
+                                      "with a tangent")
+
+
 def _tracked(name, instead, *inputs):
     """Whether autograd has to see the call."""
     torch = _O._torch
@@ -236,6 +247,8 @@ def embed(ids, table, scale: float = 1.0, offsets=None, out=None):
     tree_offsets).  Ids outside are empty slots.  Differentiable in the table."""
     if _O._torch is None:
         _O._setup()
+    if _O._forward_ad._current_level >= 0:
+        _no_tangents("embed", table, out)
     if _tracked("embed", "embed and embed_grad under no_grad()", table):
         _untracked_output(out, "embed")
         return _function("embed", _make_embed).apply(table, ids, offsets, float(scale))
@@ -308,6 +321,8 @@ def dropout(x, p: float, seed, residual=None, layer: int = 0, out=None):
     the gradient of x is ``dropout(grad, p, seed, layer=layer)``.  ``out`` may be x or residual."""
     if _O._torch is None:
         _O._setup()
+    if _O._forward_ad._current_level >= 0:
+        _no_tangents("dropout", x, residual, out)
     if _tracked("dropout", "dropout of the gradient under no_grad()", x, residual):
         _untracked_output(out, "dropout")
         return _function("dropout", _make_dropout).apply(x, residual, seed, float(p), int(layer))
@@ -428,6 +443,8 @@ def layer_norm(x, weight=None, bias=None, residual=None, eps: float = 1e-5, out=
     ``stats`` (float32 [n, 3]) is written for layer_norm_grad."""
     if _O._torch is None:
         _O._setup()
+    if _O._forward_ad._current_level >= 0:
+        _no_tangents("layer_norm", x, weight, bias, residual, out, total, stats)
     if _tracked("layer_norm", "layer_norm and layer_norm_grad under no_grad()", x, weight, bias,
                 residual):
         for t in (out, total, stats):

@@ -90,12 +90,14 @@ def bridger_matmul_q8(a_ptr, lda, a_scale_ptr, b_ptr, ldb, b_scale_ptr, bias_ptr
 # A call on few rows is bound by its way to the launch: torch and its types are looked up once, a
 # tensor's properties read once, and the entry points called without the functions above.
 _torch = None
+_forward_ad = None
 _codes = {}  # torch dtype -> BRIDGER_*
 
 
 def _setup():
-    global _torch
+    global _torch, _forward_ad
     import torch
+    _forward_ad = torch.autograd.forward_ad
     _B.load_library()
     _codes.update({torch.float32: BRIDGER_F32, torch.bfloat16: BRIDGER_BF16,
                    torch.float16: BRIDGER_F16})

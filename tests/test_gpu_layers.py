@@ -634,6 +634,29 @@ def test_layers_are_differentiated_once(call):
         grad.sum().backward()
 
 
+def test_forward_mode():
+    """No call gives up a tangent without a word: those that have gradients refuse it."""
+    import torch.autograd.forward_ad as fa
+    x, res, w, b = _norm_inputs(1, 6, 40, torch.float32)
+    ids, seed, one = torch.zeros(3, dtype=torch.int32, device="cuda"), _seed(), torch.ones(6, 40, device="cuda")
+    plain = [B.embed(ids, x), B.dropout(x, 0.5, seed), B.layer_norm(x, w, b, residual=res)[0]]
+    with fa.dual_level():
+        # beside other work in forward mode
+        same = [B.embed(ids, x), B.dropout(x, 0.5, seed), B.layer_norm(x, w, b, residual=res)[0]]
+        assert all(_same_bits(p, q) for p, q in zip(plain, same))
+        for leaf in (x, x.clone().requires_grad_()):
+            d = fa.make_dual(leaf, one)
+            for call in (lambda: B.embed(ids, d), lambda: B.dropout(d, 0.5, seed), lambda: B.dropout(x, 0.5, seed, d),
+                         lambda: B.layer_norm(d, w, b), lambda: B.layer_norm(x, w, b, residual=d)):
+                with pytest.raises(NotImplementedError):
+                    call()
+    for f in (lambda t: B.embed(ids, t), lambda t: B.dropout(t, 0.5, seed), lambda t: B.layer_norm(t)[0]):
+        with pytest.raises(RuntimeError):
+            torch.func.jvp(f, (x,), (one,))
+        with pytest.raises(RuntimeError):
+            torch.func.grad(lambda t: f(t).sum())(x)
+
+
 # ------------------------------------------------------------- together, streams, graphs
 def _every(seed=0, n=65, c=1030):
     """name -> (inputs that a replay may scale, call): each operator without autograd."""

@@ -148,6 +148,31 @@ def test_cpu_tensors_are_refused():
             call()
 
 
+def test_tangents_are_refused():
+    """What the layers differentiate gives no tangents: inputs and outputs that have one are refused, in
+    grad mode and without; tensors without one are as ever."""
+    import torch
+    import torch.autograd.forward_ad as fa
+    x, w, seed = torch.zeros(3, 8), torch.zeros(8), torch.zeros(2, dtype=torch.int64)
+    ids = torch.zeros(3, 2, dtype=torch.int32)
+    calls = [lambda d, v: B.embed(ids, d), lambda d, v: B.embed(ids, x, out=d), lambda d, v: B.dropout(d, 0.5, seed),
+             lambda d, v: B.dropout(x, 0.5, seed, residual=d), lambda d, v: B.dropout(x, 0.5, seed, out=d),
+             lambda d, v: B.layer_norm(d), lambda d, v: B.layer_norm(x, v), lambda d, v: B.layer_norm(x, w, v),
+             lambda d, v: B.layer_norm(x, residual=d), lambda d, v: B.layer_norm(x, out=d),
+             lambda d, v: B.layer_norm(x, total=d), lambda d, v: B.layer_norm(x, stats=d)]
+    with fa.dual_level():
+        d, v = fa.make_dual(x, torch.ones(3, 8)), fa.make_dual(w, torch.ones(8))
+        for i, call in enumerate(calls):
+            for grad in (True, False):
+                with torch.set_grad_enabled(grad), pytest.raises(NotImplementedError, match="tangent"):
+                    call(d, v)
+                    pytest.fail(f"call {i} was not refused")
+            with pytest.raises(TypeError, match="CUDA"):
+                call(x, w)
+    with pytest.raises(TypeError, match="CUDA"):
+        B.embed(ids, x)
+
+
 def test_raw_calls_report_their_errors():
     with pytest.raises(B.BridgerError, match="n_slots") as e:
         B.bridger_embed(A[0], 3, None, A[2], 10, 0, 5, 0, 7, 10, 1.0, A[3], 10)
