@@ -476,8 +476,8 @@ bridger_status bridger_matmul_q8(const int8_t *a, int64_t lda, const float *a_sc
  *     out[r] = scale * sum_s table[first_s + ids[r, s]]
  * over the slots s of the row.  Slot s reads the entries [offsets[s], offsets[s + 1]) of the table
  * (a forest's tree offsets: predict_leaves' ids of tree s), or all of them without offsets.  An id
- * outside its slot's entries, or outside the table, is an empty slot and adds nothing; a row of
- * empty slots is zero.
+ * outside its slot's entries, or outside the table, is an empty slot and adds nothing (a slot that
+ * begins below 0 is empty, too); a row of empty slots is zero.
  *   ids      int32 [n_rows, n_slots], rows ldi apart;  1 <= n_slots < 2^31
  *   offsets  int64 [n_slots + 1], ascending, or NULL
  *   table    [n_entries, n_features] of dtype, rows ldt apart;  1 <= n_entries, n_features < 2^31
@@ -494,6 +494,8 @@ bridger_status bridger_embed(const int32_t *ids, int64_t ldi, const int64_t *off
  *     grad_table[e] = scale * sum of grad[r] over the slots (r, s) that read entry e,
  * zero for an entry that none reads.  The slots are sorted by entry and added in an order that the
  * ids alone decide; every entry is written, with n_rows == 0 too.
+ *   offsets     as above; where they descend, so that two slots read the same entries, the gradients
+ *               of those are undefined
  *   grad        [n_rows, n_features] of dtype, rows ldg apart
  *   grad_table  [n_entries, n_features] of dtype, rows ldt apart
  *   workspace   bridger_embed_backward_workspace bytes, aligned to 16, of this call alone until it

@@ -242,8 +242,8 @@ def _make_embed(torch):
 
 def embed(ids, table, scale: float = 1.0, offsets=None, out=None):
     """Rows of ``table`` [entries, width] that ``ids`` (int32 [n] or [n, slots]) name, added over a
-    row's slots and times ``scale``: [n, width].  With ``offsets`` (int64 [slots + 1]) slot s reads
-    the entries offsets[s] to offsets[s + 1] (a forest's leaves: predict_leaves' ids and the model's
+    row's slots and times ``scale``: [n, width].  With ``offsets`` (int64 [slots + 1], ascending) slot s
+    reads the entries offsets[s] to offsets[s + 1] (a forest's leaves: predict_leaves' ids and the model's
     tree_offsets).  Ids outside are empty slots.  Differentiable in the table."""
     if _O._torch is None:
         _O._setup()
@@ -257,7 +257,8 @@ def embed(ids, table, scale: float = 1.0, offsets=None, out=None):
 
 def embed_grad(ids, grad, n_entries: int, scale: float = 1.0, offsets=None, out=None):
     """The gradient [n_entries, width] of embed's table, from that of its output ``grad``
-    [n, width] (of its type).  The same ids give the same order of sums."""
+    [n, width] (of its type).  The same ids give the same order of sums.  ``offsets`` ascend: where they
+    descend, so that two slots read the same entries, those entries' gradients are undefined."""
     if _O._torch is None:
         _O._setup()
     return _embed_grad(ids, grad, int(n_entries), float(scale), offsets, out)
@@ -439,8 +440,8 @@ def layer_norm(x, weight=None, bias=None, residual=None, eps: float = 1e-5, out=
                stats=None):
     """Layer norm of every row of x (+ residual, the sum rounded to x's type), times ``weight`` [w],
     plus ``bias`` [w]: (norm [n, w], total), total being x + residual (None without a residual or a
-    ``total`` to write).  Differentiable in all four.  ``total`` may be x or residual itself;
-    ``stats`` (float32 [n, 3]) is written for layer_norm_grad."""
+    ``total`` to write).  All four are of x's type.  Differentiable in them.  ``total`` may be x or
+    residual itself; ``stats`` (float32 [n, 3]) is written for layer_norm_grad."""
     if _O._torch is None:
         _O._setup()
     if _O._forward_ad._current_level >= 0:

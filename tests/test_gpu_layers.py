@@ -238,6 +238,23 @@ def test_embed_offsets_past_the_table():
     assert bool((grad[4:] == 0).all())
 
 
+@pytest.mark.parametrize("n", [50, 4000, 17_000])
+def test_embed_grad_offsets_past_the_table(n):
+    """The same for the gradient, however many pairs are sorted and however: by all of them, by slots, in passes.
+    Slots that share no entry may stand in any order."""
+    ids = torch.randint(-2, 12, (n, 5), generator=_gen(n), device="cuda", dtype=torch.int32)
+    table, grad = _normal(1, 8, 6), _normal(2, n, 6)
+    for off in ([0, 4, 4, 9, 30, 2 ** 62], [6, 8, 0, 3, 3, 5]):
+        _check_embed(ids, table, 0.5, torch.tensor(off, device="cuda"), f"{off}")
+        _check_embed_grad(ids, grad, 8, 0.5, torch.tensor(off, device="cuda"), f"{off}")
+    # a slot that begins below 0 is empty
+    off, cut = torch.tensor([0, 4, -3, 6, 8, 20], device="cuda"), ids.clone()
+    cut[:, 2] = -1
+    assert _same_bits(B.embed(ids, table, offsets=off), B.embed(cut, table, offsets=off))
+    _check_embed_grad(cut, grad, 8, 0.5, off)
+    assert _same_bits(B.embed_grad(ids, grad, 8, 0.5, off), B.embed_grad(cut, grad, 8, 0.5, off))
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=ids_of)
 @pytest.mark.parametrize("width", [1, 5, 64, 130, 700])
 def test_embed_one_entry_at_any_distance(width, dtype):
