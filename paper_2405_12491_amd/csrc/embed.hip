@@ -114,8 +114,10 @@ __device__ inline uint32_t of_lane(uint32_t v, int u) {
 }
 
 // Several slots a row: a.parts groups of G lanes share a row's slots and join in LDS.  Each lane of a
-// group finds the entry of one of the next slots, and all of them take each entry in turn.  Bound by the
-// caches: 16,384 rows of 100 slots, 64 floats each, 28 us (419 MB at 15 TB/s).
+// group finds the entry of one of the next slots, and all of them take each entry in turn.  16,384 rows of
+// 100 slots, 64 floats each of a table of 13 MB: 28 us, 419 MB from the caches.  Their rate (15 TB/s) and the
+// instructions (13 us of the vector units, as many for 8 bfloat16 a lane as for 4 floats) share the bound:
+// with bfloat16 19 us; of a table of 1.5 MB, which any L2 holds, 22, and 16 with bfloat16.
 template <typename T, int G, int W>
 __global__ __launch_bounds__(kThreads) void embed_bag_kernel(EmbedArgs a) {
   constexpr int groups = kThreads / G, U = G < 16 ? G : 16;
@@ -472,7 +474,7 @@ __device__ inline void sort_held(uint32_t (&held)[kFew],
 // place among all it learns from the count of lower remainders, and sorts them by the rest of the key
 // in one pass (tables below 2^16 entries) or two.  The other workgroups fill the table with zeros
 // meanwhile.  16,384 slots: 14 us, of which 8 are the walk over all slots and bound by instructions
-// (32 workgroups of 512 lanes: 22); beside 103 MB of zeros 22, at which those alone are 18.
+// (32 workgroups of 512 lanes: 22); beside 103 MB of zeros 21, at which those alone are 18.
 __global__ __launch_bounds__(kFewThreads) void embed_group_kernel(GradArgs a) {
   constexpr int waves = kFewThreads / 64, most = kFew / kFewThreads;
   __shared__ uint32_t held[kFew];  // rest of the key, place among the slots
@@ -528,8 +530,8 @@ __global__ __launch_bounds__(kFewThreads) void embed_group_kernel(GradArgs a) {
 // workgroup sorts each slot's pairs by their ids, in one pass (slots below 2^10 entries) or two.  Empty
 // slots stand behind their slot's others.  Neighbouring slots, whose ids share cache lines, go to one XCD.
 // Bound by the chain of steps within a workgroup, one a CU.  The whole gradient of 64 floats, this way / as
-// all pairs: 16,384 rows x 100 slots 78 us / 92, 4000 x 100 36 / 57, 300 x 100 17 / 41; many slots of few
-// rows leave most of a workgroup idle (40 x 4000 92 / 49).
+// all pairs: 16,384 rows x 100 slots 76 us / 90, 4000 x 100 35 / 57, 300 x 100 20 / 44; many slots of few
+// rows leave most of a workgroup idle (40 x 4000 89 / 50).
 __global__ __launch_bounds__(kFewThreads) void embed_slots_kernel(GradArgs a) {
   constexpr int waves = kFewThreads / 64, most = kFew / kFewThreads;
   __shared__ uint32_t held[kFew];  // id, row

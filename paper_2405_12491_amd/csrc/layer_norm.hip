@@ -52,8 +52,8 @@ struct RowLoads {
 // from which the mean's rest and the variance follow without cancellation.  Where a sum leaves
 // float's middle range (rows of huge or tiny elements, broken ones), or m is off by more than a quarter
 // of the deviation (elements 2^19 deviations and more from zero), both are taken in double.
-// Bound by memory: 8192 x 4096 bfloat16 with a residual and its total 45 us (5.9 TB/s, part of it stays in
-// the last cache), 1,000,000 x 28 float 50 (4.5 TB/s).
+// Bound by memory: 8192 x 4096 bfloat16 with a residual and its total 45 to 48 us (5.6 to 5.9 TB/s, part
+// of it stays in the last cache), 1,000,000 x 28 float with the statistics 47 (5.1 TB/s).
 template <typename T, int G, int C>
 __global__ __launch_bounds__(kRowThreads<G>) void layer_norm_kernel(LayerNormArgs a) {
   constexpr int V = kPerLoad<T>, W = G > 64 ? G / 64 : 1;
@@ -143,7 +143,8 @@ __global__ __launch_bounds__(kRowThreads<G>) void layer_norm_kernel(LayerNormArg
 }
 
 // Rows that do not fit a workgroup's registers: read once for the sum, once for the squares and
-// once for the norm, sums in double.
+// once for the norm, sums in double.  1000 x 40,000 bfloat16 60 to 65 us (2.6 TB/s; the second and third
+// read are the caches' for the most part: 197 MB fetched).
 constexpr int kLong = 1024;
 template <typename T>
 __global__ __launch_bounds__(kLong) void layer_norm_long_kernel(LayerNormArgs a) {
@@ -243,8 +244,8 @@ int launch_layer_norm(const LayerNormArgs &a, int32_t dtype, void *stream) {
 // and per column the sums of grad * h and of grad over the rows.  A workgroup takes every so many
 // rows; its lanes keep the sums of their columns in registers, and a second kernel adds the
 // workgroups' sums in their order: one read of the rows serves dx and both sums, and no atomics decide
-// their order.  Bound by memory: 8192 x 4096 bfloat16 with grad_total 53 us and the sums' 4.7 (5.1 TB/s),
-// 1,000,000 x 28 float 65 and 8.4 (5.2 TB/s).
+// their order.  Bound by memory: 8192 x 4096 bfloat16 with grad_total 51 us and the sums' 4.7 (5.2 TB/s),
+// 1,000,000 x 28 float 64 and 7.4 (5.4 TB/s).
 template <typename T, int G, int C>
 __global__ __launch_bounds__(kRowThreads<G>) void layer_norm_backward_kernel(LayerNormGradArgs a) {
   constexpr int V = kPerLoad<T>, W = G > 64 ? G / 64 : 1, slots = kRowsAWorkgroup<G>;
@@ -348,7 +349,8 @@ __global__ __launch_bounds__(kRowThreads<G>) void layer_norm_backward_kernel(Lay
     }
 }
 
-// Long rows: dx from two walks, a workgroup a row.
+// Long rows: dx from two walks, a workgroup a row.  1000 x 40,000 bfloat16 58 us, their columns' sums
+// 49, what joins those 8.6.
 template <typename T>
 __global__ __launch_bounds__(kLong) void layer_norm_backward_long_kernel(LayerNormGradArgs a) {
   constexpr int V = kPerLoad<T>, W = kLong / 64;

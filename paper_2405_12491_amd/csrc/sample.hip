@@ -200,7 +200,7 @@ __device__ inline void each_four(u32x4 raw, F f) {
 // A row's scores.  each(f): f(first class, 16 bytes of scores), in ascending order per lane, NaN past the
 // row's end; all lanes make the same number of calls.  Every walk reads the row again, from the caches,
 // with the next loads on their way while one is looked at: held in registers a long row leaves too few
-// of them for the rest (2048 x 128,000 bfloat16, top_k 50: 230 us, 285 from registers).  kRing loads
+// of them for the rest (2048 x 128,000 bfloat16, top_k 50: 221 to 241 us, 285 from registers).  kRing loads
 // take turns, written out; each_again() is for walks that few rows take.
 template <typename T, int G, int kRing>
 struct Scores {
@@ -390,7 +390,7 @@ struct Range {
 // One walk for a cut by quick weights: parts the scores of the range into bins of equal width, of which
 // those that may hold the cut are left.  The weights are added up as whole numbers, whose sums do not
 // depend on the order.  (512 x 50,257 float, top_p 0.95: 354 us with cut()'s bins alone, which take
-// several walks, 242 with this one first.)
+// several walks, 244 with this one first.)
 enum class Found { kRange, kUnclear, kPast };  // kPast: the whole range is less than the target
 template <typename T, int G, int A>
 __device__ inline Found narrow(const Scores<T, G, A> &x, SampleShared<G> &s, const Weights &weight,
@@ -946,9 +946,10 @@ __device__ inline void store_draw(const SampleArgs &a, int64_t row, const Sample
 
 // A workgroup of G lanes a row, with kRing loads on their way.  Many rows: few of them, in so few
 // registers that two workgroups of 1024 lanes share a compute unit and hide each other's waits, though some
-// registers spill (512 x 50,257 float, top_k 50: two loads 49 us, four 51, four with twice the registers 57;
-// top_p 0.95: 242, 258, 260; 2048 x 128,000 without cuts 682, 744, 776).  A row or two for each compute
-// unit: more (1 x 128,000 bfloat16: 22 us, 28).
+// registers spill (512 x 50,257 float, top_k 50: two loads 50 us, four 53, four with twice the registers 57;
+// top_p 0.95: 245, 256, 260; 2048 x 128,000 without cuts 682, 744, 776).  A row or two for each compute
+// unit: more, and twice the registers (1 x 128,000 bfloat16, top_k 50 and top_p 0.9: 25 us, with two loads
+// 27; top_p 0.95 148, 165).
 template <typename T, int G, int kRing>
 __global__ __launch_bounds__(G, G >= 512 && kRing < 8 ? 8 : 4) void sample_kernel(SampleArgs a) {
   __shared__ __attribute__((aligned(16))) SampleShared<G> s;
